@@ -171,6 +171,7 @@ def prepare(case, seed):
         s["penalties"] = {"repetition": 1.2, "presence": 0.3, "frequency": 0.05}
         s["out"] = torch.empty_like(s["logits"])
         s["choice"] = torch.empty(R, dtype=torch.int32, device="cuda")
+        s["workspace"] = torch.empty(1 << 16, device="cuda")
     return s
 
 
@@ -208,7 +209,8 @@ def _run_own(s):
     if kind == "counts":
         api.tl_k_token_counts(s["tokens"], s["counts"])
         return {"counts": s["counts"]}
-    api.tl_k_choose(s["logits"], s["counts"], s["out"], s["choice"], bias=s["bias"], allowed=s["allowed"], **s["penalties"])
+    api.tl_k_choose(s["logits"], s["counts"], s["out"], s["choice"], bias=s["bias"], allowed=s["allowed"],
+                    workspace=s["workspace"], **s["penalties"])
     return {"out": s["out"], "choice": s["choice"]}
 
 
