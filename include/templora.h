@@ -419,6 +419,61 @@ tl_status tl_k_attention_decode(const uint16_t* q, const uint16_t* k, const uint
                                 int32_t n_heads, int32_t d_head, uint16_t* o, float* workspace, size_t workspace_elems,
                                 void* hip_stream);
 tl_status tl_k_argmax(const float* x, int32_t n, int32_t* out, void* hip_stream);
+/*
+ * A key/value cache held in 8 bits, for generation over long texts (caller-owned device memory, 16-byte aligned).
+ * A block is 64 consecutive tokens.  A complete block holds, for each key/value head, int8 codes in [-127, 127] and one fp32 scale for
+ * its keys and one for its values:
+ *     scale = max(largest magnitude in the block, 2^-100) / 127 (rounded to fp32),   code = value / scale, to the nearest, ties to even;
+ * what it stands for is code * scale.  The tokens behind the last complete block stay bf16 in the tail until their block is complete:
+ * what a cache holds depends on the tokens alone and not on the calls that they came in.  A block with a value that is not finite has
+ * the scale NaN and stands for NaN throughout.  Places of tokens that are not cached yet are neither read nor need a value.
+ *   k      : int8 [n_blocks][n_kv_heads][d_head / 64][64 tokens][64 columns],   n_blocks = ceil(capacity / 64)
+ *   v      : int8 [n_blocks][n_kv_heads][d_head][64 tokens]
+ *   scales : fp32 [n_blocks][n_kv_heads]
+ *   tails  : bf16, laid out as one block of k and of v
+ * d_head 64 or 128.  The number of tokens cached (n_cached, n_keys) is the caller's to keep: append does not store it.
+ */
+typedef struct {
+    int8_t *k, *v;
+    float *k_scale, *v_scale;
+    uint16_t *k_tail, *v_tail;
+    int32_t n_kv_heads, d_head, capacity;   /* capacity: tokens */
+} tl_cache8_mem;
+/* Keys and values of n_new tokens, rows of [n_kv_heads * d_head] bf16 (row strides ldk, ldv in elements, first elements anywhere), become
+ * tokens n_cached .. n_cached + n_new - 1; n_cached tokens are there already (with n_cached not a multiple of 64 the tail holds the last of
+ * them, so a cache cannot be cut back into a block that has been completed).  TL_ERR_WINDOW beyond the capacity. */
+tl_status tl_k_cache8_append(const tl_cache8_mem* cache, int32_t n_cached, const uint16_t* k, int32_t ldk, const uint16_t* v, int32_t ldv,
+                             int32_t n_new, void* hip_stream);
+/* What a cache of n_cached tokens stands for, tokens first .. first + n - 1: fp32 rows of [n_kv_heads * d_head]. */
+tl_status tl_k_cache8_read(const tl_cache8_mem* cache, int32_t n_cached, int32_t first, int32_t n, float* k_out, int32_t ldk, float* v_out,
+                           int32_t ldv, void* hip_stream);
+/* Causal attention of the last n_rows of n_keys cached tokens (one row: a decoding step): row i of q (bf16 [n_rows, n_heads * d_head]) sees
+ * keys 0 .. n_keys - n_rows + i;  o = softmax(q K^T / sqrt(d_head)) V, bf16, K and V what the cache stands for.  n_heads is a multiple
+ * of n_kv_heads; query head j reads key head j / (n_heads / n_kv_heads).  n_rows <= n_keys.
+ * workspace: NULL, or device fp32 scratch of workspace_elems floats: with it the keys are cut into up to 64 ranges where the rows are few,
+ * n_rows * n_heads * ranges * (d_head + 2) floats are used; contents are undefined before and after, and calls that overlap in time need one
+ * each.  tl_k_attention_cache8_plan: the name of the kernel that these sizes get ("columns", ..), its ranges and the floats that it uses of a
+ * workspace of workspace_elems floats (host only). */
+tl_status tl_k_attention_cache8(const tl_cache8_mem* cache, int32_t n_keys, const uint16_t* q, int32_t ldq, int32_t n_rows, int32_t n_heads,
+                                uint16_t* o, int32_t ldo, float* workspace, size_t workspace_elems, void* hip_stream);
+tl_status tl_k_attention_cache8_plan(int32_t n_keys, int32_t n_rows, int32_t n_heads, int32_t n_kv_heads, int32_t d_head,
+                                     size_t workspace_elems, char* name_out, size_t name_cap, int32_t* n_ranges_out, size_t* elems_out);
+/* How often each token of the vocabulary is in a row of a text: tokens device int32 [rows, n] (row stride ldt), counts device int32
+ * [rows, vocab] (row stride ldc).  add = 0: counts are set; add = 1: added to; add = -1: taken away from (a history that slides).  Ids
+ * outside [0, vocab) are passed over, so rows of different lengths are filled up with -1. */
+tl_status tl_k_token_counts(const int32_t* tokens, int32_t ldt, int32_t rows, int32_t n, int32_t vocab, int32_t add, int32_t* counts,
+                            int32_t ldc, void* hip_stream);
+/* Penalties, a bias and a mask on logits (fp32 [rows, vocab]), and the greedy choice:  for a token with count > 0
+ *     x = x > 0 ? x / repetition : x * repetition;   x = x - (frequency * count + presence);
+ * then x = x + bias, each step rounded to fp32; a token whose bit of `allowed` (bit t % 32 of word t / 32 of a row) is 0 gets -infinity.
+ *   counts (int32), bias (fp32), allowed (uint32, ceil(vocab / 32) words a row): device, each may be NULL; a row stride of 0 means one row
+ *   for all.  out (fp32 [rows, vocab], may be NULL or the logits themselves) receives the values, choice (int32 [rows], may be NULL) the index
+ *   of the largest among the allowed tokens, the lowest index among equals, values that are NaN passed over; -1 if there is none.
+ * workspace: NULL, or device fp32 scratch (2 * rows * ceil(vocab / 1024) floats are enough): with it a row is cut into pieces, so that few rows
+ * fill the GPU; calls that overlap in time need one each. */
+tl_status tl_k_choose(const float* logits, int32_t ldl, int32_t rows, int32_t vocab, const int32_t* counts, int32_t ldc, float repetition,
+                      float presence, float frequency, const float* bias, int32_t ldb, const uint32_t* allowed, int32_t lda, float* out,
+                      int32_t ldo, int32_t* choice, float* workspace, size_t workspace_elems, void* hip_stream);
 /* dgu bf16 [T, 2f] from da bf16 [T, f] and gu. */
 tl_status tl_k_swiglu_bwd(const uint16_t* da, const uint16_t* gu, int32_t T, int32_t f, uint16_t* dgu,
                           void* hip_stream);

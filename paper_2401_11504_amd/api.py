@@ -57,6 +57,11 @@ class tl_generate_cfg(C.Structure):
     _fields_ = [("window", C.c_int32), ("chunk", C.c_int32), ("train", tl_train_cfg)]
 
 
+class tl_cache8_mem(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("k_tail", C.c_void_p),
+                ("v_tail", C.c_void_p), ("n_kv_heads", C.c_int32), ("d_head", C.c_int32), ("capacity", C.c_int32)]
+
+
 _vp, _i32, _i64, _f32, _sz = C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_size_t
 _SIGS = {
     "tl_model_create": [C.POINTER(tl_model_cfg), C.POINTER(_vp), _vp, C.POINTER(_vp)],
@@ -103,6 +108,12 @@ _SIGS = {
     "tl_k_gemv_pre": [_vp, _i32, _i32, _i32, _i32, _vp, _vp, _f32, _vp, _vp, _vp, _vp],
     "tl_k_attention_decode": [_vp, _vp, _vp, _i32, _i32, _i32, _i32, _vp, _vp, _sz, _vp],
     "tl_k_argmax": [_vp, _i32, _vp, _vp],
+    "tl_k_cache8_append": [C.POINTER(tl_cache8_mem), _i32, _vp, _i32, _vp, _i32, _i32, _vp],
+    "tl_k_cache8_read": [C.POINTER(tl_cache8_mem), _i32, _i32, _i32, _vp, _i32, _vp, _i32, _vp],
+    "tl_k_attention_cache8": [C.POINTER(tl_cache8_mem), _i32, _vp, _i32, _i32, _i32, _vp, _i32, _vp, _sz, _vp],
+    "tl_k_attention_cache8_plan": [_i32] * 5 + [_sz, C.c_char_p, _sz, C.POINTER(_i32), C.POINTER(_sz)],
+    "tl_k_token_counts": [_vp, _i32, _i32, _i32, _i32, _i32, _vp, _i32, _vp],
+    "tl_k_choose": [_vp, _i32, _i32, _i32, _vp, _i32, _f32, _f32, _f32, _vp, _i32, _vp, _i32, _vp, _i32, _vp, _vp, _sz, _vp],
     "tl_k_attention_fwd": [_vp, _vp, _vp, _i32, _i32, _i32, _i32, _vp, _i32, _vp, _vp],
     "tl_k_attention_bwd": [_vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp],
     "tl_k_cross_entropy": [_vp, _vp, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp],
@@ -442,6 +453,94 @@ def tl_k_attention_decode(q, k, v, n_heads, d_head, o, workspace=None, stream=No
 
 def tl_k_argmax(x, out, stream=None):
     _chk(_lib.tl_k_argmax(_dp(x), x.numel(), _dp(out), _s(stream)))
+
+
+class Cache8:
+    """The memory of a key/value cache held in 8 bits (tl_cache8_mem in the header): six device tensors, kept alive here.
+    k int8 [n_blocks, heads, d_head / 64, 64, 64], v int8 [n_blocks, heads, d_head, 64], scales fp32 [n_blocks, heads], tails bf16 as one block."""
+
+    def __init__(self, k, v, k_scale, v_scale, k_tail, v_tail, capacity):
+        nb, heads, d = v.shape[:3]
+        want = {"k": ((nb, heads, d // 64, 64, 64), torch.int8), "v": ((nb, heads, d, 64), torch.int8),
+                "k_scale": ((nb, heads), torch.float32), "v_scale": ((nb, heads), torch.float32),
+                "k_tail": ((heads, d // 64, 64, 64), torch.bfloat16), "v_tail": ((heads, d, 64), torch.bfloat16)}
+        self.tensors = dict(k=k, v=v, k_scale=k_scale, v_scale=v_scale, k_tail=k_tail, v_tail=v_tail)
+        for name, (shape, dtype) in want.items():
+            t = self.tensors[name]
+            assert t.is_cuda and t.is_contiguous() and tuple(t.shape) == shape and t.dtype == dtype, f"{name}: {dtype} {shape} expected"
+        assert 0 < capacity <= 64 * nb, "capacity beyond the blocks"
+        self.n_kv_heads, self.d_head, self.capacity = heads, d, capacity
+        self._mem = tl_cache8_mem(*[self.tensors[n].data_ptr() for n in want], heads, d, capacity)
+        self._ref = C.byref(self._mem)
+
+    @classmethod
+    def empty(cls, n_kv_heads, d_head, capacity, device="cuda"):
+        nb = -(-capacity // 64)
+        new = lambda dtype, *shape: torch.empty(shape, dtype=dtype, device=device)  # noqa: E731
+        return cls(new(torch.int8, nb, n_kv_heads, d_head // 64, 64, 64), new(torch.int8, nb, n_kv_heads, d_head, 64),
+                   new(torch.float32, nb, n_kv_heads), new(torch.float32, nb, n_kv_heads),
+                   new(torch.bfloat16, n_kv_heads, d_head // 64, 64, 64), new(torch.bfloat16, n_kv_heads, d_head, 64), capacity)
+
+
+def _rows(t, dtype, width):
+    assert t.dim() == 2 and t.dtype == dtype and t.shape[1] == width, f"{dtype} [n, {width}] expected"
+    return t
+
+
+def tl_k_cache8_append(cache, n_cached, k, v, stream=None):
+    """k, v bf16 [n_new, n_kv_heads * d_head] -> tokens n_cached .. of the cache"""
+    w = cache.n_kv_heads * cache.d_head
+    _rows(k, torch.bfloat16, w), _rows(v, torch.bfloat16, w)
+    assert k.shape == v.shape
+    _chk(_lib.tl_k_cache8_append(cache._ref, n_cached, _dp(k), k.stride(0), _dp(v), v.stride(0), k.shape[0], _s(stream)))
+
+
+def tl_k_cache8_read(cache, n_cached, first, k_out, v_out, stream=None):
+    """k_out, v_out fp32 [n, n_kv_heads * d_head] <- what the cache stands for, tokens first .. first + n - 1"""
+    w = cache.n_kv_heads * cache.d_head
+    _rows(k_out, torch.float32, w), _rows(v_out, torch.float32, w)
+    assert k_out.shape == v_out.shape
+    _chk(_lib.tl_k_cache8_read(cache._ref, n_cached, first, k_out.shape[0], _dp(k_out), k_out.stride(0), _dp(v_out), v_out.stride(0), _s(stream)))
+
+
+def tl_k_attention_cache8(cache, n_keys, q, o, n_heads, workspace=None, stream=None):
+    """q, o bf16 [n_rows, n_heads * d_head], the last n_rows of n_keys cached tokens"""
+    w = n_heads * cache.d_head
+    _rows(q, torch.bfloat16, w), _rows(o, torch.bfloat16, w)
+    assert q.shape == o.shape
+    _chk(_lib.tl_k_attention_cache8(cache._ref, n_keys, _dp(q), q.stride(0), q.shape[0], n_heads, _dp(o), o.stride(0), _dp(workspace),
+                                    workspace.numel() if workspace is not None else 0, _s(stream)))
+
+
+def tl_k_attention_cache8_plan(n_keys, n_rows, n_heads, n_kv_heads, d_head, workspace_elems=0):
+    """-> (name of the kernel, ranges of keys, floats used of the workspace)"""
+    buf, n, elems = C.create_string_buffer(32), _i32(0), _sz(0)
+    _chk(_lib.tl_k_attention_cache8_plan(n_keys, n_rows, n_heads, n_kv_heads, d_head, workspace_elems, buf, 32, C.byref(n), C.byref(elems)))
+    return buf.value.decode(), n.value, elems.value
+
+
+def tl_k_token_counts(tokens, counts, add=0, stream=None):
+    """tokens int32 [rows, n], counts int32 [rows, vocab]; add 0: set, 1: add, -1: take away"""
+    assert tokens.dim() == counts.dim() == 2 and tokens.shape[0] == counts.shape[0] and tokens.dtype == counts.dtype == torch.int32
+    _chk(_lib.tl_k_token_counts(_dp(tokens), tokens.stride(0), tokens.shape[0], tokens.shape[1], counts.shape[1], add, _dp(counts),
+                                counts.stride(0), _s(stream)))
+
+
+def tl_k_choose(logits, counts, out, choice, repetition=1.0, presence=0.0, frequency=0.0, bias=None, allowed=None, workspace=None, stream=None):
+    """logits fp32 [rows, vocab]; counts int32 and bias fp32 [rows, vocab] or [vocab], allowed int32 words of 32 bits, [rows, ceil(vocab / 32)] or
+    one row, each or None; out fp32 like logits or None, choice int32 [rows] or None"""
+    R, V = logits.shape
+
+    def row(t, dtype, width):
+        if t is None:
+            return None, 0
+        assert t.dtype == dtype and t.shape[-1] == width and (t.dim() == 1 or tuple(t.shape) == (R, width)), f"{dtype} [{R}, {width}] expected"
+        return _dp(t), t.stride(0) if t.dim() == 2 else 0
+
+    assert logits.dtype == torch.float32 and (choice is None or (choice.dtype == torch.int32 and choice.numel() == R))
+    _chk(_lib.tl_k_choose(*row(logits, torch.float32, V), R, V, *row(counts, torch.int32, V), repetition, presence, frequency,
+                          *row(bias, torch.float32, V), *row(allowed, torch.int32, (V + 31) // 32), *row(out, torch.float32, V), _dp(choice),
+                          _dp(workspace), workspace.numel() if workspace is not None else 0, _s(stream)))
 
 
 def tl_k_attention_fwd(q, k, v, n_heads, d_head, o, lse, stream=None):

@@ -1,0 +1,435 @@
+// The key/value cache held in 8 bits, and attention over it (generation side).
+//
+// A block is 64 consecutive tokens.  Once complete it is stored, head by head, as int8 codes with one fp32 scale for its keys and one
+// for its values:  scale = max(largest magnitude, 2^-100) / 127,  code = value / scale rounded to the nearest, ties to even.  The
+// tokens of the block that is not complete yet stay bf16 in the tail, so what the cache holds is a function of the tokens alone, not
+// of the calls that they arrived in, and no value is ever rounded twice.
+// Keys lie as [block][head][D / 64][64 tokens][64 columns], values as [block][head][D][64 tokens] (transposed): both are contiguous
+// 1 KB runs for a wave that loads matrix operands of 16 codes a lane straight from memory, and neither has to be transposed there.
+#include <algorithm>
+
+#include "kernels.h"
+
+static constexpr float kLeastMagnitude = 7.888609052210118e-31f;   // 2^-100: keeps the scale and its reciprocal normal numbers
+
+// x / s rounded to the nearest integer, ties to even, exactly, for |x| <= 127 s (1 + 2^-24) and `inv` within a few ulp of 1 / s:
+// x * inv is off by far less than 1, so its rounding n is the answer or next to it, and the remainder x - n s is exact in fp32 (x is a
+// bf16 of at least s / 2, a multiple of s's last place; the remainder is below s).
+__device__ __forceinline__ int code8(float x, float s, float inv) {
+    const float n = rintf(x * inv);
+    const float r = fmaf(-n, s, x), half = 0.5f * s;
+    const int i = (int)n, odd = i & 1;
+    const int up = r > half || (r == half && odd), down = r < -half || (r == -half && odd);
+    return i + up - down;
+}
+
+// Threads of a workgroup share a tile of 64 tokens of one head: keys by rows (thread: 8 columns of every STEP-th token), values by
+// columns (thread: two columns of TPT consecutive tokens), each as it is stored.
+template <int D>
+struct Cache8Tile {
+    static constexpr int CPR = D / 8, STEP = 256 / CPR, NK = 64 / STEP;     // keys: chunks a row, tokens a pass, passes
+    static constexpr int NG = 256 / (D / 2), TPT = 64 / NG;                 // values: token groups, tokens a thread
+};
+
+// One workgroup for a block that the new tokens complete and a head's keys or values (block by block, the heads' keys before their
+// values).  Those of the first block also put the rows behind the last complete block into the tail, after they have read the tail.
+template <int D>
+__global__ __launch_bounds__(256) void cache8_append_kernel(Cache8 c, int n_cached, const bf16_t* __restrict__ k, long ldk,
+                                                            const bf16_t* __restrict__ v, long ldv, int n_new) {
+    using T = Cache8Tile<D>;
+    __shared__ int red[4];
+    const int tid = threadIdx.x, at = blockIdx.x % (2 * c.heads), nth = blockIdx.x / (2 * c.heads);
+    const bool values = at >= c.heads;
+    const int head = values ? at - c.heads : at;
+    const int b0 = n_cached >> 6, end = n_cached + n_new, b1 = end >> 6, block = b0 + nth;
+    const int first = block << 6;                          // position of the tile's first token
+    const bf16_t* src = (values ? v : k) + (long)head * D;
+    const long ld = values ? ldv : ldk;
+    bf16_t* tail = (values ? c.vt : c.kt) + (long)head * 64 * D;
+    const long tile = ((long)block * c.heads + head) * 64 * D;
+    const int kc = tid % T::CPR * 8, kt = tid / T::CPR;                     // keys: first column, first token
+    const int vc = tid % (D / 2) * 2, vt = tid / (D / 2) * T::TPT;          // values: first column, first token
+    auto finish = [&](int amax) {                          // bf16 bits of the largest magnitude -> the scale
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) amax = max(amax, __shfl_xor(amax, off, 64));
+        if ((tid & 63) == 0) red[tid >> 6] = amax;
+        __syncthreads();
+        amax = max(max(red[0], red[1]), max(red[2], red[3]));
+        // a value that is not finite has no code: the scale is NaN, and so is everything read through it
+        const float s = amax >= 0x7f80 ? __builtin_nanf("") : fmaxf(__uint_as_float((unsigned)amax << 16), kLeastMagnitude) / 127.f;
+        if (tid == 0) (values ? c.vs : c.ks)[(long)block * c.heads + head] = s;
+        return s;
+    };
+    if (block < b1) {
+        if (!values) {
+            uint4 x[T::NK];
+#pragma unroll
+            for (int i = 0; i < T::NK; ++i) {
+                const int t = kt + i * T::STEP;
+                x[i] = first + t < n_cached ? *(const uint4*)(tail + (kc >> 6) * 4096 + t * 64 + (kc & 63))
+                                            : *(const uint4*)(src + (long)(first + t - n_cached) * ld + kc);
+            }
+            int amax = 0;
+#pragma unroll
+            for (int i = 0; i < T::NK; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const unsigned w = (&x[i].x)[e];
+                    amax = max(amax, max((int)(w & 0x7fff), (int)(w >> 16 & 0x7fff)));
+                }
+            const float s = finish(amax), inv = 1.f / s;
+#pragma unroll
+            for (int i = 0; i < T::NK; ++i) {
+                float f[8];
+                unpack8(x[i], f);
+                unsigned w[2] = {0, 0};
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w[e >> 2] |= (unsigned)(s == s ? code8(f[e], s, inv) & 255 : 0) << 8 * (e & 3);
+                *(uint2*)(c.k + tile + (kc >> 6) * 4096 + (kt + i * T::STEP) * 64 + (kc & 63)) = make_uint2(w[0], w[1]);
+            }
+        } else {
+            unsigned x[T::TPT];                            // columns vc, vc + 1
+#pragma unroll
+            for (int i = 0; i < T::TPT; ++i) {
+                const int t = vt + i;
+                x[i] = first + t < n_cached ? (unsigned)tail[vc * 64 + t] | (unsigned)tail[vc * 64 + 64 + t] << 16
+                                            : *(const unsigned*)(src + (long)(first + t - n_cached) * ld + vc);
+            }
+            int amax = 0;
+#pragma unroll
+            for (int i = 0; i < T::TPT; ++i) amax = max(amax, max((int)(x[i] & 0x7fff), (int)(x[i] >> 16 & 0x7fff)));
+            const float s = finish(amax), inv = 1.f / s;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                unsigned w[T::TPT / 4];
+#pragma unroll
+                for (int i = 0; i < T::TPT; ++i) {
+                    const float f = __uint_as_float(j ? x[i] & 0xffff0000u : x[i] << 16);
+                    const unsigned q = (unsigned)(s == s ? code8(f, s, inv) & 255 : 0) << 8 * (i & 3);
+                    w[i >> 2] = i & 3 ? w[i >> 2] | q : q;
+                }
+#pragma unroll
+                for (int i = 0; i < T::TPT / 4; i += 2)
+                    *(uint2*)(c.v + tile + (vc + j) * 64 + vt + 4 * i) = make_uint2(w[i], w[i + 1]);
+            }
+        }
+        __syncthreads();                                   // (uniform) every wave has what it needs of the tail
+    }
+    if (nth > 0) return;
+    const int base = b1 << 6, lo = max(n_cached, base);    // the new rows of the block that stays incomplete
+    if (!values) {
+        for (int t = lo - base + kt; t < end - base; t += T::STEP)
+            *(uint4*)(tail + (kc >> 6) * 4096 + t * 64 + (kc & 63)) = *(const uint4*)(src + (long)(base + t - n_cached) * ld + kc);
+    } else {
+        for (int t = max(vt, lo - base); t < min(vt + T::TPT, end - base); ++t) {
+            const unsigned w = *(const unsigned*)(src + (long)(base + t - n_cached) * ld + vc);
+            tail[vc * 64 + t] = (bf16_t)w;
+            tail[vc * 64 + 64 + t] = (bf16_t)(w >> 16);
+        }
+    }
+}
+hipError_t launch_cache8_append(const Cache8& c, int n_cached, const bf16_t* k, long ldk, const bf16_t* v, long ldv, int n_new,
+                                hipStream_t s) {
+    // at most 2^19 tokens a launch, for the grid's sake; the cache does not depend on where a text is cut
+    for (int i = 0; i < n_new;) {
+        const int m = min(n_new - i, 1 << 19), at = n_cached + i, done = ((at + m) >> 6) - (at >> 6);
+        const int grid = 2 * c.heads * (done > 1 ? done : 1);
+        const bf16_t *ki = k + (long)i * ldk, *vi = v + (long)i * ldv;
+        if (c.d == 128) cache8_append_kernel<128><<<grid, 256, 0, s>>>(c, at, ki, ldk, vi, ldv, m);
+        else cache8_append_kernel<64><<<grid, 256, 0, s>>>(c, at, ki, ldk, vi, ldv, m);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        i += m;
+    }
+    return hipSuccess;
+}
+
+// Tokens first .. first + n - 1 of a cache that holds n_cached as fp32 rows: code * scale (one rounding), the tail's widened.
+template <int D>
+__global__ __launch_bounds__(256) void cache8_read_kernel(Cache8 c, int n_cached, int first, int n, float* __restrict__ k, long ldk,
+                                                          float* __restrict__ v, long ldv) {
+    using T = Cache8Tile<D>;
+    const int tid = threadIdx.x, at = blockIdx.x % (2 * c.heads), block = (first >> 6) + blockIdx.x / (2 * c.heads);
+    const bool values = at >= c.heads, in_tail = block == n_cached >> 6;
+    const int head = values ? at - c.heads : at, base = block << 6;
+    const long tile = ((long)block * c.heads + head) * 64 * D;
+    const bf16_t* tail = (values ? c.vt : c.kt) + (long)head * 64 * D;
+    const float s = in_tail ? 1.f : (values ? c.vs : c.ks)[(long)block * c.heads + head];
+    if (!values) {
+        const int kc = tid % T::CPR * 8, kt = tid / T::CPR;
+#pragma unroll
+        for (int i = 0; i < T::NK; ++i) {
+            const int t = kt + i * T::STEP, row = base + t - first, off = (kc >> 6) * 4096 + t * 64 + (kc & 63);
+            if (row < 0 || row >= n) continue;
+            float f[8];
+            if (in_tail) unpack8(*(const uint4*)(tail + off), f);
+            else {
+                const uint2 w = *(const uint2*)(c.k + tile + off);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[e] = (float)(int8_t)((e < 4 ? w.x : w.y) >> 8 * (e & 3)) * s;
+            }
+            float* out = k + (long)row * ldk + (long)head * D + kc;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) out[e] = f[e];
+        }
+    } else {
+        const int vc = tid % (D / 2) * 2, vt = tid / (D / 2) * T::TPT;
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int i = 0; i < T::TPT; ++i) {
+                const int row = base + vt + i - first, off = (vc + j) * 64 + vt + i;
+                if (row < 0 || row >= n) continue;
+                v[(long)row * ldv + (long)head * D + vc + j] = in_tail ? bf16_to_f32(tail[off]) : (float)c.v[tile + off] * s;
+            }
+    }
+}
+hipError_t launch_cache8_read(const Cache8& c, int n_cached, int first, int n, float* k, long ldk, float* v, long ldv, hipStream_t s) {
+    for (int i = 0; i < n;) {
+        const int at = first + i, m = min(n - i, (1 << 19) - (at & 63));      // pieces end where blocks do
+        const int grid = 2 * c.heads * (((at + m - 1) >> 6) - (at >> 6) + 1);
+        float *ki = k + (long)i * ldk, *vi = v + (long)i * ldv;
+        if (c.d == 128) cache8_read_kernel<128><<<grid, 256, 0, s>>>(c, n_cached, at, m, ki, ldk, vi, ldv);
+        else cache8_read_kernel<64><<<grid, 256, 0, s>>>(c, n_cached, at, m, ki, ldk, vi, ldv);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        i += m;
+    }
+    return hipSuccess;
+}
+
+// ---------------------------------------------------------------- attention of a few rows
+// A row of queries and one of the query heads that share a key head make a column; 16 columns of one key head are a workgroup's, and
+// each of its four waves takes every fourth block of the workgroup's range of the cache:
+//   S^T[key][column] = K q^T   and   O^T[d][column] += V^T P^T     by v_mfma_f32_16x16x32_bf16
+// (lane = 16 g + m:  A: row m, contraction slots 8 g ..;  B: column m, the same slots;  D: column m, rows 4 g .. 4 g + 3).  Codes are
+// whole numbers up to 127, exact in bf16, so the scores are products of what is stored, summed in fp32, and the scales come in behind:
+// the keys' with the softmax scale, the values' with the probabilities.  Those are split into two bf16 parts, so that they are rounded
+// to 16 bits of mantissa (the matrix unit has nothing else to do here).  Row m of key group kg is key 16 (m / 4) + 4 kg + m % 4: lane
+// group g then holds the scores of keys 16 g .. 16 g + 15, which are the slots it has to bring as the second product's operand and the
+// values it loads as 16 bytes of a row of V^T; nothing is exchanged between lanes but the maximum and the sum.
+__device__ __forceinline__ f32x4_t mfma16(bf16x8_t a, bf16x8_t b, f32x4_t c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+// eight codes -> bf16
+__device__ __forceinline__ bf16x8_t codes_bf16(unsigned lo, unsigned hi) {
+    bf16x8_t r;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = (__bf16)(float)(int8_t)((e < 4 ? lo : hi) >> 8 * (e & 3));
+    return r;
+}
+// eight bf16 of a tail's value row from slot u0 on, zero from slot `end` on; *odd: whether one that stays is not finite
+__device__ __forceinline__ uint4 tail_values(const bf16_t* row, int u0, int end, bool* odd) {
+    uint4 w = *(const uint4*)(row + u0);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        unsigned& x = (&w.x)[e];
+        if (u0 + 2 * e >= end) x = 0;
+        else if (u0 + 2 * e + 1 >= end) x &= 0xffffu;
+        *odd |= (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u;
+    }
+    return w;
+}
+
+template <int D>
+__global__ __launch_bounds__(256) void attn8_cols_kernel(Cache8 c, int n_keys, const bf16_t* __restrict__ q, long ldq, int n_rows, int group,
+                                                         float scale_log2e, bf16_t* __restrict__ o, long ldo, float* __restrict__ ws,
+                                                         int blocks_per_split) {
+    constexpr int PC = D / 64, NT = D / 16, LDP = D + 4;
+    __shared__ float part[4][16][LDP];                     // a column's output, maximum and sum, wave by wave
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m16 = lane & 15, g = lane >> 4;
+    const int head = blockIdx.x, c0 = blockIdx.y * 16, n_cols = n_rows * group, heads = c.heads * group;
+    const int col = min(c0 + m16, n_cols - 1), row = col / group, seen = n_keys - n_rows + row + 1;      // keys 0 .. seen - 1
+    const int least = n_keys - n_rows + c0 / group + 1;                                                  // the first column's
+    const int most = n_keys - n_rows + min(c0 + 15, n_cols - 1) / group + 1;                             // the last column's
+    const int b_end = min((int)(blockIdx.z + 1) * blocks_per_split, (most + 63) >> 6);
+    const bf16_t* qr = q + (long)row * ldq + (long)(head * group + col % group) * D + g * 16;
+    bf16x8_t qf[2 * PC];
+#pragma unroll
+    for (int st = 0; st < 2 * PC; ++st) qf[st] = __builtin_bit_cast(bf16x8_t, *(const uint4*)(qr + (st >> 1) * 64 + (st & 1) * 8));
+
+    f32x4_t oacc[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) oacc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, l = 0.f;
+    for (int b = blockIdx.z * blocks_per_split + wave; b < b_end; b += 4) {
+        const bool tail = b == n_keys >> 6;
+        f32x4_t s[4];
+        uint4 vr[NT];
+        float ks = scale_log2e, vs = 1.f;
+        const long tile = ((long)b * c.heads + head) * 64 * D;
+        const int key0 = (m16 >> 2) * 16 + (m16 & 3);
+        if (!tail) {
+            uint4 kr[4][PC];
+#pragma unroll
+            for (int kg = 0; kg < 4; ++kg)
+#pragma unroll
+                for (int pc = 0; pc < PC; ++pc) kr[kg][pc] = *(const uint4*)(c.k + tile + pc * 4096 + (key0 + kg * 4) * 64 + g * 16);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) vr[t] = *(const uint4*)(c.v + tile + (t * 16 + m16) * 64 + g * 16);
+            ks *= c.ks[(long)b * c.heads + head];
+            vs = c.vs[(long)b * c.heads + head];
+#pragma unroll
+            for (int kg = 0; kg < 4; ++kg) {
+                s[kg] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int pc = 0; pc < PC; ++pc) {
+                    s[kg] = mfma16(codes_bf16(kr[kg][pc].x, kr[kg][pc].y), qf[2 * pc], s[kg]);
+                    s[kg] = mfma16(codes_bf16(kr[kg][pc].z, kr[kg][pc].w), qf[2 * pc + 1], s[kg]);
+                }
+            }
+        } else {
+            const bf16_t* kt = c.kt + (long)head * 64 * D;
+#pragma unroll
+            for (int kg = 0; kg < 4; ++kg) {
+                s[kg] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int st = 0; st < 2 * PC; ++st)
+                    s[kg] = mfma16(__builtin_bit_cast(bf16x8_t, *(const uint4*)(kt + (st >> 1) * 4096 + (key0 + kg * 4) * 64 + g * 16 + (st & 1) * 8)),
+                                   qf[st], s[kg]);
+            }
+        }
+        const bool masked = (b + 1) * 64L > least;         // (uniform) some column does not see all of the block
+        const bool sees = (long)b * 64 < seen;
+        float x[16], top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            x[i] = s[i >> 2][i & 3] * ks;
+            if (masked && b * 64 + g * 16 + i >= seen) x[i] = -INFINITY;
+            top = fmaxf(top, x[i]);
+        }
+        top = fmaxf(top, __shfl_xor(top, 16, 64));
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        const float mn = fmaxf(m, top), base = mn == -INFINITY ? 0.f : mn, alpha = __builtin_amdgcn_exp2f(m - base);
+        m = mn;
+        l *= alpha;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            x[i] = __builtin_amdgcn_exp2f(x[i] - base);
+            l += x[i];
+            x[i] = sees ? x[i] * vs : 0.f;                 // (a block that it does not see may have the scale NaN)
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) oacc[t] *= alpha;
+        bf16x8_t hi[2], lo[2];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            hi[i >> 3][i & 7] = (__bf16)x[i];
+            lo[i >> 3][i & 7] = (__bf16)(x[i] - (float)hi[i >> 3][i & 7]);
+        }
+        if (!tail) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const bf16x8_t a0 = codes_bf16(vr[t].x, vr[t].y), a1 = codes_bf16(vr[t].z, vr[t].w);
+                oacc[t] = mfma16(a0, hi[0], oacc[t]);
+                oacc[t] = mfma16(a1, hi[1], oacc[t]);
+                oacc[t] = mfma16(a0, lo[0], oacc[t]);
+                oacc[t] = mfma16(a1, lo[1], oacc[t]);
+            }
+        } else {
+            const bf16_t* vt = c.vt + (long)head * 64 * D;
+            const int end = n_keys & 63;
+            bool odd = false;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) (void)tail_values(vt + (t * 16 + m16) * 64, g * 16 + h * 8, end, &odd);
+            if (!__builtin_amdgcn_ballot_w64(odd)) {
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const bf16x8_t a = __builtin_bit_cast(bf16x8_t, tail_values(vt + (t * 16 + m16) * 64, g * 16 + h * 8, end, &odd));
+                        oacc[t] = mfma16(a, hi[h], oacc[t]);
+                        oacc[t] = mfma16(a, lo[h], oacc[t]);
+                    }
+            } else {
+                // a value that is not finite counts for the columns that see it alone, which a product with zeros does not give
+                float* pl = &part[wave][0][0];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) pl[(g * 16 + i) * 16 + m16] = x[i];
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+                for (int u = 0; u < end && b * 64 + u < seen; ++u) {
+                    const float p = pl[u * 16 + m16];
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) oacc[t][i] = fmaf(p, bf16_to_f32(vt[(t * 16 + g * 4 + i) * 64 + u]), oacc[t][i]);
+                }
+                __builtin_amdgcn_wave_barrier();
+            }
+        }
+    }
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) *(f32x4_t*)&part[wave][m16][t * 16 + g * 4] = oacc[t];
+    if (g == 0) { part[wave][m16][D] = m; part[wave][m16][D + 1] = l; }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 16 * D; i += 256) {
+        const int cc = i / D, e = i % D;
+        if (c0 + cc >= n_cols) break;
+        float mt = part[0][cc][D];
+#pragma unroll
+        for (int w = 1; w < 4; ++w) mt = fmaxf(mt, part[w][cc][D]);
+        const float base = mt == -INFINITY ? 0.f : mt;     // (of a range that the column sees nothing of)
+        float lt = 0.f, ot = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float a = __builtin_amdgcn_exp2f(part[w][cc][D] - base);
+            lt += a * part[w][cc][D + 1];
+            ot += a * part[w][cc][e];
+        }
+        const int r = (c0 + cc) / group, qh = head * group + (c0 + cc) % group;
+        if (!ws) o[(long)r * ldo + (long)qh * D + e] = f32_to_bf16(ot / lt);
+        else {
+            float* out = ws + (((long)r * heads + qh) * gridDim.z + blockIdx.z) * (D + 2);
+            out[e] = ot;
+            if (e == 0) { out[D] = mt; out[D + 1] = lt; }
+        }
+    }
+}
+
+// The ranges of a row and head, one thread a column: lane i holds range i's maximum and sum.
+template <int D>
+__global__ __launch_bounds__(D) void attn8_join_kernel(const float* __restrict__ ws, int n_split, int heads, bf16_t* __restrict__ o, long ldo) {
+    const int e = threadIdx.x, lane = threadIdx.x & 63;
+    const float* w = ws + (long)blockIdx.x * n_split * (D + 2);
+    const int r = min(lane, n_split - 1);
+    const float m = lane < n_split ? w[r * (D + 2) + D] : -INFINITY, l = w[r * (D + 2) + D + 1];
+    const float top = wave_max(m), a = __builtin_amdgcn_exp2f(m - top);      // (one range has keys: top is a number, or NaN)
+    const float sum = wave_sum(lane < n_split ? a * l : 0.f);
+    float acc = 0.f;
+    for (int i = 0; i < n_split; ++i) acc += __shfl(a, i, 64) * w[i * (D + 2) + e];
+    o[(long)(blockIdx.x / heads) * ldo + (long)(blockIdx.x % heads) * D + e] = f32_to_bf16(acc / sum);
+}
+
+struct Attn8Plan { int n_split, per; };       // ranges, blocks a range
+static Attn8Plan attn8_plan(int n_keys, int n_rows, int heads, int kv_heads, int d, size_t ws_elems) {
+    const int nb = cdiv(n_keys, 64), units = kv_heads * cdiv((long)n_rows * (heads / kv_heads), 16);
+    long n = std::min<long>(std::min<long>(512 / units, ATTN8_MAX_SPLIT), cdiv(nb, 4));
+    n = std::min<long>(n, (long)(ws_elems / ((size_t)n_rows * heads * (d + 2))));
+    if (n < 2) return {1, nb};
+    const int per = cdiv(nb, n);
+    return {cdiv(nb, per), per};
+}
+const char* attention_cache8_plan(int n_keys, int n_rows, int heads, int kv_heads, int d, size_t ws_elems, int* n_ranges) {
+    *n_ranges = attn8_plan(n_keys, n_rows, heads, kv_heads, d, ws_elems).n_split;
+    return "columns";
+}
+hipError_t launch_attention_cache8(const Cache8& c, int n_keys, const bf16_t* q, long ldq, int n_rows, int heads, bf16_t* o, long ldo,
+                                   float* ws, size_t ws_elems, hipStream_t s) {
+    if (n_rows <= 0) return n_rows == 0 ? hipSuccess : hipErrorInvalidValue;
+    const int group = heads / c.heads;
+    if (cdiv((long)n_rows * group, 16) > 65535) return hipErrorInvalidValue;
+    const Attn8Plan p = attn8_plan(n_keys, n_rows, heads, c.heads, c.d, ws ? ws_elems : 0);
+    const dim3 grid(c.heads, cdiv((long)n_rows * group, 16), p.n_split);
+    const float scale = 1.4426950408889634f / sqrtf((float)c.d);
+    float* w = p.n_split > 1 ? ws : nullptr;
+    if (c.d == 128) attn8_cols_kernel<128><<<grid, 256, 0, s>>>(c, n_keys, q, ldq, n_rows, group, scale, o, ldo, w, p.per);
+    else attn8_cols_kernel<64><<<grid, 256, 0, s>>>(c, n_keys, q, ldq, n_rows, group, scale, o, ldo, w, p.per);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !w) return e;
+    if (c.d == 128) attn8_join_kernel<128><<<n_rows * heads, 128, 0, s>>>(w, p.n_split, heads, o, ldo);
+    else attn8_join_kernel<64><<<n_rows * heads, 64, 0, s>>>(w, p.n_split, heads, o, ldo);
+    return hipGetLastError();
+}

@@ -1,0 +1,129 @@
+// The choice of the next token: how often each token is in a text, and penalties, a bias and a mask on the logits with the greedy choice.
+#include "kernels.h"
+
+// ---------------------------------------------------------------- counts
+// counts[r][t] = the number of j with tokens[r][j] = t.  A workgroup counts a range of the vocabulary of one row in LDS, so that the row
+// is written once and nothing has to be cleared before; ids outside the range (padding too) are passed over.
+constexpr int COUNT_RANGE = 8192;
+__global__ __launch_bounds__(256) void token_counts_kernel(const int* __restrict__ tokens, long ldt, int n, int vocab, int* __restrict__ counts,
+                                                           long ldc) {
+    __shared__ int h[COUNT_RANGE];
+    const int first = blockIdx.x * COUNT_RANGE, size = min(COUNT_RANGE, vocab - first);
+    const int* tok = tokens + (long)blockIdx.y * ldt;
+    for (int i = threadIdx.x; i < size; i += 256) h[i] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += 256) {
+        const unsigned t = (unsigned)(tok[i] - first);
+        if (tok[i] >= 0 && t < (unsigned)size) atomicAdd(&h[t], 1);
+    }
+    __syncthreads();
+    int* out = counts + (long)blockIdx.y * ldc + first;
+    for (int i = threadIdx.x; i < size; i += 256) out[i] = h[i];
+}
+// counts[r][tokens[r][j]] += add: whole numbers, so the order of the additions changes nothing
+__global__ __launch_bounds__(256) void token_counts_add_kernel(const int* __restrict__ tokens, long ldt, int n, int vocab, int add,
+                                                               int* __restrict__ counts, long ldc) {
+    const int i = blockIdx.x * 256 + threadIdx.x;
+    if (i >= n) return;
+    const int t = tokens[(long)blockIdx.y * ldt + i];
+    if (t >= 0 && t < vocab) atomicAdd(counts + (long)blockIdx.y * ldc + t, add);
+}
+hipError_t launch_token_counts(const int* tokens, long ldt, int rows, int n, int vocab, int add, int* counts, long ldc, hipStream_t s) {
+    for (int r = 0; r < rows; r += 32768) {                // (the grid's second axis is limited)
+        const int m = rows - r < 32768 ? rows - r : 32768;
+        const int* t = tokens + (long)r * ldt;
+        int* c = counts + (long)r * ldc;
+        if (!add) token_counts_kernel<<<dim3(cdiv(vocab, COUNT_RANGE), m), 256, 0, s>>>(t, ldt, n, vocab, c, ldc);
+        else if (n > 0) token_counts_add_kernel<<<dim3(cdiv(n, 256), m), 256, 0, s>>>(t, ldt, n, vocab, add, c, ldc);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+// ---------------------------------------------------------------- choice
+// Every step is rounded to fp32 by itself (no fused multiply-add), so that equal logits stay equal whatever else is done to them.
+__device__ __forceinline__ float penalised(float x, int count, float bias, const Choose& c) {
+    if (count > 0) {
+        x = x > 0.f ? __fdiv_rn(x, c.repetition) : __fmul_rn(x, c.repetition);
+        x = __fsub_rn(x, __fadd_rn(__fmul_rn((float)count, c.frequency), c.presence));
+    }
+    return __fadd_rn(x, bias);
+}
+struct Best {
+    float v = -INFINITY;
+    int i = 0x7fffffff;
+    __device__ __forceinline__ void take(float ov, int oi) {       // the lowest index among equals; NaN is never larger nor equal
+        if (ov > v || (ov == v && oi < i)) { v = ov; i = oi; }
+    }
+};
+template <int NT>
+__device__ __forceinline__ Best block_best(Best b) {
+    __shared__ float bv[NT / 64];
+    __shared__ int bi[NT / 64];
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) {
+        const float ov = __shfl_xor(b.v, off, 64);
+        const int oi = __shfl_xor(b.i, off, 64);
+        b.take(ov, oi);
+    }
+    if ((threadIdx.x & 63) == 0) { bv[threadIdx.x >> 6] = b.v; bi[threadIdx.x >> 6] = b.i; }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) b.take(bv[w], bi[w]);
+    return b;
+}
+// Grid x: pieces of a row, y: rows.  One piece a row: the choice; more: its best to ws[(row * pieces + piece) * 2], joined by choose_join_kernel.
+template <int NT>
+__global__ __launch_bounds__(NT) void choose_kernel(Choose c, int vocab, int piece, float* __restrict__ ws) {
+    const long r = blockIdx.y;
+    const int first = blockIdx.x * piece, end = min(vocab, first + piece);
+    const float* x = c.logits + r * c.ldl;
+    const int* counts = c.counts ? c.counts + r * c.ldc : nullptr;
+    const float* bias = c.bias ? c.bias + r * c.ldb : nullptr;
+    const unsigned* allowed = c.allowed ? c.allowed + r * c.lda : nullptr;
+    float* out = c.out ? c.out + r * c.ldo : nullptr;
+    Best b;
+    for (int i = first + threadIdx.x; i < end; i += NT) {
+        const bool may = !allowed || allowed[i >> 5] >> (i & 31) & 1;
+        const float y = may ? penalised(x[i], counts ? counts[i] : 0, bias ? bias[i] : 0.f, c) : -INFINITY;
+        if (out) out[i] = y;
+        if (may) b.take(y, i);
+    }
+    if (!c.choice) return;
+    b = block_best<NT>(b);
+    if (threadIdx.x) return;
+    if (!ws) c.choice[r] = b.i == 0x7fffffff ? -1 : b.i;
+    else {
+        ws[(r * gridDim.x + blockIdx.x) * 2] = b.v;
+        ws[(r * gridDim.x + blockIdx.x) * 2 + 1] = __int_as_float(b.i);
+    }
+}
+__global__ __launch_bounds__(64) void choose_join_kernel(const float* __restrict__ ws, int pieces, int* __restrict__ choice) {
+    Best b;
+    for (int i = threadIdx.x; i < pieces; i += 64) b.take(ws[((long)blockIdx.x * pieces + i) * 2], __float_as_int(ws[((long)blockIdx.x * pieces + i) * 2 + 1]));
+    b = block_best<64>(b);
+    if (threadIdx.x == 0) choice[blockIdx.x] = b.i == 0x7fffffff ? -1 : b.i;
+}
+hipError_t launch_choose(const Choose& c, int rows, int vocab, float* ws, size_t ws_elems, hipStream_t s) {
+    for (int r = 0; r < rows; r += 32768) {
+        const int m = rows - r < 32768 ? rows - r : 32768;
+        Choose p = c;
+        p.logits += (long)r * c.ldl;
+        if (p.counts) p.counts += (long)r * c.ldc;
+        if (p.bias) p.bias += (long)r * c.ldb;
+        if (p.allowed) p.allowed += (long)r * c.lda;
+        if (p.out) p.out += (long)r * c.ldo;
+        if (p.choice) p.choice += r;
+        const int pieces = cdiv(vocab, 2048);
+        if (ws && pieces > 1 && (size_t)m * pieces * 2 <= ws_elems) {
+            choose_kernel<256><<<dim3(pieces, m), 256, 0, s>>>(p, vocab, 2048, ws);
+            if (p.choice) choose_join_kernel<<<m, 64, 0, s>>>(ws, pieces, p.choice);
+        } else {
+            choose_kernel<1024><<<dim3(1, m), 1024, 0, s>>>(p, vocab, vocab, nullptr);
+        }
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}

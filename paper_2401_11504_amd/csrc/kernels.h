@@ -211,3 +211,32 @@ hipError_t launch_attention_decode(const bf16_t* q, bf16_t* k, bf16_t* v, long l
                                    const DecodeFresh& fresh = DecodeFresh{});
 // index of the largest of n floats, lowest index among equals
 hipError_t launch_argmax(const float* x, int n, int* out, hipStream_t s);
+
+// ---------------------------------------------------------------- key/value cache in 8 bits (cache8.hip)
+struct Cache8 {                           // see cache8.hip for the layout
+    int8_t *k, *v;                        // [blocks][heads][d / 64][64][64], [blocks][heads][d][64]
+    float *ks, *vs;                       // [blocks][heads]
+    bf16_t *kt, *vt;                      // the incomplete block: [heads][d / 64][64][64], [heads][d][64]
+    int heads, d;
+};
+// tokens n_cached .. n_cached + n_new - 1; k, v: rows of [heads * d]
+hipError_t launch_cache8_append(const Cache8& c, int n_cached, const bf16_t* k, long ldk, const bf16_t* v, long ldv, int n_new, hipStream_t s);
+hipError_t launch_cache8_read(const Cache8& c, int n_cached, int first, int n, float* k, long ldk, float* v, long ldv, hipStream_t s);
+// o = attention of rows of queries, the last n_rows of n_keys tokens; heads a multiple of c.heads, 1 <= n_rows <= n_keys
+constexpr int ATTN8_MAX_SPLIT = 64;
+hipError_t launch_attention_cache8(const Cache8& c, int n_keys, const bf16_t* q, long ldq, int n_rows, int heads, bf16_t* o, long ldo,
+                                   float* ws, size_t ws_elems, hipStream_t s);
+const char* attention_cache8_plan(int n_keys, int n_rows, int heads, int kv_heads, int d, size_t ws_elems, int* n_ranges);   // a static string
+
+// ---------------------------------------------------------------- choice of the next token (choose.hip)
+hipError_t launch_token_counts(const int* tokens, long ldt, int rows, int n, int vocab, int add, int* counts, long ldc, hipStream_t s);
+struct Choose {
+    const float* logits; long ldl;
+    const int* counts; long ldc;          // may be null; a stride of 0: one row for all, here and below
+    const float* bias; long ldb;          // may be null
+    const unsigned* allowed; long lda;    // may be null
+    float* out; long ldo;                 // may be null
+    int* choice;                          // may be null
+    float repetition, presence, frequency;
+};
+hipError_t launch_choose(const Choose& c, int rows, int vocab, float* ws, size_t ws_elems, hipStream_t s);

@@ -1598,6 +1598,81 @@ extern "C" tl_status tl_k_argmax(const float* x, int32_t n, int32_t* out, void* 
     HIPCHK(launch_argmax(x, n, out, (hipStream_t)hip_stream));
     return TL_OK;
 }
+// what every call on a cache needs of it
+static tl_status cache8_of(const tl_cache8_mem* m, const char* name, Cache8* out) {
+    if (!m || !m->k || !m->v || !m->k_scale || !m->v_scale || !m->k_tail || !m->v_tail) return fail(TL_ERR_ARG, "%s: null pointer", name);
+    if (((uintptr_t)m->k | (uintptr_t)m->v | (uintptr_t)m->k_tail | (uintptr_t)m->v_tail) & 15)
+        return fail(TL_ERR_ARG, "%s: codes and tails start at multiples of 16 bytes", name);
+    if (m->n_kv_heads < 1 || m->n_kv_heads > 4096 || (m->d_head != 64 && m->d_head != 128) || m->capacity < 1)
+        return fail(TL_ERR_ARG, "%s: %d heads of %d, capacity %d", name, m->n_kv_heads, m->d_head, m->capacity);
+    *out = Cache8{m->k, m->v, m->k_scale, m->v_scale, m->k_tail, m->v_tail, m->n_kv_heads, m->d_head};
+    return TL_OK;
+}
+extern "C" tl_status tl_k_cache8_append(const tl_cache8_mem* cache, int32_t n_cached, const uint16_t* k, int32_t ldk, const uint16_t* v,
+                                        int32_t ldv, int32_t n_new, void* hip_stream) {
+    Cache8 c;
+    TLCHK(cache8_of(cache, "tl_k_cache8_append", &c));
+    KARGS_OK(((k && v) || n_new == 0) && n_cached >= 0 && n_new >= 0 && (n_new <= 1 || (ldk >= c.heads * c.d && ldv >= c.heads * c.d)), "tl_k_cache8_append");
+    if ((int64_t)n_cached + n_new > cache->capacity)
+        return fail(TL_ERR_WINDOW, "tl_k_cache8_append: %d + %d tokens, capacity %d", n_cached, n_new, cache->capacity);
+    HIPCHK(launch_cache8_append(c, n_cached, k, ldk, v, ldv, n_new, (hipStream_t)hip_stream));
+    return TL_OK;
+}
+extern "C" tl_status tl_k_cache8_read(const tl_cache8_mem* cache, int32_t n_cached, int32_t first, int32_t n, float* k_out, int32_t ldk,
+                                      float* v_out, int32_t ldv, void* hip_stream) {
+    Cache8 c;
+    TLCHK(cache8_of(cache, "tl_k_cache8_read", &c));
+    KARGS_OK(((k_out && v_out) || n == 0) && first >= 0 && n >= 0 && (n <= 1 || (ldk >= c.heads * c.d && ldv >= c.heads * c.d)), "tl_k_cache8_read");
+    if (n_cached > cache->capacity || (int64_t)first + n > n_cached)
+        return fail(TL_ERR_WINDOW, "tl_k_cache8_read: tokens %d + %d of %d, capacity %d", first, n, n_cached, cache->capacity);
+    HIPCHK(launch_cache8_read(c, n_cached, first, n, k_out, ldk, v_out, ldv, (hipStream_t)hip_stream));
+    return TL_OK;
+}
+extern "C" tl_status tl_k_attention_cache8(const tl_cache8_mem* cache, int32_t n_keys, const uint16_t* q, int32_t ldq, int32_t n_rows,
+                                           int32_t n_heads, uint16_t* o, int32_t ldo, float* workspace, size_t workspace_elems,
+                                           void* hip_stream) {
+    Cache8 c;
+    TLCHK(cache8_of(cache, "tl_k_attention_cache8", &c));
+    KARGS_OK(((q && o) || n_rows == 0) && n_rows >= 0 && n_keys >= 1 && n_heads >= 1 && n_heads <= 65536 && n_heads % c.heads == 0 && (int64_t)n_rows * n_heads <= 1 << 24 &&
+                 (n_rows <= 1 || (ldq >= n_heads * c.d && ldo >= n_heads * c.d)), "tl_k_attention_cache8");
+    if (n_keys > cache->capacity || n_rows > n_keys)
+        return fail(TL_ERR_WINDOW, "tl_k_attention_cache8: %d rows, %d keys, capacity %d", n_rows, n_keys, cache->capacity);
+    HIPCHK(launch_attention_cache8(c, n_keys, q, ldq, n_rows, n_heads, o, ldo, workspace, workspace_elems, (hipStream_t)hip_stream));
+    return TL_OK;
+}
+extern "C" tl_status tl_k_attention_cache8_plan(int32_t n_keys, int32_t n_rows, int32_t n_heads, int32_t n_kv_heads, int32_t d_head,
+                                                size_t workspace_elems, char* name_out, size_t name_cap, int32_t* n_ranges_out,
+                                                size_t* elems_out) {
+    KARGS_OK(name_out && name_cap > 0 && n_ranges_out && elems_out && n_keys >= 1 && n_rows >= 1 && n_rows <= n_keys && n_kv_heads >= 1 &&
+                 n_kv_heads <= 4096 && n_heads >= 1 && n_heads <= 65536 && n_heads % n_kv_heads == 0 && (int64_t)n_rows * n_heads <= 1 << 24 &&
+                 (d_head == 64 || d_head == 128), "tl_k_attention_cache8_plan");
+    int n = 1;
+    snprintf(name_out, name_cap, "%s", attention_cache8_plan(n_keys, n_rows, n_heads, n_kv_heads, d_head, workspace_elems, &n));
+    *n_ranges_out = n;
+    *elems_out = n > 1 ? (size_t)n_rows * n_heads * n * (d_head + 2) : 0;
+    return TL_OK;
+}
+extern "C" tl_status tl_k_token_counts(const int32_t* tokens, int32_t ldt, int32_t rows, int32_t n, int32_t vocab, int32_t add, int32_t* counts,
+                                       int32_t ldc, void* hip_stream) {
+    KARGS_OK((tokens || n == 0 || rows == 0) && (counts || rows == 0) && rows >= 0 && n >= 0 && vocab >= 1 && add >= -1 && add <= 1 &&
+                 (rows <= 1 || (ldt >= n && ldc >= vocab)), "tl_k_token_counts");
+    HIPCHK(launch_token_counts(tokens, ldt, rows, n, vocab, add, counts, ldc, (hipStream_t)hip_stream));
+    return TL_OK;
+}
+extern "C" tl_status tl_k_choose(const float* logits, int32_t ldl, int32_t rows, int32_t vocab, const int32_t* counts, int32_t ldc,
+                                 float repetition, float presence, float frequency, const float* bias, int32_t ldb, const uint32_t* allowed,
+                                 int32_t lda, float* out, int32_t ldo, int32_t* choice, float* workspace, size_t workspace_elems,
+                                 void* hip_stream) {
+    auto row = [&](int32_t ld, int32_t n) { return rows <= 1 || ld == 0 || ld >= n; };      // 0: one row for all
+    KARGS_OK((logits || rows == 0) && rows >= 0 && vocab >= 1 && (rows <= 1 || (ldl >= vocab && (!out || ldo >= vocab))) && (!counts || row(ldc, vocab)) &&
+                 (!bias || row(ldb, vocab)) && (!allowed || row(lda, cdiv(vocab, 32))) && (out != logits || rows <= 1 || ldo == ldl),
+             "tl_k_choose");
+    if (!(repetition > 0.f) || !std::isfinite(repetition) || !std::isfinite(presence) || !std::isfinite(frequency))
+        return fail(TL_ERR_ARG, "tl_k_choose: repetition %g (above 0), presence %g, frequency %g", repetition, presence, frequency);
+    const Choose c{logits, ldl, counts, ldc, bias, ldb, allowed, lda, out, ldo, choice, repetition, presence, frequency};
+    HIPCHK(launch_choose(c, rows, vocab, workspace, workspace_elems, (hipStream_t)hip_stream));
+    return TL_OK;
+}
 extern "C" tl_status tl_k_swiglu_bwd(const uint16_t* da, const uint16_t* gu, int32_t T, int32_t f, uint16_t* dgu,
                                      void* hip_stream) {
     KARGS_OK(da && gu && dgu && T >= 0 && f > 0 && (f & 7) == 0, "tl_k_swiglu_bwd");
