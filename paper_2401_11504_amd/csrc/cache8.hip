@@ -7,8 +7,10 @@
 // Keys lie as [block][head][D / 64][64 tokens][64 columns], values as [block][head][D][64 tokens] (transposed): both are contiguous
 // 1 KB runs for a wave that loads matrix operands of 16 codes a lane straight from memory, and neither has to be transposed there.
 #include <algorithm>
+#include <type_traits>
 
 #include "kernels.h"
+#include "tiles.h"
 
 static constexpr float kLeastMagnitude = 7.888609052210118e-31f;   // 2^-100: keeps the scale and its reciprocal normal numbers
 
@@ -403,33 +405,267 @@ __global__ __launch_bounds__(D) void attn8_join_kernel(const float* __restrict__
     o[(long)(blockIdx.x / heads) * ldo + (long)(blockIdx.x % heads) * D + e] = f32_to_bf16(acc / sum);
 }
 
-struct Attn8Plan { int n_split, per; };       // ranges, blocks a range
+// ---------------------------------------------------------------- attention of many rows
+// The same columns, 32 to a wave, NC waves to a workgroup, which takes one tile (a block of the cache) after another:
+//   S^T[key][column] = K q^T   and   O^T[d][column] += V^T P^T     by v_mfma_f32_32x32x16_bf16 (operand layout: tiles.h)
+// The workgroup's threads widen a tile's codes to bf16 on their way to LDS, each once, so that a code is converted once for 32 NC columns;
+// the codes of the tile after are on their way into registers meanwhile, and two buffers make one barrier a tile enough.  Probabilities
+// (times the values' scale) are rounded to bf16, as in the attention of a chunk.  16-byte pieces of a row lie in LDS at a place of
+// their own for each of 16 rows, so that the fragment reads of 16 lanes meet in no bank; a value row's pieces hold the tokens in the
+// order in which a score fragment serves as second operand.
+template <int D>
+__device__ __forceinline__ unsigned k_piece_at(int key, int c) { return key * D * 2 + ((c ^ (D == 128 ? key & 15 : key >> 1 & 7)) << 4); }
+__device__ __forceinline__ unsigned v_piece_at(int d, int c) { return d * 128 + ((c ^ (d >> 1 & 7)) << 4); }
+
+template <int D, int NC>
+__global__ __launch_bounds__(NC * 64, 2) void attn8_rows_kernel(Cache8 c, int n_keys, const bf16_t* __restrict__ q, long ldq, int n_rows, int group,
+                                                             float scale_log2e, bf16_t* __restrict__ o, long ldo, float* __restrict__ ws,
+                                                             int blocks_per_split, int n_split) {
+    constexpr int KS = D / 16, ND = D / 32, NT = NC * 64, NP = 64 * D / 16, PT = 2 * NP / NT;   // pieces of 16 codes: of K, a thread
+    constexpr int TB = 64 * D * 2, STAGE = 2 * TB + 16;                                        // a tile's bytes in LDS, K, V and scales
+    extern __shared__ __align__(16) unsigned char smem[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, g = lane >> 5;
+    // the last columns see most: they come first, every head's before any head's second; a head's workgroups are a multiple of
+    // c.heads apart, on one XCD if that is a multiple of eight
+    const int n_cols = n_rows * group, heads = c.heads * group, n_blocks = (n_cols + 32 * NC - 1) / (32 * NC);
+    const int head = blockIdx.x % c.heads, rest = blockIdx.x / c.heads;
+    const int c0 = (n_blocks - 1 - rest % n_blocks) * 32 * NC, split = rest / n_blocks;
+    const int w0 = c0 + 32 * wave, col = min(w0 + l32, n_cols - 1), row = col / group, seen = n_keys - n_rows + row + 1;
+    const int most = n_keys - n_rows + min(c0 + 32 * NC - 1, n_cols - 1) / group + 1;          // keys that the block's last column sees
+    const int w_most = w0 < n_cols ? n_keys - n_rows + min(w0 + 31, n_cols - 1) / group + 1 : 0;     // the wave's
+    const int w_least = n_keys - n_rows + w0 / group + 1;
+    const int b_begin = split * blocks_per_split, b_end = min(b_begin + blocks_per_split, (most + 63) >> 6), b_tail = n_keys >> 6;
+
+    bf16x8_t qf[KS];
+    const bf16_t* qr = q + (long)row * ldq + (long)(head * group + col % group) * D + g * 8;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = __builtin_bit_cast(bf16x8_t, *(const uint4*)(qr + ks * 16));
+    f32x16_t oacc[ND];
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt) oacc[dt] = zero16();
+    float m = -INFINITY, l = 0.f;
+
+    uint4 code[PT];
+    float sc = 0.f;                                          // of threads 0 and 1: the tile's scales
+    auto fetch = [&](int b) {                                // (of a complete block)
+        const long at = (long)b * c.heads + head;
+#pragma unroll
+        for (int i = 0; i < PT; ++i) {
+            const int p = i * NT + tid;
+            code[i] = *(const uint4*)((p < NP ? c.k + p * 16 : c.v + (p - NP) * 16) + at * 64 * D);
+        }
+        if (tid < 2) sc = (tid ? c.vs : c.ks)[at];
+    };
+    auto widen = [&](unsigned char* st) {
+#pragma unroll
+        for (int i = 0; i < PT; ++i) {
+            const int p = i * NT + tid;
+            const uint4 w = code[i];
+            if (p < NP) {
+                const int key = p >> 2 & 63, ch = (p >> 8) * 8 + (p & 3) * 2;
+                *(bf16x8_t*)(st + k_piece_at<D>(key, ch)) = codes_bf16(w.x, w.y);
+                *(bf16x8_t*)(st + k_piece_at<D>(key, ch + 1)) = codes_bf16(w.z, w.w);
+            } else {
+                const int d = (p - NP) >> 2, ch = (p & 3) * 2;
+                *(bf16x8_t*)(st + TB + v_piece_at(d, ch)) = codes_bf16(w.x, w.z);
+                *(bf16x8_t*)(st + TB + v_piece_at(d, ch + 1)) = codes_bf16(w.y, w.w);
+            }
+        }
+        if (tid < 2) ((float*)(st + 2 * TB))[tid] = tid ? sc : sc * scale_log2e;
+    };
+    // the tail as a tile; whether a value of it is not finite
+    auto tail_tile = [&](unsigned char* st) {
+        const bf16_t *kt = c.kt + (long)head * 64 * D, *vt = c.vt + (long)head * 64 * D;
+        bool odd = false;
+#pragma unroll
+        for (int i = 0; i < PT; ++i) {
+            const int p = i * NT + tid;
+            if (p < NP) {
+                const int key = p >> 2 & 63, ch = (p >> 8) * 8 + (p & 3) * 2;
+                *(uint4*)(st + k_piece_at<D>(key, ch)) = *(const uint4*)(kt + p * 16);
+                *(uint4*)(st + k_piece_at<D>(key, ch + 1)) = *(const uint4*)(kt + p * 16 + 8);
+            } else {
+                const int d = (p - NP) >> 2, ch = (p & 3) * 2, u0 = (p & 3) * 16;
+                const uint4 a = tail_values(vt + d * 64, u0, n_keys & 63, &odd), b = tail_values(vt + d * 64, u0 + 8, n_keys & 63, &odd);
+                *(uint4*)(st + TB + v_piece_at(d, ch)) = make_uint4(a.x, a.y, b.x, b.y);
+                *(uint4*)(st + TB + v_piece_at(d, ch + 1)) = make_uint4(a.z, a.w, b.z, b.w);
+            }
+        }
+        if (tid < 2) ((float*)(st + 2 * TB))[tid] = tid ? 1.f : scale_log2e;
+        return odd;
+    };
+    // probs (bf16 [64][32] of this wave) is set for a tail with values that are not finite
+    auto tile = [&](int b, const unsigned char* st, unsigned short* probs) {
+        const int u0 = b << 6;
+        if (u0 >= w_most) return;                            // (uniform) no column of the wave sees it
+        f32x16_t s0 = zero16(), s1 = zero16();
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            s0 = mfma32(*(const bf16x8_t*)(st + k_piece_at<D>(l32, 2 * ks + g)), qf[ks], s0);
+            s1 = mfma32(*(const bf16x8_t*)(st + k_piece_at<D>(32 + l32, 2 * ks + g)), qf[ks], s1);
+        }
+        const float ks = ((const float*)(st + 2 * TB))[0], vs = ((const float*)(st + 2 * TB))[1];
+        float x[32], top = -INFINITY;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            x[v] = s0[v] * ks;
+            x[16 + v] = s1[v] * ks;
+        }
+        if (u0 + 64 > w_least) {                             // some column does not see all of it
+#pragma unroll
+            for (int v = 0; v < 32; ++v)
+                if (u0 + 32 * (v >> 4) + 8 * (v >> 2 & 3) + 4 * g + (v & 3) >= seen) x[v] = -INFINITY;
+        }
+#pragma unroll
+        for (int v = 0; v < 32; ++v) top = fmaxf(top, x[v]);
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        const float mn = fmaxf(m, top), base = mn == -INFINITY ? 0.f : mn, alpha = __builtin_amdgcn_exp2f(m - base);
+        m = mn;
+        float sum = 0.f;
+        const bool sees = u0 < seen;
+#pragma unroll
+        for (int v = 0; v < 32; ++v) {
+            x[v] = __builtin_amdgcn_exp2f(x[v] - base);
+            sum += x[v];
+        }
+        l = l * alpha + sum;
+        const float f = sees ? vs : 0.f;                     // (a block that a column does not see may have the scale NaN)
+#pragma unroll
+        for (int v = 0; v < 32; ++v) x[v] *= f;
+        if (__builtin_amdgcn_ballot_w64(alpha != 1.f)) {
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) oacc[dt][v] *= alpha;
+        }
+        if (!probs) {
+#pragma unroll
+            for (int G = 0; G < 4; ++G) {
+                const bf16x8_t p = pack_b_from_d(x + 16 * (G >> 1), G & 1);
+#pragma unroll
+                for (int dt = 0; dt < ND; ++dt)
+                    oacc[dt] = mfma32(*(const bf16x8_t*)(st + TB + v_piece_at(dt * 32 + l32, 2 * G + g)), p, oacc[dt]);
+            }
+        } else {
+            // a value that is not finite counts for the columns that see it alone, which a product with zeros does not give
+            const bf16_t* vt = c.vt + (long)head * 64 * D;
+#pragma unroll
+            for (int v = 0; v < 32; ++v) probs[(32 * (v >> 4) + 8 * (v >> 2 & 3) + 4 * g + (v & 3)) * 32 + l32] = f32_to_bf16(x[v]);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            for (int u = 0; u < (n_keys & 63) && u0 + u < seen; ++u) {
+                const float p = bf16_to_f32(probs[u * 32 + l32]);
+#pragma unroll
+                for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) oacc[dt][v] = fmaf(p, bf16_to_f32(vt[(dt * 32 + 8 * (v >> 2) + 4 * g + (v & 3)) * 64 + u]), oacc[dt][v]);
+            }
+        }
+    };
+
+    const int full = min(b_end, b_tail) - b_begin;           // complete blocks
+    if (full > 0) {
+        fetch(b_begin);
+        widen(smem);
+        if (full > 1) fetch(b_begin + 1);
+    }
+    for (int i = 0; i < full; ++i) {
+        __syncthreads();                                     // tile i is there, tile i - 1 has been read
+        if (i + 1 < full) widen(smem + (i + 1 & 1) * STAGE);
+        if (i + 2 < full) fetch(b_begin + i + 2);
+        tile(b_begin + i, smem + (i & 1) * STAGE, nullptr);
+    }
+    if (b_end > b_tail && b_tail >= b_begin) {
+        __syncthreads();
+        const bool odd = tail_tile(smem);
+        unsigned short* probs = (unsigned short*)(smem + STAGE) + wave * 64 * 32;
+        if (__syncthreads_or(odd)) tile(b_tail, smem, probs);
+        else tile(b_tail, smem, nullptr);
+    }
+    l += __shfl_xor(l, 32, 64);
+    if (n_split > 1) {
+        if (w0 + l32 >= n_cols) return;
+        float* out = ws + (((long)row * heads + head * group + col % group) * n_split + split) * (D + 2);
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+            for (int v = 0; v < 16; v += 2) *(float2*)(out + dt * 32 + 8 * (v >> 2) + 4 * g + (v & 3)) = make_float2(oacc[dt][v], oacc[dt][v + 1]);
+        if (g == 0) *(float2*)(out + D) = make_float2(m, l);
+        return;
+    }
+    __syncthreads();
+    constexpr int LD = D + 8;
+    bf16_t* slab = (bf16_t*)smem + wave * 32 * LD;           // the wave's 32 columns leave in 16-byte pieces
+    const float inv = 1.f / l;
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+        for (int v = 0; v < 16; v += 4)
+            *(uint2*)(slab + l32 * LD + dt * 32 + 2 * v + 4 * g) = make_uint2(pack_bf16x2(oacc[dt][v] * inv, oacc[dt][v + 1] * inv),
+                                                                            pack_bf16x2(oacc[dt][v + 2] * inv, oacc[dt][v + 3] * inv));
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int i = lane; i < 32 * D / 8; i += 64) {
+        const int cc = w0 + i / (D / 8), e = i % (D / 8) * 8;
+        if (cc < n_cols) *(uint4*)(o + (long)(cc / group) * ldo + (long)(head * group + cc % group) * D + e) = *(const uint4*)(slab + (i / (D / 8)) * LD + e);
+    }
+}
+// two tiles; the probabilities behind the first of them; the output slab
+template <int D, int NC>
+static constexpr size_t attn8_rows_lds() {
+    constexpr size_t stage = 2 * 64 * D * 2 + 16;
+    return std::max({2 * stage, stage + NC * 64 * 32 * 2, (size_t)NC * 32 * (D + 8) * 2});
+}
+
+// Which kernel, and how the keys are cut.
+//   columns  16 columns a workgroup: its waves read the cache at once and convert every code for 16 columns
+//   rows64, rows128, rows256  that many columns a workgroup
+struct Attn8Plan { int cols, n_split, per; };       // columns a workgroup, ranges, blocks a range
 static Attn8Plan attn8_plan(int n_keys, int n_rows, int heads, int kv_heads, int d, size_t ws_elems) {
-    const int nb = cdiv(n_keys, 64), units = kv_heads * cdiv((long)n_rows * (heads / kv_heads), 16);
-    long n = std::min<long>(std::min<long>(512 / units, ATTN8_MAX_SPLIT), cdiv(nb, 4));
-    n = std::min<long>(n, (long)(ws_elems / ((size_t)n_rows * heads * (d + 2))));
-    if (n < 2) return {1, nb};
+    const int nb = cdiv(n_keys, 64);
+    const long n_cols = (long)n_rows * (heads / kv_heads);
+    const int cols = n_cols <= 32 ? 16 : n_cols <= 64 ? 64 : n_cols <= 128 ? 128 : 256;
+    const long units = kv_heads * (long)cdiv(n_cols, cols);
+    long n = cols == 16 ? std::min<long>(512 / units, cdiv(nb, 4)) : std::min<long>((cols == 256 ? 256 : 512) / units, cdiv(nb, 4));
+    n = std::min<long>(std::min<long>(n, ATTN8_MAX_SPLIT), (long)(ws_elems / ((size_t)n_rows * heads * (d + 2))));
+    if (n < 2) return {cols, 1, nb};
     const int per = cdiv(nb, n);
-    return {cdiv(nb, per), per};
+    return {cols, cdiv(nb, per), per};
 }
 const char* attention_cache8_plan(int n_keys, int n_rows, int heads, int kv_heads, int d, size_t ws_elems, int* n_ranges) {
-    *n_ranges = attn8_plan(n_keys, n_rows, heads, kv_heads, d, ws_elems).n_split;
-    return "columns";
+    const Attn8Plan p = attn8_plan(n_keys, n_rows, heads, kv_heads, d, ws_elems);
+    *n_ranges = p.n_split;
+    return p.cols == 16 ? "columns" : p.cols == 64 ? "rows64" : p.cols == 128 ? "rows128" : "rows256";
+}
+template <int D>
+static hipError_t run_attention_cache8(const Attn8Plan& p, const Cache8& c, int n_keys, const bf16_t* q, long ldq, int n_rows, int group, bf16_t* o,
+                                       long ldo, float* ws, hipStream_t s) {
+    const float scale = 1.4426950408889634f / sqrtf((float)D);
+    const long n_cols = (long)n_rows * group;
+    float* w = p.n_split > 1 ? ws : nullptr;
+    auto rows = [&](auto nc) {
+        constexpr int NC = decltype(nc)::value;
+        constexpr size_t lds = attn8_rows_lds<D, NC>();
+        const hipError_t e = hipFuncSetAttribute((const void*)attn8_rows_kernel<D, NC>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e != hipSuccess) return e;
+        attn8_rows_kernel<D, NC><<<c.heads * cdiv(n_cols, 32 * NC) * p.n_split, NC * 64, lds, s>>>(c, n_keys, q, ldq, n_rows, group, scale, o, ldo, w,
+                                                                                             p.per, p.n_split);
+        return hipGetLastError();
+    };
+    hipError_t e;
+    if (p.cols == 16) {
+        attn8_cols_kernel<D><<<dim3(c.heads, cdiv(n_cols, 16), p.n_split), 256, 0, s>>>(c, n_keys, q, ldq, n_rows, group, scale, o, ldo, w, p.per);
+        e = hipGetLastError();
+    } else e = p.cols == 64 ? rows(std::integral_constant<int, 2>{}) : p.cols == 128 ? rows(std::integral_constant<int, 4>{}) : rows(std::integral_constant<int, 8>{});
+    if (e != hipSuccess || !w) return e;
+    attn8_join_kernel<D><<<n_rows * c.heads * group, D, 0, s>>>(w, p.n_split, c.heads * group, o, ldo);
+    return hipGetLastError();
 }
 hipError_t launch_attention_cache8(const Cache8& c, int n_keys, const bf16_t* q, long ldq, int n_rows, int heads, bf16_t* o, long ldo,
                                    float* ws, size_t ws_elems, hipStream_t s) {
     if (n_rows <= 0) return n_rows == 0 ? hipSuccess : hipErrorInvalidValue;
-    const int group = heads / c.heads;
-    if (cdiv((long)n_rows * group, 16) > 65535) return hipErrorInvalidValue;
     const Attn8Plan p = attn8_plan(n_keys, n_rows, heads, c.heads, c.d, ws ? ws_elems : 0);
-    const dim3 grid(c.heads, cdiv((long)n_rows * group, 16), p.n_split);
-    const float scale = 1.4426950408889634f / sqrtf((float)c.d);
-    float* w = p.n_split > 1 ? ws : nullptr;
-    if (c.d == 128) attn8_cols_kernel<128><<<grid, 256, 0, s>>>(c, n_keys, q, ldq, n_rows, group, scale, o, ldo, w, p.per);
-    else attn8_cols_kernel<64><<<grid, 256, 0, s>>>(c, n_keys, q, ldq, n_rows, group, scale, o, ldo, w, p.per);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || !w) return e;
-    if (c.d == 128) attn8_join_kernel<128><<<n_rows * heads, 128, 0, s>>>(w, p.n_split, heads, o, ldo);
-    else attn8_join_kernel<64><<<n_rows * heads, 64, 0, s>>>(w, p.n_split, heads, o, ldo);
-    return hipGetLastError();
+    return c.d == 128 ? run_attention_cache8<128>(p, c, n_keys, q, ldq, n_rows, heads / c.heads, o, ldo, ws, s)
+                      : run_attention_cache8<64>(p, c, n_keys, q, ldq, n_rows, heads / c.heads, o, ldo, ws, s);
 }

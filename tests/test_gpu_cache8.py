@@ -178,6 +178,24 @@ def test_rows(api, rows, n, heads, kv, d):
         check(api, c, n, k, v, q, heads, kv, ws)
 
 
+@pytest.mark.parametrize("heads,kv,d,rows,n", [
+    (1, 1, 64, 300, 301), (1, 1, 128, 256, 512), (2, 2, 128, 257, 400), (6, 2, 64, 90, 700), (8, 1, 128, 33, 500), (8, 1, 64, 130, 131),
+    (1, 1, 128, 700, 700), (3, 1, 64, 11, 4000), (5, 1, 128, 13, 2500), (2, 2, 64, 40, 63), (4, 4, 128, 100, 2063)])
+def test_many_columns(api, heads, kv, d, rows, n):
+    k, v = draw(n + rows, n, kv, d)
+    c = fill(api, k, v, kv, capacity=n + 1)
+    q = queries(n, rows, heads * d)
+    for ws in (None, torch.full((1 << 20,), math.nan, device="cuda")):
+        check(api, c, n, k, v, q, heads, kv, ws)
+
+
+def test_every_kernel_is_reached(api):
+    """by the sizes above, with and without ranges"""
+    sizes = [(n, r, 2, 2, 64) for r, n in ((5, 66), (33, 33), (65, 200), (200, 200))] + [(4000, 11, 3, 1, 64), (2063, 100, 4, 4, 128), (700, 90, 6, 2, 64)]
+    seen = {api.tl_k_attention_cache8_plan(*s, elems)[0] for s in sizes for elems in (0, 1 << 20)}
+    assert seen == {"columns", "rows64", "rows128", "rows256"}
+
+
 def test_ranges_with_nothing_to_see(api):
     """more ranges than the first rows reach: their part of the join is empty"""
     heads, d, n, rows = 1, 64, 2000, 1000
