@@ -153,7 +153,8 @@ def _dp(t):
 
 
 def current_stream_handle():
-    return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+    # (torch.cuda.current_stream() builds an object: 2.8 us of every call, this 0.2)
+    return C.c_void_p(torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()))
 
 
 # ------------------------------------------------------------------ life cycle
@@ -470,8 +471,9 @@ class Cache8:
             assert t.is_cuda and t.is_contiguous() and tuple(t.shape) == shape and t.dtype == dtype, f"{name}: {dtype} {shape} expected"
         assert 0 < capacity <= 64 * nb, "capacity beyond the blocks"
         self.n_kv_heads, self.d_head, self.capacity = heads, d, capacity
-        self._mem = tl_cache8_mem(*[self.tensors[n].data_ptr() for n in want], heads, d, capacity)
-        self._ref = C.byref(self._mem)
+        self.width = heads * d
+        self.mem = tl_cache8_mem(*[self.tensors[n].data_ptr() for n in want], heads, d, capacity)
+        self.ref = C.byref(self.mem)
 
     @classmethod
     def empty(cls, n_kv_heads, d_head, capacity, device="cuda"):
@@ -482,34 +484,38 @@ class Cache8:
                    new(torch.bfloat16, n_kv_heads, d_head // 64, 64, 64), new(torch.bfloat16, n_kv_heads, d_head, 64), capacity)
 
 
-def _rows(t, dtype, width):
-    assert t.dim() == 2 and t.dtype == dtype and t.shape[1] == width, f"{dtype} [n, {width}] expected"
-    return t
+def _rows2(a, b, dtype, width):
+    """(address, row stride) of each of two tensors [n, width]"""
+    assert a.shape == b.shape and a.dim() == 2 and a.shape[1] == width and a.dtype == b.dtype == dtype, f"{dtype} [n, {width}] expected"
+    (la, ua), (lb, ub) = a.stride(), b.stride()
+    assert a.is_cuda and b.is_cuda and ua == ub == 1, "device tensors with unit inner stride expected"
+    return a.data_ptr(), la, b.data_ptr(), lb
+
+
+def _ws(workspace):
+    if workspace is None:
+        return None, 0
+    assert workspace.is_cuda and workspace.dtype == torch.float32 and workspace.is_contiguous(), "fp32 device scratch expected"
+    return workspace.data_ptr(), workspace.numel()
 
 
 def tl_k_cache8_append(cache, n_cached, k, v, stream=None):
     """k, v bf16 [n_new, n_kv_heads * d_head] -> tokens n_cached .. of the cache"""
-    w = cache.n_kv_heads * cache.d_head
-    _rows(k, torch.bfloat16, w), _rows(v, torch.bfloat16, w)
-    assert k.shape == v.shape
-    _chk(_lib.tl_k_cache8_append(cache._ref, n_cached, _dp(k), k.stride(0), _dp(v), v.stride(0), k.shape[0], _s(stream)))
+    kp, ldk, vp, ldv = _rows2(k, v, torch.bfloat16, cache.width)
+    _chk(_lib.tl_k_cache8_append(cache.ref, n_cached, kp, ldk, vp, ldv, k.shape[0], _s(stream)))
 
 
 def tl_k_cache8_read(cache, n_cached, first, k_out, v_out, stream=None):
     """k_out, v_out fp32 [n, n_kv_heads * d_head] <- what the cache stands for, tokens first .. first + n - 1"""
-    w = cache.n_kv_heads * cache.d_head
-    _rows(k_out, torch.float32, w), _rows(v_out, torch.float32, w)
-    assert k_out.shape == v_out.shape
-    _chk(_lib.tl_k_cache8_read(cache._ref, n_cached, first, k_out.shape[0], _dp(k_out), k_out.stride(0), _dp(v_out), v_out.stride(0), _s(stream)))
+    kp, ldk, vp, ldv = _rows2(k_out, v_out, torch.float32, cache.width)
+    _chk(_lib.tl_k_cache8_read(cache.ref, n_cached, first, k_out.shape[0], kp, ldk, vp, ldv, _s(stream)))
 
 
 def tl_k_attention_cache8(cache, n_keys, q, o, n_heads, workspace=None, stream=None):
     """q, o bf16 [n_rows, n_heads * d_head], the last n_rows of n_keys cached tokens"""
-    w = n_heads * cache.d_head
-    _rows(q, torch.bfloat16, w), _rows(o, torch.bfloat16, w)
-    assert q.shape == o.shape
-    _chk(_lib.tl_k_attention_cache8(cache._ref, n_keys, _dp(q), q.stride(0), q.shape[0], n_heads, _dp(o), o.stride(0), _dp(workspace),
-                                    workspace.numel() if workspace is not None else 0, _s(stream)))
+    qp, ldq, op, ldo = _rows2(q, o, torch.bfloat16, n_heads * cache.d_head)
+    wp, n = _ws(workspace)
+    _chk(_lib.tl_k_attention_cache8(cache.ref, n_keys, qp, ldq, q.shape[0], n_heads, op, ldo, wp, n, _s(stream)))
 
 
 def tl_k_attention_cache8_plan(n_keys, n_rows, n_heads, n_kv_heads, d_head, workspace_elems=0):
@@ -521,26 +527,37 @@ def tl_k_attention_cache8_plan(n_keys, n_rows, n_heads, n_kv_heads, d_head, work
 
 def tl_k_token_counts(tokens, counts, add=0, stream=None):
     """tokens int32 [rows, n], counts int32 [rows, vocab]; add 0: set, 1: add, -1: take away"""
-    assert tokens.dim() == counts.dim() == 2 and tokens.shape[0] == counts.shape[0] and tokens.dtype == counts.dtype == torch.int32
-    _chk(_lib.tl_k_token_counts(_dp(tokens), tokens.stride(0), tokens.shape[0], tokens.shape[1], counts.shape[1], add, _dp(counts),
-                                counts.stride(0), _s(stream)))
+    (rows, n), (again, vocab) = tokens.shape, counts.shape
+    (ldt, ut), (ldc, uc) = tokens.stride(), counts.stride()
+    assert rows == again and tokens.dtype == counts.dtype == torch.int32 and tokens.is_cuda and counts.is_cuda, "int32 [rows, n], [rows, vocab] expected"
+    assert (ut == 1 or n <= 1) and (uc == 1 or vocab == 1), "unit inner stride expected"
+    _chk(_lib.tl_k_token_counts(tokens.data_ptr(), ldt, rows, n, vocab, add, counts.data_ptr(), ldc, _s(stream)))
+
+
+def _row(t, dtype, rows, width):
+    """(address, row stride) of [rows, width], of one row for all, or of nothing"""
+    if t is None:
+        return None, 0
+    shape, stride = t.shape, t.stride()
+    assert t.is_cuda and t.dtype == dtype and shape[-1] == width and (stride[-1] == 1 or width == 1), f"{dtype} [{rows}, {width}] expected"
+    if len(shape) == 1:
+        return t.data_ptr(), 0
+    assert len(shape) == 2 and shape[0] == rows, f"{dtype} [{rows}, {width}] expected"
+    return t.data_ptr(), stride[0]
 
 
 def tl_k_choose(logits, counts, out, choice, repetition=1.0, presence=0.0, frequency=0.0, bias=None, allowed=None, workspace=None, stream=None):
     """logits fp32 [rows, vocab]; counts int32 and bias fp32 [rows, vocab] or [vocab], allowed int32 words of 32 bits, [rows, ceil(vocab / 32)] or
     one row, each or None; out fp32 like logits or None, choice int32 [rows] or None"""
     R, V = logits.shape
-
-    def row(t, dtype, width):
-        if t is None:
-            return None, 0
-        assert t.dtype == dtype and t.shape[-1] == width and (t.dim() == 1 or tuple(t.shape) == (R, width)), f"{dtype} [{R}, {width}] expected"
-        return _dp(t), t.stride(0) if t.dim() == 2 else 0
-
-    assert logits.dtype == torch.float32 and (choice is None or (choice.dtype == torch.int32 and choice.numel() == R))
-    _chk(_lib.tl_k_choose(*row(logits, torch.float32, V), R, V, *row(counts, torch.int32, V), repetition, presence, frequency,
-                          *row(bias, torch.float32, V), *row(allowed, torch.int32, (V + 31) // 32), *row(out, torch.float32, V), _dp(choice),
-                          _dp(workspace), workspace.numel() if workspace is not None else 0, _s(stream)))
+    lp, ldl = _row(logits, torch.float32, R, V)
+    cp, ldc = _row(counts, torch.int32, R, V)
+    bp, ldb = _row(bias, torch.float32, R, V)
+    ap, lda = _row(allowed, torch.int32, R, (V + 31) // 32)
+    op, ldo = _row(out, torch.float32, R, V)
+    hp, _ = _row(choice, torch.int32, 1, R)
+    wp, n = _ws(workspace)
+    _chk(_lib.tl_k_choose(lp, ldl, R, V, cp, ldc, repetition, presence, frequency, bp, ldb, ap, lda, op, ldo, hp, wp, n, _s(stream)))
 
 
 def tl_k_attention_fwd(q, k, v, n_heads, d_head, o, lse, stream=None):

@@ -232,7 +232,7 @@ __device__ __forceinline__ uint4 tail_values(const bf16_t* row, int u0, int end,
 }
 
 template <int D>
-__global__ __launch_bounds__(256) void attn8_cols_kernel(Cache8 c, int n_keys, const bf16_t* __restrict__ q, long ldq, int n_rows, int group,
+__global__ __launch_bounds__(256, 2) void attn8_cols_kernel(Cache8 c, int n_keys, const bf16_t* __restrict__ q, long ldq, int n_rows, int group,
                                                          float scale_log2e, bf16_t* __restrict__ o, long ldo, float* __restrict__ ws,
                                                          int blocks_per_split) {
     constexpr int PC = D / 64, NT = D / 16, LDP = D + 4;
@@ -252,113 +252,121 @@ __global__ __launch_bounds__(256) void attn8_cols_kernel(Cache8 c, int n_keys, c
 #pragma unroll
     for (int t = 0; t < NT; ++t) oacc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
-    for (int b = blockIdx.z * blocks_per_split + wave; b < b_end; b += 4) {
-        const bool tail = b == n_keys >> 6;
-        f32x4_t s[4];
-        uint4 vr[NT];
-        float ks = scale_log2e, vs = 1.f;
-        const long tile = ((long)b * c.heads + head) * 64 * D;
-        const int key0 = (m16 >> 2) * 16 + (m16 & 3);
-        if (!tail) {
-            uint4 kr[4][PC];
+    const int key0 = (m16 >> 2) * 16 + (m16 & 3), b_tail = n_keys >> 6, b_full = min(b_end, b_tail);
+    f32x4_t s[4];
+    float x[16];
+    bf16x8_t hi[2], lo[2];
+    // scores -> probabilities (times the values' scale), in two bf16 parts
+    auto softmax = [&](int b, float ks, float vs) {
+        float top = -INFINITY;
 #pragma unroll
-            for (int kg = 0; kg < 4; ++kg)
+        for (int i = 0; i < 16; ++i) x[i] = s[i >> 2][i & 3] * ks;
+        if ((b + 1) * 64L > least) {                       // (uniform) some column does not see all of the block
 #pragma unroll
-                for (int pc = 0; pc < PC; ++pc) kr[kg][pc] = *(const uint4*)(c.k + tile + pc * 4096 + (key0 + kg * 4) * 64 + g * 16);
-#pragma unroll
-            for (int t = 0; t < NT; ++t) vr[t] = *(const uint4*)(c.v + tile + (t * 16 + m16) * 64 + g * 16);
-            ks *= c.ks[(long)b * c.heads + head];
-            vs = c.vs[(long)b * c.heads + head];
-#pragma unroll
-            for (int kg = 0; kg < 4; ++kg) {
-                s[kg] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int pc = 0; pc < PC; ++pc) {
-                    s[kg] = mfma16(codes_bf16(kr[kg][pc].x, kr[kg][pc].y), qf[2 * pc], s[kg]);
-                    s[kg] = mfma16(codes_bf16(kr[kg][pc].z, kr[kg][pc].w), qf[2 * pc + 1], s[kg]);
-                }
-            }
-        } else {
-            const bf16_t* kt = c.kt + (long)head * 64 * D;
-#pragma unroll
-            for (int kg = 0; kg < 4; ++kg) {
-                s[kg] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int st = 0; st < 2 * PC; ++st)
-                    s[kg] = mfma16(__builtin_bit_cast(bf16x8_t, *(const uint4*)(kt + (st >> 1) * 4096 + (key0 + kg * 4) * 64 + g * 16 + (st & 1) * 8)),
-                                   qf[st], s[kg]);
-            }
+            for (int i = 0; i < 16; ++i)
+                if (b * 64 + g * 16 + i >= seen) x[i] = -INFINITY;
         }
-        const bool masked = (b + 1) * 64L > least;         // (uniform) some column does not see all of the block
-        const bool sees = (long)b * 64 < seen;
-        float x[16], top = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            x[i] = s[i >> 2][i & 3] * ks;
-            if (masked && b * 64 + g * 16 + i >= seen) x[i] = -INFINITY;
-            top = fmaxf(top, x[i]);
-        }
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, x[i]);
         top = fmaxf(top, __shfl_xor(top, 16, 64));
         top = fmaxf(top, __shfl_xor(top, 32, 64));
         const float mn = fmaxf(m, top), base = mn == -INFINITY ? 0.f : mn, alpha = __builtin_amdgcn_exp2f(m - base);
         m = mn;
         l *= alpha;
+        const float f = (long)b * 64 < seen ? vs : 0.f;    // (a block that a column does not see may have the scale NaN)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             x[i] = __builtin_amdgcn_exp2f(x[i] - base);
             l += x[i];
-            x[i] = sees ? x[i] * vs : 0.f;                 // (a block that it does not see may have the scale NaN)
-        }
-#pragma unroll
-        for (int t = 0; t < NT; ++t) oacc[t] *= alpha;
-        bf16x8_t hi[2], lo[2];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
+            x[i] *= f;
             hi[i >> 3][i & 7] = (__bf16)x[i];
             lo[i >> 3][i & 7] = (__bf16)(x[i] - (float)hi[i >> 3][i & 7]);
         }
-        if (!tail) {
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                const bf16x8_t a0 = codes_bf16(vr[t].x, vr[t].y), a1 = codes_bf16(vr[t].z, vr[t].w);
-                oacc[t] = mfma16(a0, hi[0], oacc[t]);
-                oacc[t] = mfma16(a1, hi[1], oacc[t]);
-                oacc[t] = mfma16(a0, lo[0], oacc[t]);
-                oacc[t] = mfma16(a1, lo[1], oacc[t]);
+        for (int t = 0; t < NT; ++t) oacc[t] *= alpha;
+    };
+    // a block's keys are asked for when the block before has used its own, its values when those have been used
+    uint4 kr[4][PC], vr[NT];
+    float ks_next = 0.f;
+    auto keys = [&](int b) {
+        const long at = (long)b * c.heads + head;
+#pragma unroll
+        for (int kg = 0; kg < 4; ++kg)
+#pragma unroll
+            for (int pc = 0; pc < PC; ++pc) kr[kg][pc] = *(const uint4*)(c.k + at * 64 * D + pc * 4096 + (key0 + kg * 4) * 64 + g * 16);
+        ks_next = c.ks[at];
+    };
+    int b = blockIdx.z * blocks_per_split + wave;
+    if (b < b_full) keys(b);
+    for (; b < b_full; b += 4) {
+        const long at = (long)b * c.heads + head;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) vr[t] = *(const uint4*)(c.v + at * 64 * D + (t * 16 + m16) * 64 + g * 16);
+        const float ks = ks_next * scale_log2e, vs = c.vs[at];
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int kg = 0; kg < 4; ++kg) {
+            s[kg] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int pc = 0; pc < PC; ++pc) {
+                s[kg] = mfma16(codes_bf16(kr[kg][pc].x, kr[kg][pc].y), qf[2 * pc], s[kg]);
+                s[kg] = mfma16(codes_bf16(kr[kg][pc].z, kr[kg][pc].w), qf[2 * pc + 1], s[kg]);
             }
-        } else {
-            const bf16_t* vt = c.vt + (long)head * 64 * D;
-            const int end = n_keys & 63;
-            bool odd = false;
+            __builtin_amdgcn_sched_barrier(0);             // (widened codes of more than one group would not fit the registers)
+        }
+        if (b + 4 < b_full) keys(b + 4);
+        softmax(b, ks, vs);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const bf16x8_t a0 = codes_bf16(vr[t].x, vr[t].y), a1 = codes_bf16(vr[t].z, vr[t].w);
+            oacc[t] = mfma16(a0, hi[0], oacc[t]);
+            oacc[t] = mfma16(a1, hi[1], oacc[t]);
+            oacc[t] = mfma16(a0, lo[0], oacc[t]);
+            oacc[t] = mfma16(a1, lo[1], oacc[t]);
+            if (t & 1) __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    if (b == b_tail && b < b_end) {                        // the tail, bf16: one wave's
+        const bf16_t *kt = c.kt + (long)head * 64 * D, *vt = c.vt + (long)head * 64 * D;
+        const int end = n_keys & 63;
+        bool odd = false;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) (void)tail_values(vt + (t * 16 + m16) * 64, g * 16 + h * 8, end, &odd);
+#pragma unroll
+        for (int kg = 0; kg < 4; ++kg) {
+            s[kg] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int st = 0; st < 2 * PC; ++st)
+                s[kg] = mfma16(__builtin_bit_cast(bf16x8_t, *(const uint4*)(kt + (st >> 1) * 4096 + (key0 + kg * 4) * 64 + g * 16 + (st & 1) * 8)),
+                               qf[st], s[kg]);
+        }
+        softmax(b, scale_log2e, 1.f);
+        if (!__builtin_amdgcn_ballot_w64(odd)) {
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) (void)tail_values(vt + (t * 16 + m16) * 64, g * 16 + h * 8, end, &odd);
-            if (!__builtin_amdgcn_ballot_w64(odd)) {
+                for (int h = 0; h < 2; ++h) {
+                    const bf16x8_t a = __builtin_bit_cast(bf16x8_t, tail_values(vt + (t * 16 + m16) * 64, g * 16 + h * 8, end, &odd));
+                    oacc[t] = mfma16(a, hi[h], oacc[t]);
+                    oacc[t] = mfma16(a, lo[h], oacc[t]);
+                }
+        } else {
+            // a value that is not finite counts for the columns that see it alone, which a product with zeros does not give
+            float* pl = &part[wave][0][0];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) pl[(g * 16 + i) * 16 + m16] = x[i];
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            for (int u = 0; u < end && b * 64 + u < seen; ++u) {
+                const float p = pl[u * 16 + m16];
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const bf16x8_t a = __builtin_bit_cast(bf16x8_t, tail_values(vt + (t * 16 + m16) * 64, g * 16 + h * 8, end, &odd));
-                        oacc[t] = mfma16(a, hi[h], oacc[t]);
-                        oacc[t] = mfma16(a, lo[h], oacc[t]);
-                    }
-            } else {
-                // a value that is not finite counts for the columns that see it alone, which a product with zeros does not give
-                float* pl = &part[wave][0][0];
-#pragma unroll
-                for (int i = 0; i < 16; ++i) pl[(g * 16 + i) * 16 + m16] = x[i];
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                __builtin_amdgcn_wave_barrier();
-                for (int u = 0; u < end && b * 64 + u < seen; ++u) {
-                    const float p = pl[u * 16 + m16];
-#pragma unroll
-                    for (int t = 0; t < NT; ++t)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) oacc[t][i] = fmaf(p, bf16_to_f32(vt[(t * 16 + g * 4 + i) * 64 + u]), oacc[t][i]);
-                }
-                __builtin_amdgcn_wave_barrier();
+                    for (int i = 0; i < 4; ++i) oacc[t][i] = fmaf(p, bf16_to_f32(vt[(t * 16 + g * 4 + i) * 64 + u]), oacc[t][i]);
             }
+            __builtin_amdgcn_wave_barrier();
         }
     }
     l += __shfl_xor(l, 16, 64);
@@ -391,17 +399,33 @@ __global__ __launch_bounds__(256) void attn8_cols_kernel(Cache8 c, int n_keys, c
     }
 }
 
-// The ranges of a row and head, one thread a column: lane i holds range i's maximum and sum.
+// The ranges of a row and head, one thread a column: lane i holds range i's maximum and sum, and sixteen ranges' columns are asked for before
+// the first is used.
 template <int D>
 __global__ __launch_bounds__(D) void attn8_join_kernel(const float* __restrict__ ws, int n_split, int heads, bf16_t* __restrict__ o, long ldo) {
     const int e = threadIdx.x, lane = threadIdx.x & 63;
     const float* w = ws + (long)blockIdx.x * n_split * (D + 2);
     const int r = min(lane, n_split - 1);
-    const float m = lane < n_split ? w[r * (D + 2) + D] : -INFINITY, l = w[r * (D + 2) + D + 1];
-    const float top = wave_max(m), a = __builtin_amdgcn_exp2f(m - top);      // (one range has keys: top is a number, or NaN)
+    const float m = w[r * (D + 2) + D], l = w[r * (D + 2) + D + 1];
+    float t[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) t[i] = w[min(i, n_split - 1) * (D + 2) + e];
+    __builtin_amdgcn_sched_barrier(0);
+    const float top = wave_max(lane < n_split ? m : -INFINITY);
+    const float a = lane < n_split ? __builtin_amdgcn_exp2f(m - top) : 0.f;      // (one range has keys: top is a number, or all is NaN)
     const float sum = wave_sum(lane < n_split ? a * l : 0.f);
     float acc = 0.f;
-    for (int i = 0; i < n_split; ++i) acc += __shfl(a, i, 64) * w[i * (D + 2) + e];
+    for (int i0 = 0; i0 < n_split; i0 += 16) {
+        if (i0) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) t[i] = w[min(i0 + i, n_split - 1) * (D + 2) + e];
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float ai = __shfl(a, i0 + i, 64);
+            acc += i0 + i < n_split ? ai * t[i] : 0.f;
+        }
+    }
     o[(long)(blockIdx.x / heads) * ldo + (long)(blockIdx.x % heads) * D + e] = f32_to_bf16(acc / sum);
 }
 
