@@ -25,109 +25,135 @@ __device__ __forceinline__ int code8(float x, float s, float inv) {
     return i + up - down;
 }
 
-// Threads of a workgroup share a tile of 64 tokens of one head: keys by rows (thread: 8 columns of every STEP-th token), values by
-// columns (thread: two columns of TPT consecutive tokens), each as it is stored.
+// A workgroup of 2 D threads shares a tile of 64 tokens of one head; a thread has 8 columns of 4 consecutive tokens, in 16-byte pieces of a row.
 template <int D>
 struct Cache8Tile {
-    static constexpr int CPR = D / 8, STEP = 256 / CPR, NK = 64 / STEP;     // keys: chunks a row, tokens a pass, passes
-    static constexpr int NG = 256 / (D / 2), TPT = 64 / NG;                 // values: token groups, tokens a thread
+    static constexpr int CPR = D / 8, NT = 2 * D;
+    static_assert(NT / CPR == 16, "16 groups of 4 tokens");
 };
+constexpr int VP = 17;      // words of a value row (64 codes) in LDS: odd, so that rows begin in different banks
 
 // One workgroup for a block that the new tokens complete and a head's keys or values (block by block, the heads' keys before their
 // values).  Those of the first block also put the rows behind the last complete block into the tail, after they have read the tail.
 template <int D>
-__global__ __launch_bounds__(256) void cache8_append_kernel(Cache8 c, int n_cached, const bf16_t* __restrict__ k, long ldk,
-                                                            const bf16_t* __restrict__ v, long ldv, int n_new) {
+__global__ __launch_bounds__(2 * D) void cache8_append_kernel(Cache8 c, int n_cached, const bf16_t* __restrict__ k, long ldk,
+                                                              const bf16_t* __restrict__ v, long ldv, int n_new) {
     using T = Cache8Tile<D>;
     __shared__ int red[4];
+    __shared__ unsigned sv[D * VP];
     const int tid = threadIdx.x, at = blockIdx.x % (2 * c.heads), nth = blockIdx.x / (2 * c.heads);
     const bool values = at >= c.heads;
     const int head = values ? at - c.heads : at;
-    const int b0 = n_cached >> 6, end = n_cached + n_new, b1 = end >> 6, block = b0 + nth;
-    const int first = block << 6;                          // position of the tile's first token
-    const bf16_t* src = (values ? v : k) + (long)head * D;
+    const int end = n_cached + n_new, b1 = end >> 6, block = (n_cached >> 6) + nth;
+    const int col = tid % T::CPR * 8, t0 = tid / T::CPR * 4;
+    const bf16_t* src = (values ? v : k) + (long)head * D + col;
     const long ld = values ? ldv : ldk;
     bf16_t* tail = (values ? c.vt : c.kt) + (long)head * 64 * D;
-    const long tile = ((long)block * c.heads + head) * 64 * D;
-    const int kc = tid % T::CPR * 8, kt = tid / T::CPR;                     // keys: first column, first token
-    const int vc = tid % (D / 2) * 2, vt = tid / (D / 2) * T::TPT;          // values: first column, first token
-    auto finish = [&](int amax) {                          // bf16 bits of the largest magnitude -> the scale
+    bf16_t* k_slot = tail + (col >> 6) * 4096 + t0 * 64 + (col & 63);       // keys: token t0, the thread's columns; a token further: + 64
+    bf16_t* v_slot = tail + col * 64 + t0;                                  // values: the thread's tokens, its first column; a column further: + 64
+    // the rows of the block that stays incomplete: on their way before anything else is done
+    const int base = b1 << 6, lo = max(n_cached, base);
+    uint4 rest[4];
+    if (nth == 0) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (base + t0 + i >= lo && base + t0 + i < end) rest[i] = *(const uint4*)(src + (long)(base + t0 + i - n_cached) * ld);
+    }
+    if (block < b1) {
+        const int first = block << 6;
+        uint4 x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (first + t0 + i >= n_cached) x[i] = *(const uint4*)(src + (long)(first + t0 + i - n_cached) * ld);
+        if (first + t0 < n_cached) {                       // some of its tokens are in the tail
+            if (!values) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (first + t0 + i < n_cached) x[i] = *(const uint4*)(k_slot + 64 * i);
+            } else {
+                uint2 w[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w[e] = *(const uint2*)(v_slot + 64 * e);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (first + t0 + i < n_cached) {
+                        auto get = [&](int e) { return ((i < 2 ? w[e].x : w[e].y) >> 16 * (i & 1)) & 0xffffu; };
+                        x[i] = make_uint4(get(0) | get(1) << 16, get(2) | get(3) << 16, get(4) | get(5) << 16, get(6) | get(7) << 16);
+                    }
+            }
+        }
+        int amax = 0;                                      // bf16 bits of the largest magnitude
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const unsigned w = (&x[i].x)[e];
+                amax = max(amax, max((int)(w & 0x7fff), (int)(w >> 16 & 0x7fff)));
+            }
 #pragma unroll
         for (int off = 32; off > 0; off >>= 1) amax = max(amax, __shfl_xor(amax, off, 64));
         if ((tid & 63) == 0) red[tid >> 6] = amax;
-        __syncthreads();
-        amax = max(max(red[0], red[1]), max(red[2], red[3]));
+        __syncthreads();                                   // (and every thread has what it needs of the tail)
+#pragma unroll
+        for (int w = 0; w < T::NT / 64; ++w) amax = max(amax, red[w]);
         // a value that is not finite has no code: the scale is NaN, and so is everything read through it
-        const float s = amax >= 0x7f80 ? __builtin_nanf("") : fmaxf(__uint_as_float((unsigned)amax << 16), kLeastMagnitude) / 127.f;
+        const bool fine = amax < 0x7f80;
+        const float s = fine ? fmaxf(__uint_as_float((unsigned)amax << 16), kLeastMagnitude) / 127.f : __builtin_nanf(""), inv = 1.f / s;
         if (tid == 0) (values ? c.vs : c.ks)[(long)block * c.heads + head] = s;
-        return s;
-    };
-    if (block < b1) {
+        const long tile = ((long)block * c.heads + head) * 64 * D;
+        unsigned q[4][2];                                  // token by token
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float f[8];
+            unpack8(x[i], f);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                unsigned w = 0;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w |= (unsigned)(code8(f[4 * h + e], s, inv) & 255) << 8 * e;
+                q[i][h] = fine ? w : 0;
+            }
+        }
         if (!values) {
-            uint4 x[T::NK];
 #pragma unroll
-            for (int i = 0; i < T::NK; ++i) {
-                const int t = kt + i * T::STEP;
-                x[i] = first + t < n_cached ? *(const uint4*)(tail + (kc >> 6) * 4096 + t * 64 + (kc & 63))
-                                            : *(const uint4*)(src + (long)(first + t - n_cached) * ld + kc);
-            }
-            int amax = 0;
-#pragma unroll
-            for (int i = 0; i < T::NK; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const unsigned w = (&x[i].x)[e];
-                    amax = max(amax, max((int)(w & 0x7fff), (int)(w >> 16 & 0x7fff)));
-                }
-            const float s = finish(amax), inv = 1.f / s;
-#pragma unroll
-            for (int i = 0; i < T::NK; ++i) {
-                float f[8];
-                unpack8(x[i], f);
-                unsigned w[2] = {0, 0};
-#pragma unroll
-                for (int e = 0; e < 8; ++e) w[e >> 2] |= (unsigned)(s == s ? code8(f[e], s, inv) & 255 : 0) << 8 * (e & 3);
-                *(uint2*)(c.k + tile + (kc >> 6) * 4096 + (kt + i * T::STEP) * 64 + (kc & 63)) = make_uint2(w[0], w[1]);
-            }
+            for (int i = 0; i < 4; ++i) *(uint2*)(c.k + tile + (col >> 6) * 4096 + (t0 + i) * 64 + (col & 63)) = make_uint2(q[i][0], q[i][1]);
         } else {
-            unsigned x[T::TPT];                            // columns vc, vc + 1
 #pragma unroll
-            for (int i = 0; i < T::TPT; ++i) {
-                const int t = vt + i;
-                x[i] = first + t < n_cached ? (unsigned)tail[vc * 64 + t] | (unsigned)tail[vc * 64 + 64 + t] << 16
-                                            : *(const unsigned*)(src + (long)(first + t - n_cached) * ld + vc);
+            for (int e = 0; e < 8; ++e) {                  // byte e % 4 of the four tokens' words
+                const unsigned sel = 0x0c0c0400u + 0x0101u * (e & 3);
+                const unsigned lo2 = __builtin_amdgcn_perm(q[1][e >> 2], q[0][e >> 2], sel), hi2 = __builtin_amdgcn_perm(q[3][e >> 2], q[2][e >> 2], sel);
+                sv[(col + e) * VP + (t0 >> 2)] = lo2 | hi2 << 16;
             }
-            int amax = 0;
+            __syncthreads();
 #pragma unroll
-            for (int i = 0; i < T::TPT; ++i) amax = max(amax, max((int)(x[i] & 0x7fff), (int)(x[i] >> 16 & 0x7fff)));
-            const float s = finish(amax), inv = 1.f / s;
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                unsigned w[T::TPT / 4];
-#pragma unroll
-                for (int i = 0; i < T::TPT; ++i) {
-                    const float f = __uint_as_float(j ? x[i] & 0xffff0000u : x[i] << 16);
-                    const unsigned q = (unsigned)(s == s ? code8(f, s, inv) & 255 : 0) << 8 * (i & 3);
-                    w[i >> 2] = i & 3 ? w[i >> 2] | q : q;
-                }
-#pragma unroll
-                for (int i = 0; i < T::TPT / 4; i += 2)
-                    *(uint2*)(c.v + tile + (vc + j) * 64 + vt + 4 * i) = make_uint2(w[i], w[i + 1]);
+            for (int i = 0; i < 2; ++i) {
+                const int p = i * T::NT + tid;             // 16 bytes of the tile
+                const unsigned* w = sv + (p >> 2) * VP + (p & 3) * 4;
+                *(uint4*)(c.v + tile + p * 16) = make_uint4(w[0], w[1], w[2], w[3]);
             }
         }
-        __syncthreads();                                   // (uniform) every wave has what it needs of the tail
     }
-    if (nth > 0) return;
-    const int base = b1 << 6, lo = max(n_cached, base);    // the new rows of the block that stays incomplete
+    if (nth > 0 || base + t0 + 3 < lo || base + t0 >= end) return;
     if (!values) {
-        for (int t = lo - base + kt; t < end - base; t += T::STEP)
-            *(uint4*)(tail + (kc >> 6) * 4096 + t * 64 + (kc & 63)) = *(const uint4*)(src + (long)(base + t - n_cached) * ld + kc);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (base + t0 + i >= lo && base + t0 + i < end) *(uint4*)(k_slot + 64 * i) = rest[i];
     } else {
-        for (int t = max(vt, lo - base); t < min(vt + T::TPT, end - base); ++t) {
-            const unsigned w = *(const unsigned*)(src + (long)(base + t - n_cached) * ld + vc);
-            tail[vc * 64 + t] = (bf16_t)w;
-            tail[vc * 64 + 64 + t] = (bf16_t)(w >> 16);
-        }
+        uint2 w[8];                                        // the thread's four tokens as they are, the new ones put in
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = *(const uint2*)(v_slot + 64 * e);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (base + t0 + i >= lo && base + t0 + i < end) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const unsigned u = (&rest[i].x)[e >> 1] >> 16 * (e & 1) & 0xffffu;
+                    unsigned& old = i < 2 ? w[e].x : w[e].y;
+                    old = i & 1 ? (old & 0xffffu) | u << 16 : (old & 0xffff0000u) | u;
+                }
+            }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) *(uint2*)(v_slot + 64 * e) = w[e];
     }
 }
 hipError_t launch_cache8_append(const Cache8& c, int n_cached, const bf16_t* k, long ldk, const bf16_t* v, long ldv, int n_new,
@@ -138,7 +164,7 @@ hipError_t launch_cache8_append(const Cache8& c, int n_cached, const bf16_t* k, 
         const int grid = 2 * c.heads * (done > 1 ? done : 1);
         const bf16_t *ki = k + (long)i * ldk, *vi = v + (long)i * ldv;
         if (c.d == 128) cache8_append_kernel<128><<<grid, 256, 0, s>>>(c, at, ki, ldk, vi, ldv, m);
-        else cache8_append_kernel<64><<<grid, 256, 0, s>>>(c, at, ki, ldk, vi, ldv, m);
+        else cache8_append_kernel<64><<<grid, 128, 0, s>>>(c, at, ki, ldk, vi, ldv, m);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         i += m;
@@ -146,44 +172,60 @@ hipError_t launch_cache8_append(const Cache8& c, int n_cached, const bf16_t* k, 
     return hipSuccess;
 }
 
-// Tokens first .. first + n - 1 of a cache that holds n_cached as fp32 rows: code * scale (one rounding), the tail's widened.
+// Tokens first .. first + n - 1 of a cache that holds n_cached as fp32 rows: code * scale (one rounding), the tail's widened.  A thread
+// writes 4 columns of a row at a time; values are turned round through LDS, as codes.
 template <int D>
-__global__ __launch_bounds__(256) void cache8_read_kernel(Cache8 c, int n_cached, int first, int n, float* __restrict__ k, long ldk,
-                                                          float* __restrict__ v, long ldv) {
-    using T = Cache8Tile<D>;
+__global__ __launch_bounds__(2 * D) void cache8_read_kernel(Cache8 c, int n_cached, int first, int n, float* __restrict__ k, long ldk,
+                                                            float* __restrict__ v, long ldv) {
+    constexpr int NT = 2 * D, CPR = D / 4, NP = 64 * CPR / NT;              // pieces of 4 columns: a row, a thread
+    __shared__ unsigned sv[D * VP];
     const int tid = threadIdx.x, at = blockIdx.x % (2 * c.heads), block = (first >> 6) + blockIdx.x / (2 * c.heads);
     const bool values = at >= c.heads, in_tail = block == n_cached >> 6;
-    const int head = values ? at - c.heads : at, base = block << 6;
+    const int head = values ? at - c.heads : at, row0 = (block << 6) - first;
     const long tile = ((long)block * c.heads + head) * 64 * D;
     const bf16_t* tail = (values ? c.vt : c.kt) + (long)head * 64 * D;
-    const float s = in_tail ? 1.f : (values ? c.vs : c.ks)[(long)block * c.heads + head];
-    if (!values) {
-        const int kc = tid % T::CPR * 8, kt = tid / T::CPR;
-#pragma unroll
-        for (int i = 0; i < T::NK; ++i) {
-            const int t = kt + i * T::STEP, row = base + t - first, off = (kc >> 6) * 4096 + t * 64 + (kc & 63);
-            if (row < 0 || row >= n) continue;
-            float f[8];
-            if (in_tail) unpack8(*(const uint4*)(tail + off), f);
-            else {
-                const uint2 w = *(const uint2*)(c.k + tile + off);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) f[e] = (float)(int8_t)((e < 4 ? w.x : w.y) >> 8 * (e & 3)) * s;
-            }
-            float* out = k + (long)row * ldk + (long)head * D + kc;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) out[e] = f[e];
+    const int col = tid % CPR * 4, t0 = tid / CPR;                          // 8 token groups
+    float* out = (values ? v : k) + (long)head * D + col;
+    const long ld = values ? ldv : ldk;
+    auto put = [&](int t, float a, float b, float e, float f) {
+        const int row = row0 + t;
+        if (row >= 0 && row < n) *(float4*)(out + (long)row * ld) = make_float4(a, b, e, f);
+    };
+    if (in_tail) {
+        for (int t = t0; t < 64; t += 8) {
+            if (row0 + t < 0 || row0 + t >= n) continue;
+            const bf16_t* p = values ? tail + col * 64 + t : tail + (col >> 6) * 4096 + t * 64 + (col & 63);
+            const int step = values ? 64 : 1;
+            put(t, bf16_to_f32(p[0]), bf16_to_f32(p[step]), bf16_to_f32(p[2 * step]), bf16_to_f32(p[3 * step]));
         }
-    } else {
-        const int vc = tid % (D / 2) * 2, vt = tid / (D / 2) * T::TPT;
+        return;
+    }
+    const float s = (values ? c.vs : c.ks)[(long)block * c.heads + head];
+    auto value = [&](unsigned w, int e) { return (float)(int8_t)(w >> 8 * e) * s; };
+    if (!values) {
+        unsigned w[NP];
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int i = 0; i < NP; ++i) w[i] = *(const unsigned*)(c.k + tile + (col >> 6) * 4096 + (t0 + 8 * i) * 64 + (col & 63));
 #pragma unroll
-            for (int i = 0; i < T::TPT; ++i) {
-                const int row = base + vt + i - first, off = (vc + j) * 64 + vt + i;
-                if (row < 0 || row >= n) continue;
-                v[(long)row * ldv + (long)head * D + vc + j] = in_tail ? bf16_to_f32(tail[off]) : (float)c.v[tile + off] * s;
-            }
+        for (int i = 0; i < NP; ++i) put(t0 + 8 * i, value(w[i], 0), value(w[i], 1), value(w[i], 2), value(w[i], 3));
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int p = i * NT + tid;
+        const uint4 w = *(const uint4*)(c.v + tile + p * 16);
+        unsigned* to = sv + (p >> 2) * VP + (p & 3) * 4;
+        to[0] = w.x, to[1] = w.y, to[2] = w.z, to[3] = w.w;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {                                          // four tokens of the thread's columns
+        const int tg = t0 + 8 * i;
+        unsigned w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = sv[(col + j) * VP + tg];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) put(tg * 4 + e, value(w[0], e), value(w[1], e), value(w[2], e), value(w[3], e));
     }
 }
 hipError_t launch_cache8_read(const Cache8& c, int n_cached, int first, int n, float* k, long ldk, float* v, long ldv, hipStream_t s) {
@@ -192,7 +234,7 @@ hipError_t launch_cache8_read(const Cache8& c, int n_cached, int first, int n, f
         const int grid = 2 * c.heads * (((at + m - 1) >> 6) - (at >> 6) + 1);
         float *ki = k + (long)i * ldk, *vi = v + (long)i * ldv;
         if (c.d == 128) cache8_read_kernel<128><<<grid, 256, 0, s>>>(c, n_cached, at, m, ki, ldk, vi, ldv);
-        else cache8_read_kernel<64><<<grid, 256, 0, s>>>(c, n_cached, at, m, ki, ldk, vi, ldv);
+        else cache8_read_kernel<64><<<grid, 128, 0, s>>>(c, n_cached, at, m, ki, ldk, vi, ldv);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         i += m;
