@@ -243,8 +243,8 @@ hipError_t launch_cache8_read(const Cache8& c, int n_cached, int first, int n, f
 }
 
 // ---------------------------------------------------------------- attention of a few rows
-// A row of queries and one of the query heads that share a key head make a column; 16 columns of one key head are a workgroup's, and
-// each of its four waves takes every fourth block of the workgroup's range of the cache:
+// A row of queries and one of the query heads that share a key head make a column; a workgroup has the (up to 16) columns of one key head,
+// and each of its four waves takes every fourth block of the workgroup's range of the cache:
 //   S^T[key][column] = K q^T   and   O^T[d][column] += V^T P^T     by v_mfma_f32_16x16x32_bf16
 // (lane = 16 g + m:  A: row m, contraction slots 8 g ..;  B: column m, the same slots;  D: column m, rows 4 g .. 4 g + 3).  Codes are
 // whole numbers up to 127, exact in bf16, so the scores are products of what is stored, summed in fp32, and the scales come in behind:
@@ -253,6 +253,12 @@ hipError_t launch_cache8_read(const Cache8& c, int n_cached, int first, int n, f
 // group g then holds the scores of keys 16 g .. 16 g + 15, which are the slots it has to bring as the second product's operand and the
 // values it loads as 16 bytes of a row of V^T; nothing is exchanged between lanes but the maximum and the sum.
 __device__ __forceinline__ f32x4_t mfma16(bf16x8_t a, bf16x8_t b, f32x4_t c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+// 16 codes that are read once: non-temporal, 131072 keys of 8 heads 52 -> 47 us
+typedef unsigned u32x4_t __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ uint4 load_once(const void* p) {
+    const u32x4_t v = __builtin_nontemporal_load((const u32x4_t*)p);
+    return make_uint4(v.x, v.y, v.z, v.w);
+}
 // eight codes -> bf16
 __device__ __forceinline__ bf16x8_t codes_bf16(unsigned lo, unsigned hi) {
     bf16x8_t r;
@@ -280,11 +286,10 @@ __global__ __launch_bounds__(256, 2) void attn8_cols_kernel(Cache8 c, int n_keys
     constexpr int PC = D / 64, NT = D / 16, LDP = D + 4;
     __shared__ float part[4][16][LDP];                     // a column's output, maximum and sum, wave by wave
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m16 = lane & 15, g = lane >> 4;
-    const int head = blockIdx.x, c0 = blockIdx.y * 16, n_cols = n_rows * group, heads = c.heads * group;
-    const int col = min(c0 + m16, n_cols - 1), row = col / group, seen = n_keys - n_rows + row + 1;      // keys 0 .. seen - 1
-    const int least = n_keys - n_rows + c0 / group + 1;                                                  // the first column's
-    const int most = n_keys - n_rows + min(c0 + 15, n_cols - 1) / group + 1;                             // the last column's
-    const int b_end = min((int)(blockIdx.z + 1) * blocks_per_split, (most + 63) >> 6);
+    const int head = blockIdx.x, n_cols = n_rows * group, heads = c.heads * group;
+    const int col = min(m16, n_cols - 1), row = col / group, seen = n_keys - n_rows + row + 1;      // keys 0 .. seen - 1
+    const int least = n_keys - n_rows + 1;                                                              // the first column's
+    const int b_end = min((int)(blockIdx.y + 1) * blocks_per_split, (n_keys + 63) >> 6);
     const bf16_t* qr = q + (long)row * ldq + (long)(head * group + col % group) * D + g * 16;
     bf16x8_t qf[2 * PC];
 #pragma unroll
@@ -335,15 +340,15 @@ __global__ __launch_bounds__(256, 2) void attn8_cols_kernel(Cache8 c, int n_keys
 #pragma unroll
         for (int kg = 0; kg < 4; ++kg)
 #pragma unroll
-            for (int pc = 0; pc < PC; ++pc) kr[kg][pc] = *(const uint4*)(c.k + at * 64 * D + pc * 4096 + (key0 + kg * 4) * 64 + g * 16);
+            for (int pc = 0; pc < PC; ++pc) kr[kg][pc] = load_once(c.k + at * 64 * D + pc * 4096 + (key0 + kg * 4) * 64 + g * 16);
         ks_next = c.ks[at];
     };
-    int b = blockIdx.z * blocks_per_split + wave;
+    int b = blockIdx.y * blocks_per_split + wave;
     if (b < b_full) keys(b);
     for (; b < b_full; b += 4) {
         const long at = (long)b * c.heads + head;
 #pragma unroll
-        for (int t = 0; t < NT; ++t) vr[t] = *(const uint4*)(c.v + at * 64 * D + (t * 16 + m16) * 64 + g * 16);
+        for (int t = 0; t < NT; ++t) vr[t] = load_once(c.v + at * 64 * D + (t * 16 + m16) * 64 + g * 16);
         const float ks = ks_next * scale_log2e, vs = c.vs[at];
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -419,7 +424,7 @@ __global__ __launch_bounds__(256, 2) void attn8_cols_kernel(Cache8 c, int n_keys
     __syncthreads();
     for (int i = threadIdx.x; i < 16 * D; i += 256) {
         const int cc = i / D, e = i % D;
-        if (c0 + cc >= n_cols) break;
+        if (cc >= n_cols) break;
         float mt = part[0][cc][D];
 #pragma unroll
         for (int w = 1; w < 4; ++w) mt = fmaxf(mt, part[w][cc][D]);
@@ -431,10 +436,10 @@ __global__ __launch_bounds__(256, 2) void attn8_cols_kernel(Cache8 c, int n_keys
             lt += a * part[w][cc][D + 1];
             ot += a * part[w][cc][e];
         }
-        const int r = (c0 + cc) / group, qh = head * group + (c0 + cc) % group;
+        const int r = cc / group, qh = head * group + cc % group;
         if (!ws) o[(long)r * ldo + (long)qh * D + e] = f32_to_bf16(ot / lt);
         else {
-            float* out = ws + (((long)r * heads + qh) * gridDim.z + blockIdx.z) * (D + 2);
+            float* out = ws + (((long)r * heads + qh) * gridDim.y + blockIdx.y) * (D + 2);
             out[e] = ot;
             if (e == 0) { out[D] = mt; out[D + 1] = lt; }
         }
@@ -685,16 +690,37 @@ static constexpr size_t attn8_rows_lds() {
 }
 
 // Which kernel, and how the keys are cut.
-//   columns  16 columns a workgroup: its waves read the cache at once and convert every code for 16 columns
-//   rows64, rows128, rows256  that many columns a workgroup
+//   columns16         up to 16 columns of a key head.  us for 2 rows of 32 heads of 128, this and rows128: 300 keys 8.2 and 8.1, 1500 9.5 and 12.5,
+//                     4000 12.2 and 18.6; 17 rows: 300 keys 10.2 and 8.7, 1500 13.3 and 13.2, 4000 19.1 and 15.5
+//   rows128, rows256  more columns: 256 to a workgroup where that leaves 16 workgroups or more for a range of the keys (2048 rows of 32 heads over 8192
+//                     keys 286; 200 rows, 4000 keys, 128 and 256: 32 heads 37.2 and 34.5, 4 heads 16.7 and 19.0)
+// Ranges, columns16: none up to 8 blocks (one row of 32 heads, 500 keys: 8.6 without, 8.7 at best; 700 keys 11.0 and 9.0); else two workgroups a CU, of
+// three blocks or more, but one a CU where each has over 16 blocks (131072 keys of 8 heads 52.1 and 50.2, 32768 of 32 52.0 and 49.5).
+// Ranges, rows: what costs least of a launch's tiles one after another (1.75 us each with one workgroup of 128 columns on a CU, 2.7 with two; 2.3 of 256
+// columns) and of the join (3 us, and its floats written and read at 3.5 TB/s).
 struct Attn8Plan { int cols, n_split, per; };       // columns a workgroup, ranges, blocks a range
 static Attn8Plan attn8_plan(int n_keys, int n_rows, int heads, int kv_heads, int d, size_t ws_elems) {
     const int nb = cdiv(n_keys, 64);
     const long n_cols = (long)n_rows * (heads / kv_heads);
-    const int cols = n_cols <= 32 ? 16 : n_cols <= 64 ? 64 : n_cols <= 128 ? 128 : 256;
-    const long units = kv_heads * (long)cdiv(n_cols, cols);
-    long n = cols == 16 ? std::min<long>(512 / units, cdiv(nb, 4)) : std::min<long>((cols == 256 ? 256 : 512) / units, cdiv(nb, 4));
-    n = std::min<long>(std::min<long>(n, ATTN8_MAX_SPLIT), (long)(ws_elems / ((size_t)n_rows * heads * (d + 2))));
+    const int cols = n_cols <= 16 ? 16 : n_cols <= 128 || kv_heads * (long)cdiv(n_cols, 256) < 16 ? 128 : 256;
+    const long units = kv_heads * (long)cdiv(n_cols, cols), range_elems = (long)n_rows * heads * (d + 2);
+    const long most = std::min<long>(std::min<long>(nb, ATTN8_MAX_SPLIT), (long)(ws_elems / (size_t)range_elems));
+    long n = 1;
+    if (cols == 16) {
+        if (nb > 8) {
+            n = std::min<long>(512 / units, cdiv(nb, 3));
+            if (n > 1 && cdiv(nb, n) > 16) n = 256 / units;
+        }
+        n = std::min(n, most);
+    } else {
+        auto cost = [&](long r) {
+            const long w = units * r, slots = cols == 128 ? 512 : 256, rest = w % slots;
+            const double tile = cols == 128 ? 2.7 : 2.3, last = rest == 0 ? 0. : cols == 128 && rest <= 256 ? 1.75 : tile;
+            return cdiv(nb, r) * ((double)(w / slots) * tile + last) + (r > 1 ? 3. + 8. * r * range_elems / 3.5e6 : 0.);
+        };
+        for (long r = 2; r <= most; ++r)
+            if (cost(r) < cost(n)) n = r;
+    }
     if (n < 2) return {cols, 1, nb};
     const int per = cdiv(nb, n);
     return {cols, cdiv(nb, per), per};
@@ -702,7 +728,7 @@ static Attn8Plan attn8_plan(int n_keys, int n_rows, int heads, int kv_heads, int
 const char* attention_cache8_plan(int n_keys, int n_rows, int heads, int kv_heads, int d, size_t ws_elems, int* n_ranges) {
     const Attn8Plan p = attn8_plan(n_keys, n_rows, heads, kv_heads, d, ws_elems);
     *n_ranges = p.n_split;
-    return p.cols == 16 ? "columns" : p.cols == 64 ? "rows64" : p.cols == 128 ? "rows128" : "rows256";
+    return p.cols == 16 ? "columns16" : p.cols == 128 ? "rows128" : "rows256";
 }
 template <int D>
 static hipError_t run_attention_cache8(const Attn8Plan& p, const Cache8& c, int n_keys, const bf16_t* q, long ldq, int n_rows, int group, bf16_t* o,
@@ -720,10 +746,10 @@ static hipError_t run_attention_cache8(const Attn8Plan& p, const Cache8& c, int 
         return hipGetLastError();
     };
     hipError_t e;
-    if (p.cols == 16) {
-        attn8_cols_kernel<D><<<dim3(c.heads, cdiv(n_cols, 16), p.n_split), 256, 0, s>>>(c, n_keys, q, ldq, n_rows, group, scale, o, ldo, w, p.per);
+    if (p.cols == 16) {                                    // (one workgroup holds all the columns of a key head)
+        attn8_cols_kernel<D><<<dim3(c.heads, p.n_split), 256, 0, s>>>(c, n_keys, q, ldq, n_rows, group, scale, o, ldo, w, p.per);
         e = hipGetLastError();
-    } else e = p.cols == 64 ? rows(std::integral_constant<int, 2>{}) : p.cols == 128 ? rows(std::integral_constant<int, 4>{}) : rows(std::integral_constant<int, 8>{});
+    } else e = p.cols == 128 ? rows(std::integral_constant<int, 4>{}) : rows(std::integral_constant<int, 8>{});
     if (e != hipSuccess || !w) return e;
     attn8_join_kernel<D><<<n_rows * c.heads * group, D, 0, s>>>(w, p.n_split, c.heads * group, o, ldo);
     return hipGetLastError();

@@ -147,7 +147,7 @@ def check(api, c, n, k, v, q, heads, kv, workspace=None, p_rounding=None):
     d = c.d_head
     if p_rounding is None:
         name = api.tl_k_attention_cache8_plan(n, q.shape[0], heads, kv, d, 0 if workspace is None else workspace.numel())[0]
-        p_rounding = HI_LO if name == "columns" else BF16
+        p_rounding = HI_LO if name == "columns16" else BF16
     got = attend(api, c, n, q, heads, workspace).double().view(q.shape[0], heads, d)
     want, size, reach = oracle.attention(q, oracle.held(k[:n], kv)[0], oracle.held(v[:n], kv)[0], heads)
     far = (got - want).abs() - oracle.attention_bound(want, size, reach, d, n, p_rounding)
@@ -180,7 +180,7 @@ def test_rows(api, rows, n, heads, kv, d):
 
 @pytest.mark.parametrize("heads,kv,d,rows,n", [
     (1, 1, 64, 300, 301), (1, 1, 128, 256, 512), (2, 2, 128, 257, 400), (6, 2, 64, 90, 700), (8, 1, 128, 33, 500), (8, 1, 64, 130, 131),
-    (1, 1, 128, 700, 700), (3, 1, 64, 11, 4000), (5, 1, 128, 13, 2500), (2, 2, 64, 40, 63), (4, 4, 128, 100, 2063)])
+    (1, 1, 128, 700, 700), (16, 16, 64, 140, 300), (16, 16, 128, 257, 321), (16, 16, 64, 300, 300), (3, 1, 64, 11, 4000), (5, 1, 128, 13, 2500), (2, 2, 64, 40, 63), (4, 4, 128, 100, 2063)])
 def test_many_columns(api, heads, kv, d, rows, n):
     k, v = draw(n + rows, n, kv, d)
     c = fill(api, k, v, kv, capacity=n + 1)
@@ -191,9 +191,9 @@ def test_many_columns(api, heads, kv, d, rows, n):
 
 def test_every_kernel_is_reached(api):
     """by the sizes above, with and without ranges"""
-    sizes = [(n, r, 2, 2, 64) for r, n in ((5, 66), (33, 33), (65, 200), (200, 200))] + [(4000, 11, 3, 1, 64), (2063, 100, 4, 4, 128), (700, 90, 6, 2, 64)]
+    sizes = [(66, 5, 2, 2, 64), (200, 65, 2, 2, 64), (4000, 11, 3, 1, 64), (2063, 100, 4, 4, 128), (300, 140, 16, 16, 64)]
     seen = {api.tl_k_attention_cache8_plan(*s, elems)[0] for s in sizes for elems in (0, 1 << 20)}
-    assert seen == {"columns", "rows64", "rows128", "rows256"}
+    assert seen == {"columns16", "rows128", "rows256"}
 
 
 def test_ranges_with_nothing_to_see(api):
