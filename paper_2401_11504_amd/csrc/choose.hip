@@ -4,21 +4,33 @@
 // ---------------------------------------------------------------- counts
 // counts[r][t] = the number of j with tokens[r][j] = t.  A workgroup counts a range of the vocabulary of one row in LDS, so that the row
 // is written once and nothing has to be cleared before; ids outside the range (padding too) are passed over.
-constexpr int COUNT_RANGE = 8192;
+template <int RANGE>
 __global__ __launch_bounds__(256) void token_counts_kernel(const int* __restrict__ tokens, long ldt, int n, int vocab, int* __restrict__ counts,
                                                            long ldc) {
-    __shared__ int h[COUNT_RANGE];
-    const int first = blockIdx.x * COUNT_RANGE, size = min(COUNT_RANGE, vocab - first);
+    __shared__ __align__(16) int h[RANGE];
+    const int first = blockIdx.x * RANGE, size = min(RANGE, vocab - first), tid = threadIdx.x;
     const int* tok = tokens + (long)blockIdx.y * ldt;
-    for (int i = threadIdx.x; i < size; i += 256) h[i] = 0;
+    int t[8];                                              // eight tokens a thread on their way at a time
+    auto fetch = [&](int i0) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) t[j] = i0 + j * 256 + tid < n ? tok[i0 + j * 256 + tid] : -1;
+    };
+    fetch(0);
+#pragma unroll
+    for (int i = 0; i < RANGE / 1024; ++i) *(int4*)(h + (i * 256 + tid) * 4) = make_int4(0, 0, 0, 0);
     __syncthreads();
-    for (int i = threadIdx.x; i < n; i += 256) {
-        const unsigned t = (unsigned)(tok[i] - first);
-        if (tok[i] >= 0 && t < (unsigned)size) atomicAdd(&h[t], 1);
+    for (int i0 = 0; i0 < n; i0 += 2048) {
+        if (i0) fetch(i0);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (t[j] >= first && t[j] - first < size) atomicAdd(&h[t[j] - first], 1);
     }
     __syncthreads();
     int* out = counts + (long)blockIdx.y * ldc + first;
-    for (int i = threadIdx.x; i < size; i += 256) out[i] = h[i];
+    for (int i = tid * 4; i < size; i += 1024) {           // (rows begin at any multiple of 4 bytes, which wide stores take)
+        if (i + 4 <= size) *(int4*)(out + i) = *(const int4*)(h + i);
+        else for (int j = i; j < size; ++j) out[j] = h[j];
+    }
 }
 // counts[r][tokens[r][j]] += add: whole numbers, so the order of the additions changes nothing
 __global__ __launch_bounds__(256) void token_counts_add_kernel(const int* __restrict__ tokens, long ldt, int n, int vocab, int add,
@@ -33,7 +45,9 @@ hipError_t launch_token_counts(const int* tokens, long ldt, int rows, int n, int
         const int m = rows - r < 32768 ? rows - r : 32768;
         const int* t = tokens + (long)r * ldt;
         int* c = counts + (long)r * ldc;
-        if (!add) token_counts_kernel<<<dim3(cdiv(vocab, COUNT_RANGE), m), 256, 0, s>>>(t, ldt, n, vocab, c, ldc);
+        // wide ranges read the tokens fewer times, narrow ones fill the GPU with few rows
+        if (!add && (long)m * cdiv(vocab, 8192) < 256) token_counts_kernel<1024><<<dim3(cdiv(vocab, 1024), m), 256, 0, s>>>(t, ldt, n, vocab, c, ldc);
+        else if (!add) token_counts_kernel<8192><<<dim3(cdiv(vocab, 8192), m), 256, 0, s>>>(t, ldt, n, vocab, c, ldc);
         else if (n > 0) token_counts_add_kernel<<<dim3(cdiv(n, 256), m), 256, 0, s>>>(t, ldt, n, vocab, add, c, ldc);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
@@ -74,7 +88,9 @@ __device__ __forceinline__ Best block_best(Best b) {
     return b;
 }
 // Grid x: pieces of a row, y: rows.  One piece a row: the choice; more: its best to ws[(row * pieces + piece) * 2], joined by choose_join_kernel.
-template <int NT>
+// A thread has four tokens at a time, U times, all asked for before the first is used (rows begin at any multiple of 4 bytes, which 16-byte
+// accesses take).  piece: a multiple of 4 NT U.
+template <int NT, int U>
 __global__ __launch_bounds__(NT) void choose_kernel(Choose c, int vocab, int piece, float* __restrict__ ws) {
     const long r = blockIdx.y;
     const int first = blockIdx.x * piece, end = min(vocab, first + piece);
@@ -84,11 +100,48 @@ __global__ __launch_bounds__(NT) void choose_kernel(Choose c, int vocab, int pie
     const unsigned* allowed = c.allowed ? c.allowed + r * c.lda : nullptr;
     float* out = c.out ? c.out + r * c.ldo : nullptr;
     Best b;
-    for (int i = first + threadIdx.x; i < end; i += NT) {
-        const bool may = !allowed || allowed[i >> 5] >> (i & 31) & 1;
-        const float y = may ? penalised(x[i], counts ? counts[i] : 0, bias ? bias[i] : 0.f, c) : -INFINITY;
-        if (out) out[i] = y;
-        if (may) b.take(y, i);
+    for (int i0 = first; i0 < end; i0 += 4 * NT * U) {
+        float4 xv[U], bv[U];
+        int4 cv[U];
+        unsigned may[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = i0 + (u * NT + (int)threadIdx.x) * 4;
+            bv[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+            cv[u] = make_int4(0, 0, 0, 0);
+            may[u] = i < end ? 15u : 0u;
+            if (i + 4 <= end) {
+                xv[u] = *(const float4*)(x + i);
+                if (counts) cv[u] = *(const int4*)(counts + i);
+                if (bias) bv[u] = *(const float4*)(bias + i);
+            } else {                                       // the last tokens of a row
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const bool in = i + e < end;
+                    (&xv[u].x)[e] = in ? x[i + e] : 0.f;
+                    if (counts && in) (&cv[u].x)[e] = counts[i + e];
+                    if (bias && in) (&bv[u].x)[e] = bias[i + e];
+                }
+            }
+            if (allowed && i < end) may[u] = allowed[i >> 5] >> (i & 31) & 15u;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = i0 + (u * NT + (int)threadIdx.x) * 4;
+            float y[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const bool ok = may[u] >> e & 1;
+                y[e] = ok ? penalised((&xv[u].x)[e], (&cv[u].x)[e], (&bv[u].x)[e], c) : -INFINITY;
+                if (ok && i + e < end) b.take(y[e], i + e);
+            }
+            if (out && i + 4 <= end) *(float4*)(out + i) = make_float4(y[0], y[1], y[2], y[3]);
+            else if (out) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (i + e < end) out[i + e] = y[e];
+            }
+        }
     }
     if (!c.choice) return;
     b = block_best<NT>(b);
@@ -115,12 +168,13 @@ hipError_t launch_choose(const Choose& c, int rows, int vocab, float* ws, size_t
         if (p.allowed) p.allowed += (long)r * c.lda;
         if (p.out) p.out += (long)r * c.ldo;
         if (p.choice) p.choice += r;
-        const int pieces = cdiv(vocab, 2048);
-        if (ws && pieces > 1 && (size_t)m * pieces * 2 <= ws_elems) {
-            choose_kernel<256><<<dim3(pieces, m), 256, 0, s>>>(p, vocab, 2048, ws);
+        const int piece = (long)m * vocab < 1 << 19 ? 1024 : 4096, pieces = cdiv(vocab, piece);
+        if (m < 256 && ws && pieces > 1 && (size_t)m * pieces * 2 <= ws_elems) {
+            if (piece == 1024) choose_kernel<256, 1><<<dim3(pieces, m), 256, 0, s>>>(p, vocab, piece, ws);
+            else choose_kernel<256, 4><<<dim3(pieces, m), 256, 0, s>>>(p, vocab, piece, ws);
             if (p.choice) choose_join_kernel<<<m, 64, 0, s>>>(ws, pieces, p.choice);
         } else {
-            choose_kernel<1024><<<dim3(1, m), 1024, 0, s>>>(p, vocab, vocab, nullptr);
+            choose_kernel<1024, 2><<<dim3(1, m), 1024, 0, s>>>(p, vocab, cdiv(vocab, 8192) * 8192, nullptr);
         }
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
