@@ -4,8 +4,8 @@
 // ---------------------------------------------------------------- counts
 // counts[r][t] = the number of j with tokens[r][j] = t.  A workgroup counts a range of the vocabulary of one row in LDS, so that the row
 // is written once and nothing has to be cleared before; ids outside the range (padding too) are passed over.
-template <int RANGE>
-__global__ __launch_bounds__(256) void token_counts_kernel(const int* __restrict__ tokens, long ldt, int n, int vocab, int* __restrict__ counts,
+template <int RANGE, int NT>
+__global__ __launch_bounds__(NT) void token_counts_kernel(const int* __restrict__ tokens, long ldt, int n, int vocab, int* __restrict__ counts,
                                                            long ldc) {
     __shared__ __align__(16) int h[RANGE];
     const int first = blockIdx.x * RANGE, size = min(RANGE, vocab - first), tid = threadIdx.x;
@@ -13,13 +13,12 @@ __global__ __launch_bounds__(256) void token_counts_kernel(const int* __restrict
     int t[8];                                              // eight tokens a thread on their way at a time
     auto fetch = [&](int i0) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) t[j] = i0 + j * 256 + tid < n ? tok[i0 + j * 256 + tid] : -1;
+        for (int j = 0; j < 8; ++j) t[j] = i0 + j * NT + tid < n ? tok[i0 + j * NT + tid] : -1;
     };
     fetch(0);
-#pragma unroll
-    for (int i = 0; i < RANGE / 1024; ++i) *(int4*)(h + (i * 256 + tid) * 4) = make_int4(0, 0, 0, 0);
+    for (int i = tid * 4; i < RANGE; i += NT * 4) *(int4*)(h + i) = make_int4(0, 0, 0, 0);
     __syncthreads();
-    for (int i0 = 0; i0 < n; i0 += 2048) {
+    for (int i0 = 0; i0 < n; i0 += 8 * NT) {
         if (i0) fetch(i0);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
@@ -27,7 +26,7 @@ __global__ __launch_bounds__(256) void token_counts_kernel(const int* __restrict
     }
     __syncthreads();
     int* out = counts + (long)blockIdx.y * ldc + first;
-    for (int i = tid * 4; i < size; i += 1024) {           // (rows begin at any multiple of 4 bytes, which wide stores take)
+    for (int i = tid * 4; i < size; i += NT * 4) {           // (rows begin at any multiple of 4 bytes, which wide stores take)
         if (i + 4 <= size) *(int4*)(out + i) = *(const int4*)(h + i);
         else for (int j = i; j < size; ++j) out[j] = h[j];
     }
@@ -45,9 +44,11 @@ hipError_t launch_token_counts(const int* tokens, long ldt, int rows, int n, int
         const int m = rows - r < 32768 ? rows - r : 32768;
         const int* t = tokens + (long)r * ldt;
         int* c = counts + (long)r * ldc;
-        // wide ranges read the tokens fewer times, narrow ones fill the GPU with few rows
-        if (!add && (long)m * cdiv(vocab, 8192) < 256) token_counts_kernel<1024><<<dim3(cdiv(vocab, 1024), m), 256, 0, s>>>(t, ldt, n, vocab, c, ldc);
-        else if (!add) token_counts_kernel<8192><<<dim3(cdiv(vocab, 8192), m), 256, 0, s>>>(t, ldt, n, vocab, c, ldc);
+        // wide ranges read the tokens fewer times, narrow ones fill the GPU with few rows; more threads where there are many tokens to a row
+        auto set = [&](auto kernel, int range, int threads) { kernel<<<dim3(cdiv(vocab, range), m), threads, 0, s>>>(t, ldt, n, vocab, c, ldc); };
+        const bool few = (long)m * cdiv(vocab, 8192) < 256, many = n > 4096;
+        if (!add && few) many ? set(token_counts_kernel<1024, 1024>, 1024, 1024) : set(token_counts_kernel<1024, 256>, 1024, 256);
+        else if (!add) many ? set(token_counts_kernel<8192, 1024>, 8192, 1024) : set(token_counts_kernel<8192, 256>, 8192, 256);
         else if (n > 0) token_counts_add_kernel<<<dim3(cdiv(n, 256), m), 256, 0, s>>>(t, ldt, n, vocab, add, c, ldc);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
@@ -169,7 +170,7 @@ hipError_t launch_choose(const Choose& c, int rows, int vocab, float* ws, size_t
         if (p.out) p.out += (long)r * c.ldo;
         if (p.choice) p.choice += r;
         const int piece = (long)m * vocab < 1 << 19 ? 1024 : 4096, pieces = cdiv(vocab, piece);
-        if (m < 256 && ws && pieces > 1 && (size_t)m * pieces * 2 <= ws_elems) {
+        if (ws && pieces > 1 && (size_t)m * pieces * 2 <= ws_elems) {
             if (piece == 1024) choose_kernel<256, 1><<<dim3(pieces, m), 256, 0, s>>>(p, vocab, piece, ws);
             else choose_kernel<256, 4><<<dim3(pieces, m), 256, 0, s>>>(p, vocab, piece, ws);
             if (p.choice) choose_join_kernel<<<m, 64, 0, s>>>(ws, pieces, p.choice);
