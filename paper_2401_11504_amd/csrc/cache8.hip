@@ -575,40 +575,40 @@ __global__ __launch_bounds__(NC * 64, 2) void attn8_rows_kernel(Cache8 c, int n_
             s0 = mfma32(*(const bf16x8_t*)(st + k_piece_at<D>(l32, 2 * ks + g)), qf[ks], s0);
             s1 = mfma32(*(const bf16x8_t*)(st + k_piece_at<D>(32 + l32, 2 * ks + g)), qf[ks], s1);
         }
-        const float ks = ((const float*)(st + 2 * TB))[0], vs = ((const float*)(st + 2 * TB))[1];
-        float x[32], top = -INFINITY;
-#pragma unroll
-        for (int v = 0; v < 16; ++v) {
-            x[v] = s0[v] * ks;
-            x[16 + v] = s1[v] * ks;
-        }
+        // The scales are positive, or NaN: a column that sees nothing of the block takes 1 and 0 instead, so that it learns of no NaN.
+        const bool sees = u0 < seen;
+        const float ks = sees ? ((const float*)(st + 2 * TB))[0] : 1.f, vs = sees ? ((const float*)(st + 2 * TB))[1] : 0.f;
         if (u0 + 64 > w_least) {                             // some column does not see all of it
 #pragma unroll
-            for (int v = 0; v < 32; ++v)
-                if (u0 + 32 * (v >> 4) + 8 * (v >> 2 & 3) + 4 * g + (v & 3) >= seen) x[v] = -INFINITY;
+            for (int v = 0; v < 16; ++v) {
+                const int u = u0 + 8 * (v >> 2) + 4 * g + (v & 3);
+                s0[v] = u >= seen ? -INFINITY : s0[v];
+                s1[v] = u + 32 >= seen ? -INFINITY : s1[v];
+            }
         }
+        float x[32], top = s0[0], sum = 0.f;
 #pragma unroll
-        for (int v = 0; v < 32; ++v) top = fmaxf(top, x[v]);
-        top = fmaxf(top, __shfl_xor(top, 32, 64));
-        const float mn = fmaxf(m, top), base = mn == -INFINITY ? 0.f : mn, alpha = __builtin_amdgcn_exp2f(m - base);
-        m = mn;
-        float sum = 0.f;
-        const bool sees = u0 < seen;
-#pragma unroll
-        for (int v = 0; v < 32; ++v) {
-            x[v] = __builtin_amdgcn_exp2f(x[v] - base);
-            sum += x[v];
-        }
-        l = l * alpha + sum;
-        const float f = sees ? vs : 0.f;                     // (a block that a column does not see may have the scale NaN)
-#pragma unroll
-        for (int v = 0; v < 32; ++v) x[v] *= f;
-        if (__builtin_amdgcn_ballot_w64(alpha != 1.f)) {
+        for (int v = 0; v < 32; ++v) top = fmaxf(top, v < 16 ? s0[v & 15] : s1[v & 15]);
+        top = fmaxf(top, __shfl_xor(top, 32, 64)) * ks;
+        // m, what the exponents are taken from, follows the maximum only when that is 8 (a factor of 256) ahead: sums and accumulators have the room,
+        // and are hardly ever rescaled after the first tiles
+        const float mn = top > m + 8.f ? top : m, base = mn == -INFINITY ? 0.f : mn;
+        if (__builtin_amdgcn_ballot_w64(mn != m)) {
+            const float alpha = __builtin_amdgcn_exp2f(m - base);
+            l *= alpha;
 #pragma unroll
             for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
                 for (int v = 0; v < 16; ++v) oacc[dt][v] *= alpha;
+            m = mn;
         }
+#pragma unroll
+        for (int v = 0; v < 32; ++v) {
+            x[v] = __builtin_amdgcn_exp2f(fmaf(v < 16 ? s0[v & 15] : s1[v & 15], ks, -base));
+            sum += x[v];
+            x[v] *= vs;
+        }
+        l += sum;
         if (!probs) {
 #pragma unroll
             for (int G = 0; G < 4; ++G) {
