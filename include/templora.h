@@ -242,6 +242,41 @@ tl_status tl_generate(tl_lora* lora, const int32_t* prompt, int32_t n_prompt, in
  * default, the cache is dropped.  Errors: TL_ERR_ARG, TL_ERR_DISCARDED, TL_ERR_OOM, TL_ERR_DEVICE. */
 tl_status tl_cache_reuse(tl_lora* lora, int32_t on);
 
+/* The cache in 8 bits, for long windows.  on != 0: keys and values move to buffers of their own (allocated on the first call: n_layers *
+ * max_tokens * 2 d_model bytes and what belongs to them), held as tl_cache8_mem describes with n_heads heads; a cache that exists moves along.
+ * tl_prefill fills it (the prompt's own attention works on its bf16 keys and values), tl_decode_step and tl_extend add to it and attend
+ * to what it stands for once the new tokens are in.  Whether it survives training-side calls is tl_cache_reuse's to say, as for the bf16 cache.  on == 0
+ * (the initial state): back to the bf16 cache; the cache is dropped.  Errors: TL_ERR_ARG, TL_ERR_DISCARDED, TL_ERR_OOM, TL_ERR_DEVICE. */
+tl_status tl_cache_8bit(tl_lora* lora, int32_t on);
+
+/* n_tokens given tokens at once behind the kv_length cached ones (a text that goes on as it stands, a draft to be checked): what as many
+ * tl_decode_step calls would leave in the cache, to within rounding, in one forward pass.  Returns the next token behind the last, as tl_decode_step.
+ * Needs tl_cache_8bit and a cache (TL_ERR_ARG); kv_length + n_tokens <= max_tokens (TL_ERR_WINDOW).  After an error past these checks the cache
+ * is dropped.  Other errors as tl_prefill. */
+tl_status tl_extend(tl_lora* lora, const int32_t* tokens, int32_t n_tokens, int32_t* next_token, float* logits_out);
+
+/* What the cache holds of tokens first .. first + n - 1 of a layer: host fp32 [n, d_model] each, keys rotated; whichever kind of cache is on. */
+tl_status tl_get_kv(tl_lora* lora, int32_t layer, int32_t first, int32_t n, float* k_out, float* v_out);
+
+/*
+ * What the choice of the next token takes into account (tl_prefill, tl_decode_step, tl_extend, tl_generate), in this order; without any of it
+ * the choice is the largest logit, as above.  logits_out stays what the model gives.
+ *   tl_set_penalties: for a token that is count > 0 times among the last last_n tokens of the cached text (0: all of it, the newest included)
+ *     x = x > 0 ? x / repetition : x * repetition;   x = x - (frequency * count + presence).      NULL: none.
+ *   tl_set_bias     : host fp32 [vocab], copied, is added.      NULL: none.
+ *   tl_set_allowed  : host uint32 [ceil(vocab / 32)], copied; a token whose bit (bit t % 32 of word t / 32) is 0 is not chosen.  NULL: every token
+ *                     may be.  For a grammar: set before each step.  A step that finds no token to choose returns TL_ERR_ARG; a decode step can
+ *                     then be made again with another mask.
+ * They stay until they are set again.  Errors: TL_ERR_ARG, TL_ERR_SHAPE (vocab = 0), TL_ERR_DISCARDED, TL_ERR_OOM, TL_ERR_DEVICE.
+ */
+typedef struct {
+    float repetition, presence, frequency; /* 1, 0, 0: none; repetition > 0 */
+    int32_t last_n;
+} tl_penalties;
+tl_status tl_set_penalties(tl_lora* lora, const tl_penalties* penalties);
+tl_status tl_set_bias(tl_lora* lora, const float* bias);
+tl_status tl_set_allowed(tl_lora* lora, const uint32_t* allowed);
+
 /* Release the (discarded or not) handle itself. NULL is accepted. */
 tl_status tl_lora_free(tl_lora* lora);
 

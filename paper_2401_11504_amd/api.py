@@ -57,6 +57,10 @@ class tl_generate_cfg(C.Structure):
     _fields_ = [("window", C.c_int32), ("chunk", C.c_int32), ("train", tl_train_cfg)]
 
 
+class tl_penalties(C.Structure):
+    _fields_ = [("repetition", C.c_float), ("presence", C.c_float), ("frequency", C.c_float), ("last_n", C.c_int32)]
+
+
 class tl_cache8_mem(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("k_tail", C.c_void_p),
                 ("v_tail", C.c_void_p), ("n_kv_heads", C.c_int32), ("d_head", C.c_int32), ("capacity", C.c_int32)]
@@ -75,6 +79,12 @@ _SIGS = {
     "tl_kv_length": [_vp, C.POINTER(_i32)],
     "tl_generate": [_vp, _vp, _i32, _i32, C.POINTER(tl_generate_cfg), _vp, _vp, C.POINTER(_i32)],
     "tl_cache_reuse": [_vp, _i32],
+    "tl_cache_8bit": [_vp, _i32],
+    "tl_extend": [_vp, _vp, _i32, C.POINTER(_i32), _vp],
+    "tl_get_kv": [_vp, _i32, _i32, _i32, _vp, _vp],
+    "tl_set_penalties": [_vp, C.POINTER(tl_penalties)],
+    "tl_set_bias": [_vp, _vp],
+    "tl_set_allowed": [_vp, _vp],
     "tl_discard": [_vp],
     "tl_lora_free": [_vp],
     "tl_get_factor": [_vp, _i32, _i32, _i32, _vp, _sz],
@@ -251,6 +261,51 @@ def tl_generate(lora, prompt, n_new, window, chunk, n_ctx_max=1024, batch=0, epo
 
 def tl_cache_reuse(lora, on=True):
     _chk(_lib.tl_cache_reuse(lora, int(on)))
+
+
+def tl_cache_8bit(lora, on=True):
+    _chk(_lib.tl_cache_8bit(lora, int(on)))
+
+
+def tl_extend(lora, tokens, vocab=0):
+    """-> (next greedy token, logits of the last position or None)"""
+    a, p = _tok(tokens)
+    nxt = _i32()
+    logits = np.empty(vocab, dtype=np.float32) if vocab else None
+    _chk(_lib.tl_extend(lora, p, a.size, C.byref(nxt), logits.ctypes.data_as(_vp) if vocab else None))
+    return nxt.value, logits
+
+
+def tl_get_kv(lora, layer, first, n, d_model):
+    """-> keys, values of tokens first .. first + n - 1: fp32 [n, d_model] each"""
+    k, v = (np.empty((n, d_model), dtype=np.float32) for _ in range(2))
+    _chk(_lib.tl_get_kv(lora, layer, first, n, k.ctypes.data_as(_vp), v.ctypes.data_as(_vp)))
+    return k, v
+
+
+def tl_set_penalties(lora, repetition=1.0, presence=0.0, frequency=0.0, last_n=0):
+    """tl_set_penalties(lora) takes them off"""
+    p = tl_penalties(repetition, presence, frequency, last_n)
+    off = (repetition, presence, frequency) == (1.0, 0.0, 0.0)
+    _chk(_lib.tl_set_penalties(lora, None if off else C.byref(p)))
+
+
+def tl_set_bias(lora, bias, vocab):
+    """bias: vocab numbers, or None"""
+    a = None if bias is None else np.ascontiguousarray(bias, dtype=np.float32)
+    assert a is None or a.size == vocab
+    _chk(_lib.tl_set_bias(lora, None if a is None else a.ctypes.data_as(_vp)))
+
+
+def tl_set_allowed(lora, allowed, vocab):
+    """allowed: vocab truth values, or None"""
+    if allowed is None:
+        return _chk(_lib.tl_set_allowed(lora, None))
+    bits = np.packbits(np.asarray(allowed, dtype=bool), bitorder="little")
+    assert len(allowed) == vocab
+    words = np.zeros(4 * ((vocab + 31) // 32), dtype=np.uint8)
+    words[:bits.size] = bits
+    _chk(_lib.tl_set_allowed(lora, words.ctypes.data_as(_vp)))
 
 
 def tl_kv_length(lora):

@@ -9,7 +9,7 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "kernels.h"
+#include "decode_token.h"
 #include "tiles.h"
 
 static constexpr float kLeastMagnitude = 7.888609052210118e-31f;   // 2^-100: keeps the scale and its reciprocal normal numbers
@@ -279,27 +279,69 @@ __device__ __forceinline__ uint4 tail_values(const bf16_t* row, int u0, int end,
     return w;
 }
 
-template <int D>
+// FRESH: the token being decoded, one row of as many query as key heads.  Its q, k and v do not exist as rows yet: every workgroup forms its head's q
+// (while its first codes are on their way), and the one whose range ends with the tail forms k and v and puts them there.  The token must not
+// complete a block.
+template <int D, bool FRESH>
 __global__ __launch_bounds__(256, 2) void attn8_cols_kernel(Cache8 c, int n_keys, const bf16_t* __restrict__ q, long ldq, int n_rows, int group,
-                                                         float scale_log2e, bf16_t* __restrict__ o, long ldo, float* __restrict__ ws,
-                                                         int blocks_per_split) {
+                                                            float scale_log2e, bf16_t* __restrict__ o, long ldo, float* __restrict__ ws,
+                                                            int blocks_per_split, DecodeFresh fresh, DecodeOut more) {
     constexpr int PC = D / 64, NT = D / 16, LDP = D + 4;
     __shared__ float part[4][16][LDP];                     // a column's output, maximum and sum, wave by wave
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m16 = lane & 15, g = lane >> 4;
     const int head = blockIdx.x, n_cols = n_rows * group, heads = c.heads * group;
     const int col = min(m16, n_cols - 1), row = col / group, seen = n_keys - n_rows + row + 1;      // keys 0 .. seen - 1
     const int least = n_keys - n_rows + 1;                                                              // the first column's
-    const int b_end = min((int)(blockIdx.y + 1) * blocks_per_split, (n_keys + 63) >> 6);
-    const bf16_t* qr = q + (long)row * ldq + (long)(head * group + col % group) * D + g * 16;
-    bf16x8_t qf[2 * PC];
+    const int b_begin = (int)blockIdx.y * blocks_per_split, b_end = min(b_begin + blocks_per_split, (n_keys + 63) >> 6);
+    const int key0 = (m16 >> 2) * 16 + (m16 & 3), b_tail = n_keys >> 6, b_full = min(b_end, b_tail);
+    // a block's keys are asked for when the block before has used its own, its values when those have been used
+    uint4 kr[4][PC], vr[NT];
+    float ks_next = 0.f;
+    auto keys = [&](int b) {
+        const long at = (long)b * c.heads + head;
 #pragma unroll
-    for (int st = 0; st < 2 * PC; ++st) qf[st] = __builtin_bit_cast(bf16x8_t, *(const uint4*)(qr + (st >> 1) * 64 + (st & 1) * 8));
+        for (int kg = 0; kg < 4; ++kg)
+#pragma unroll
+            for (int pc = 0; pc < PC; ++pc) kr[kg][pc] = load_once(c.k + at * 64 * D + pc * 4096 + (key0 + kg * 4) * 64 + g * 16);
+        ks_next = c.ks[at];
+    };
+    int b = b_begin + wave;
+    if (b < b_full) keys(b);
+    bf16x8_t qf[2 * PC];
+    if constexpr (FRESH) {
+        constexpr int LPK = D / 8;
+        __shared__ float fr[3][D];
+        __shared__ __align__(16) bf16_t sq[D];
+        __builtin_amdgcn_sched_barrier(0);
+        const bool last = b_tail >= b_begin && b_tail < b_end;
+        fresh_rows<D, 256>(fresh, head, last, fr);
+        const int which = threadIdx.x / LPK, sub = threadIdx.x % LPK, slot = n_keys - 1 & 63;
+        __syncthreads();
+        if (which == 0 || (which == 1 && last)) {          // q and k, rotated
+            float2 cs[8];
+            float t[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) cs[e] = fresh.rope[sub % (LPK >> 1) * 8 + e];
+            rope8(fr[which] + sub * 8, fr[which] + (sub ^ (LPK >> 1)) * 8, cs, sub, LPK, t);
+            bf16_t* to = which ? c.kt + (long)head * 64 * D + (sub >> 3) * 4096 + slot * 64 + (sub & 7) * 8 : sq + sub * 8;
+            *(uint4*)to = pack8(t);
+        } else if (which == 2 && last) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) c.vt[(long)head * 64 * D + (sub * 8 + e) * 64 + slot] = f32_to_bf16(fr[2][sub * 8 + e]);
+        }
+        __syncthreads();                                   // (the tail's wave reads what the others have stored)
+#pragma unroll
+        for (int st = 0; st < 2 * PC; ++st) qf[st] = __builtin_bit_cast(bf16x8_t, *(const uint4*)(sq + g * 16 + (st >> 1) * 64 + (st & 1) * 8));
+    } else {
+        const bf16_t* qr = q + (long)row * ldq + (long)(head * group + col % group) * D + g * 16;
+#pragma unroll
+        for (int st = 0; st < 2 * PC; ++st) qf[st] = __builtin_bit_cast(bf16x8_t, *(const uint4*)(qr + (st >> 1) * 64 + (st & 1) * 8));
+    }
 
     f32x4_t oacc[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) oacc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
-    const int key0 = (m16 >> 2) * 16 + (m16 & 3), b_tail = n_keys >> 6, b_full = min(b_end, b_tail);
     f32x4_t s[4];
     float x[16];
     bf16x8_t hi[2], lo[2];
@@ -332,19 +374,6 @@ __global__ __launch_bounds__(256, 2) void attn8_cols_kernel(Cache8 c, int n_keys
 #pragma unroll
         for (int t = 0; t < NT; ++t) oacc[t] *= alpha;
     };
-    // a block's keys are asked for when the block before has used its own, its values when those have been used
-    uint4 kr[4][PC], vr[NT];
-    float ks_next = 0.f;
-    auto keys = [&](int b) {
-        const long at = (long)b * c.heads + head;
-#pragma unroll
-        for (int kg = 0; kg < 4; ++kg)
-#pragma unroll
-            for (int pc = 0; pc < PC; ++pc) kr[kg][pc] = load_once(c.k + at * 64 * D + pc * 4096 + (key0 + kg * 4) * 64 + g * 16);
-        ks_next = c.ks[at];
-    };
-    int b = blockIdx.y * blocks_per_split + wave;
-    if (b < b_full) keys(b);
     for (; b < b_full; b += 4) {
         const long at = (long)b * c.heads + head;
 #pragma unroll
@@ -421,7 +450,11 @@ __global__ __launch_bounds__(256, 2) void attn8_cols_kernel(Cache8 c, int n_keys
 #pragma unroll
     for (int t = 0; t < NT; ++t) *(f32x4_t*)&part[wave][m16][t * 16 + g * 4] = oacc[t];
     if (g == 0) { part[wave][m16][D] = m; part[wave][m16][D + 1] = l; }
+    uint4 av[4];
+    if constexpr (FRESH)
+        if (!ws) head_output_fetch<D, 256>(head, heads, more, av);
     __syncthreads();
+    float one = 0.f;                                       // FRESH without ranges: this thread's column of the output
     for (int i = threadIdx.x; i < 16 * D; i += 256) {
         const int cc = i / D, e = i % D;
         if (cc >= n_cols) break;
@@ -437,26 +470,32 @@ __global__ __launch_bounds__(256, 2) void attn8_cols_kernel(Cache8 c, int n_keys
             ot += a * part[w][cc][e];
         }
         const int r = cc / group, qh = head * group + cc % group;
-        if (!ws) o[(long)r * ldo + (long)qh * D + e] = f32_to_bf16(ot / lt);
-        else {
+        if (!ws) {
+            if constexpr (FRESH) one = ot / lt;
+            else o[(long)r * ldo + (long)qh * D + e] = f32_to_bf16(ot / lt);
+        } else {
             float* out = ws + (((long)r * heads + qh) * gridDim.y + blockIdx.y) * (D + 2);
             out[e] = ot;
             if (e == 0) { out[D] = mt; out[D + 1] = lt; }
         }
     }
+    if constexpr (FRESH)
+        if (!ws) head_output<D, 256>(one, threadIdx.x % D, head, heads, more, av);
 }
 
 // The ranges of a row and head, one thread a column: lane i holds range i's maximum and sum, and sixteen ranges' columns are asked for before
 // the first is used.
 template <int D>
-__global__ __launch_bounds__(D) void attn8_join_kernel(const float* __restrict__ ws, int n_split, int heads, bf16_t* __restrict__ o, long ldo) {
-    const int e = threadIdx.x, lane = threadIdx.x & 63;
+__global__ __launch_bounds__(D) void attn8_join_kernel(const float* __restrict__ ws, int n_split, int heads, long ldo, DecodeOut out) {
+    const int e = threadIdx.x, lane = threadIdx.x & 63, head = blockIdx.x % heads;
     const float* w = ws + (long)blockIdx.x * n_split * (D + 2);
     const int r = min(lane, n_split - 1);
     const float m = w[r * (D + 2) + D], l = w[r * (D + 2) + D + 1];
     float t[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) t[i] = w[min(i, n_split - 1) * (D + 2) + e];
+    uint4 av[8];
+    head_output_fetch<D, D>(head, heads, out, av);
     __builtin_amdgcn_sched_barrier(0);
     const float top = wave_max(lane < n_split ? m : -INFINITY);
     const float a = lane < n_split ? __builtin_amdgcn_exp2f(m - top) : 0.f;      // (one range has keys: top is a number, or all is NaN)
@@ -473,7 +512,8 @@ __global__ __launch_bounds__(D) void attn8_join_kernel(const float* __restrict__
             acc += i0 + i < n_split ? ai * t[i] : 0.f;
         }
     }
-    o[(long)(blockIdx.x / heads) * ldo + (long)(blockIdx.x % heads) * D + e] = f32_to_bf16(acc / sum);
+    out.o += (long)(blockIdx.x / heads) * ldo;
+    head_output<D, D>(acc / sum, e, head, heads, out, av);
 }
 
 // ---------------------------------------------------------------- attention of many rows
@@ -733,10 +773,10 @@ const char* attention_cache8_plan(int n_keys, int n_rows, int heads, int kv_head
 }
 template <int D>
 static hipError_t run_attention_cache8(const Attn8Plan& p, const Cache8& c, int n_keys, const bf16_t* q, long ldq, int n_rows, int group, bf16_t* o,
-                                       long ldo, float* ws, hipStream_t s) {
+                                       long ldo, float* ws, hipStream_t s, const DecodeFresh* fresh, const DecodeOut& out) {
     const float scale = 1.4426950408889634f / sqrtf((float)D);
     const long n_cols = (long)n_rows * group;
-    float* w = p.n_split > 1 ? ws : nullptr;
+    float* w = p.n_split > 1 || (out.a && !fresh) ? ws : nullptr;       // (the join leaves the shares of A o)
     auto rows = [&](auto nc) {
         constexpr int NC = decltype(nc)::value;
         constexpr size_t lds = attn8_rows_lds<D, NC>();
@@ -748,17 +788,60 @@ static hipError_t run_attention_cache8(const Attn8Plan& p, const Cache8& c, int 
     };
     hipError_t e;
     if (p.cols == 16) {                                    // (one workgroup holds all the columns of a key head)
-        attn8_cols_kernel<D><<<dim3(c.heads, p.n_split), 256, 0, s>>>(c, n_keys, q, ldq, n_rows, group, scale, o, ldo, w, p.per);
+        auto kernel = fresh ? attn8_cols_kernel<D, true> : attn8_cols_kernel<D, false>;
+        kernel<<<dim3(c.heads, p.n_split), 256, 0, s>>>(c, n_keys, q, ldq, n_rows, group, scale, o, ldo, w, p.per, fresh ? *fresh : DecodeFresh{}, out);
         e = hipGetLastError();
     } else e = p.cols == 128 ? rows(std::integral_constant<int, 4>{}) : rows(std::integral_constant<int, 8>{});
     if (e != hipSuccess || !w) return e;
-    attn8_join_kernel<D><<<n_rows * c.heads * group, D, 0, s>>>(w, p.n_split, c.heads * group, o, ldo);
+    attn8_join_kernel<D><<<n_rows * c.heads * group, D, 0, s>>>(w, p.n_split, c.heads * group, ldo, out);
     return hipGetLastError();
 }
 hipError_t launch_attention_cache8(const Cache8& c, int n_keys, const bf16_t* q, long ldq, int n_rows, int heads, bf16_t* o, long ldo,
                                    float* ws, size_t ws_elems, hipStream_t s) {
     if (n_rows <= 0) return n_rows == 0 ? hipSuccess : hipErrorInvalidValue;
     const Attn8Plan p = attn8_plan(n_keys, n_rows, heads, c.heads, c.d, ws ? ws_elems : 0);
-    return c.d == 128 ? run_attention_cache8<128>(p, c, n_keys, q, ldq, n_rows, heads / c.heads, o, ldo, ws, s)
-                      : run_attention_cache8<64>(p, c, n_keys, q, ldq, n_rows, heads / c.heads, o, ldo, ws, s);
+    DecodeOut out;
+    out.o = o;
+    return c.d == 128 ? run_attention_cache8<128>(p, c, n_keys, q, ldq, n_rows, heads / c.heads, o, ldo, ws, s, nullptr, out)
+                      : run_attention_cache8<64>(p, c, n_keys, q, ldq, n_rows, heads / c.heads, o, ldo, ws, s, nullptr, out);
+}
+
+// ---------------------------------------------------------------- the token being decoded
+// The rows q | k | v of a token, [3 d] bf16, q and k rotated: one workgroup a head.
+template <int D>
+__global__ __launch_bounds__(256) void decode_token_kernel(DecodeFresh fresh, bf16_t* __restrict__ qkv) {
+    constexpr int LPK = D / 8;
+    __shared__ float fr[3][D];
+    const int head = blockIdx.x, which = threadIdx.x / LPK, sub = threadIdx.x % LPK;
+    fresh_rows<D, 256>(fresh, head, true, fr);
+    __syncthreads();
+    if (which > 2) return;
+    float t[8];
+    if (which < 2) {
+        float2 cs[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) cs[e] = fresh.rope[sub % (LPK >> 1) * 8 + e];
+        rope8(fr[which] + sub * 8, fr[which] + (sub ^ (LPK >> 1)) * 8, cs, sub, LPK, t);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) t[e] = fr[2][sub * 8 + e];
+    }
+    *(uint4*)(qkv + (long)which * fresh.d + (long)head * D + sub * 8) = pack8(t);
+}
+// Puts the token into the cache as token n_keys - 1 and attends to all n_keys: in the attention launch itself, but for one token in 64, which completes
+// a block: its rows are formed, appended (the block becomes codes) and attended with one after another, in `qkv` ([3 d], scratch).
+hipError_t launch_decode_cache8(const Cache8& c, int n_keys, const DecodeFresh& fresh, const DecodeOut& out, bf16_t* qkv, float* ws, size_t ws_elems,
+                                hipStream_t s) {
+    if (n_keys < 1 || fresh.d != c.heads * c.d || (fresh.r & 7) || (out.a && (out.r & 7)) || !ws || ws_elems < (size_t)fresh.d + 2 * c.heads) return hipErrorInvalidValue;
+    const Attn8Plan p = attn8_plan(n_keys, 1, c.heads, c.heads, c.d, ws ? ws_elems : 0);
+    const bool whole = (n_keys & 63) == 0;
+    if (whole) {
+        if (c.d == 128) decode_token_kernel<128><<<c.heads, 256, 0, s>>>(fresh, qkv);
+        else decode_token_kernel<64><<<c.heads, 256, 0, s>>>(fresh, qkv);
+        hipError_t e = hipGetLastError();
+        if (e == hipSuccess) e = launch_cache8_append(c, n_keys - 1, qkv + fresh.d, 3L * fresh.d, qkv + 2L * fresh.d, 3L * fresh.d, 1, s);
+        if (e != hipSuccess) return e;
+    }
+    return c.d == 128 ? run_attention_cache8<128>(p, c, n_keys, qkv, 3L * fresh.d, 1, 1, out.o, fresh.d, ws, s, whole ? nullptr : &fresh, out)
+                      : run_attention_cache8<64>(p, c, n_keys, qkv, 3L * fresh.d, 1, 1, out.o, fresh.d, ws, s, whole ? nullptr : &fresh, out);
 }

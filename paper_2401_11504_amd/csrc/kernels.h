@@ -226,6 +226,9 @@ hipError_t launch_cache8_read(const Cache8& c, int n_cached, int first, int n, f
 constexpr int ATTN8_MAX_SPLIT = 64;
 hipError_t launch_attention_cache8(const Cache8& c, int n_keys, const bf16_t* q, long ldq, int n_rows, int heads, bf16_t* o, long ldo,
                                    float* ws, size_t ws_elems, hipStream_t s);
+// the newest token of a cache, formed, put in as token n_keys - 1, and its attention: qkv [3 d] and ws (heads * (d + 2) floats or more) are scratch
+hipError_t launch_decode_cache8(const Cache8& c, int n_keys, const DecodeFresh& fresh, const DecodeOut& out, bf16_t* qkv, float* ws, size_t ws_elems,
+                                hipStream_t s);
 const char* attention_cache8_plan(int n_keys, int n_rows, int heads, int kv_heads, int d, size_t ws_elems, int* n_ranges);   // a static string
 
 // ---------------------------------------------------------------- choice of the next token (choose.hip)

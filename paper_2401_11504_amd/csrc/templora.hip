@@ -169,6 +169,18 @@ struct tl_lora {
     // the previous module computed.
     bool kv_keep = false;
     std::vector<bf16_t*> kvbuf;
+    // tl_cache_8bit: with kv8 the cache is cache8 (buffers of its own as well, so that kvbuf is not needed for kv_keep)
+    bool kv8 = false;
+    std::vector<Cache8> cache8;
+    float* ws8 = nullptr;         // scratch of the attention over it
+    // choice of the next token (emit_next): what is set of penalties, bias and mask, and the tokens that the cache holds (pinned, read by the counts)
+    bool penalties = false, biased = false, masked = false;
+    tl_penalties pen = {1.f, 0.f, 0.f, 0};
+    int* text = nullptr;          // pinned [max_tokens]
+    int* counts = nullptr;        // [vocab], allocated with the next three by the first call that needs them
+    float* bias = nullptr;        // [vocab]
+    unsigned* allowed = nullptr;  // [ceil(vocab / 32)]
+    float* choose_ws = nullptr;
     float* lora_h = nullptr;      // [3 r] scaled low-rank activations of the projection group in flight
     float* dec_raw = nullptr;     // [max(3 d, 2 f)] frozen part of one token's q|k|v or gate|up
     float* dec_part = nullptr;    // shares of A o (one per head) or A_down act (one per DECODE_SW columns), r each
@@ -194,6 +206,7 @@ struct tl_lora {
 // Events that order the two streams of one GPU against each other: no timing, and no system-scope fence when they are
 // recorded (that fence writes the caches back and invalidates them for the host's and other devices' sake; kernels of
 // one device see each other's results through the release at the end of every kernel).
+static constexpr size_t kWs8Elems = (size_t)1 << 22;       // 16 MB: 64 ranges for up to 500 columns of 128
 static constexpr unsigned kSyncEvent = hipEventDisableTiming | hipEventDisableSystemFence;
 // Events that only bracket launches for timing: no system-scope fence either, which would lengthen what they measure.
 static constexpr unsigned kTimingEvent = hipEventDisableSystemFence;
@@ -328,6 +341,8 @@ static void lora_release(tl_lora* L) {
     if (L->verdict_host) (void)hipHostFree(L->verdict_host);
     L->verdict_host = nullptr;
     if (L->next_host) (void)hipHostFree(L->next_host);
+    if (L->text) (void)hipHostFree(L->text);
+    L->text = nullptr;
     L->tok_host = nullptr;
     L->next_host = nullptr;
     L->kv_len = 0;
@@ -471,6 +486,7 @@ extern "C" tl_status tl_lora_init(tl_model* m, const tl_lora_cfg* cfg, tl_lora**
         }
         HIPCHK(hipHostMalloc((void**)&L->tok_host, (size_t)Tm * sizeof(int), hipHostMallocDefault));
         HIPCHK(hipHostMalloc((void**)&L->next_host, 4 * sizeof(int), hipHostMallocDefault));
+        HIPCHK(hipHostMalloc((void**)&L->text, (size_t)Tm * sizeof(int), hipHostMallocDefault));
         TLCHK(L->pool.alloc(&L->lora_h, (size_t)3 * r));
         TLCHK(L->pool.alloc(&L->dec_raw, (size_t)std::max(3 * d, 2 * f)));
         TLCHK(L->pool.alloc(&L->dec_part, (size_t)std::max(mc.n_heads, cdiv(f, DECODE_SW)) * r));
@@ -620,7 +636,8 @@ static tl_status group_bwd(tl_lora* L, int l, int g, const bf16_t* dY, const bf1
 }
 
 // ---------------------------------------------------------------- one decoder layer
-static tl_status layer_forward(tl_lora* L, int l, const float* h_in, float* h_out, int T) {
+// n_past >= 0 (tl_extend): the T tokens follow n_past tokens of the 8-bit cache, which they join, and attend to all of it
+static tl_status layer_forward(tl_lora* L, int l, const float* h_in, float* h_out, int T, int n_past = -1) {
     tl_model* m = L->model;
     const tl_model_cfg& c = m->cfg;
     hipStream_t s = m->stream;
@@ -629,8 +646,13 @@ static tl_status layer_forward(tl_lora* L, int l, const float* h_in, float* h_ou
     const LayerW& W = m->layers[l];
     TLCHK(norm_fwd(L, h_in, W.g1, T, sv.x1));
     TLCHK(group_fwd(L, l, G_QKV, sv.x1, T, sv.qkv, nullptr, nullptr));
-    HIPCHK(launch_rope(sv.qkv, 3L * d, T, 2 * c.n_heads, c.d_head, c.rope_base, 0, +1, m->rope, s));  // q and k
-    HIPCHK(launch_attention_fwd(sv.qkv, sv.qkv + d, sv.qkv + 2 * d, 3L * d, T, c.n_heads, c.d_head, sv.o, d, sv.lse, s));
+    HIPCHK(launch_rope(sv.qkv, 3L * d, T, 2 * c.n_heads, c.d_head, c.rope_base, std::max(n_past, 0), +1, m->rope, s));  // q and k
+    if (n_past >= 0) {
+        HIPCHK(launch_cache8_append(L->cache8[l], n_past, sv.qkv + d, 3L * d, sv.qkv + 2 * d, 3L * d, T, s));
+        HIPCHK(launch_attention_cache8(L->cache8[l], n_past + T, sv.qkv, 3L * d, T, c.n_heads, sv.o, d, L->ws8, kWs8Elems, s));
+    } else {
+        HIPCHK(launch_attention_fwd(sv.qkv, sv.qkv + d, sv.qkv + 2 * d, 3L * d, T, c.n_heads, c.d_head, sv.o, d, sv.lse, s));
+    }
     int nsp_o = 0;
     TLCHK(group_fwd(L, l, G_O, sv.o, T, nullptr, sv.hmid, h_in, &nsp_o));
     if (nsp_o > 0) { L->pend_n = nsp_o; L->pend_h = sv.hmid; L->pend_resid = h_in; L->pend_T = T; }
@@ -930,8 +952,34 @@ extern "C" tl_status tl_chunk_train(tl_lora* L, const int32_t* tokens, int32_t n
 }
 
 // ---------------------------------------------------------------- generation side (Algorithm 1, the token loop)
-// Last-position logits -> greedy token; optional copy of the logits to the host.
-static tl_status emit_next(tl_lora* L, const float* h_last, int32_t* next_token, float* logits_out) {
+// n floats to the host, behind everything on the model's stream.  One copy on that stream and one wait: 12.3 us for 16 KB into
+// page-locked memory, where a synchronize and hipMemcpy took 14.9.
+static tl_status copy_out(tl_lora* L, float* host_out, const float* src, size_t n) {
+    hipStream_t s = L->model->stream;
+    hipError_t e = hipMemcpyAsync(host_out, src, n * sizeof(float), hipMemcpyDeviceToHost, s);
+    const hipError_t done = hipStreamSynchronize(s);       // (also after an error: nothing may still write to the caller's memory)
+    HIPCHK(e != hipSuccess ? e : done);
+    return TL_OK;
+}
+
+static size_t choose_ws_elems(int vocab) { return (size_t)2 * cdiv(vocab, 1024); }
+// the first n rows of a layer's bf16 cache into its 8-bit one
+static tl_status append_8bit(tl_lora* L, int l, const bf16_t* qkv, int n) {
+    const long d = L->model->cfg.d_model;
+    HIPCHK(launch_cache8_append(L->cache8[l], 0, qkv + d, 3 * d, qkv + 2 * d, 3 * d, n, L->model->stream));
+    return TL_OK;
+}
+static tl_status alloc_kvbuf(tl_lora* L) {
+    const tl_model_cfg& c = L->model->cfg;
+    std::vector<bf16_t*> bufs(c.n_layers, nullptr);
+    for (int l = 0; l < c.n_layers; ++l) TLCHK(L->pool.alloc(&bufs[l], (size_t)c.max_tokens * 3 * c.d_model));
+    L->kvbuf = bufs;
+    return TL_OK;
+}
+
+// Last-position logits -> the next token (greedy, behind what is set of penalties, bias and mask); optional copy of the logits to the host.
+// n_text: tokens of the text so far, in L->text.
+static tl_status emit_next(tl_lora* L, const float* h_last, int n_text, int32_t* next_token, float* logits_out) {
     tl_model* m = L->model;
     const tl_model_cfg& c = m->cfg;
     hipStream_t s = m->stream;
@@ -942,11 +990,35 @@ static tl_status emit_next(tl_lora* L, const float* h_last, int32_t* next_token,
     prof_mark(L);
     if (L->prof_on) L->prof_flop += 2.0 * c.vocab * (double)c.d_model;
     HIPCHK(e);
-    HIPCHK(launch_argmax(L->logits, c.vocab, L->next_host, s));
+    if (L->penalties || L->biased || L->masked) {
+        if (L->penalties) {
+            const int n = L->pen.last_n > 0 ? std::min(n_text, L->pen.last_n) : n_text;
+            HIPCHK(launch_token_counts(L->text + n_text - n, n, 1, n, c.vocab, 0, L->counts, c.vocab, s));
+        }
+        const Choose ch{L->logits, 0, L->penalties ? L->counts : nullptr, 0, L->biased ? L->bias : nullptr, 0, L->masked ? L->allowed : nullptr, 0,
+                        nullptr, 0, L->next_host, L->pen.repetition, L->pen.presence, L->pen.frequency};
+        HIPCHK(launch_choose(ch, 1, c.vocab, L->choose_ws, choose_ws_elems(c.vocab), s));
+    } else {
+        HIPCHK(launch_argmax(L->logits, c.vocab, L->next_host, s));
+    }
     if (logits_out)
         HIPCHK(hipMemcpyAsync(logits_out, L->logits, (size_t)c.vocab * sizeof(float), hipMemcpyDeviceToHost, s));
     HIPCHK(hipStreamSynchronize(s));
+    if (L->next_host[0] < 0) return fail(TL_ERR_ARG, "no token to choose: none is allowed, or the values of all allowed ones are undefined");
     *next_token = L->next_host[0];
+    return TL_OK;
+}
+
+// tokens that are to follow n_past cached ones, checked against the window and the vocabulary
+static tl_status check_text(tl_lora* L, const int32_t* tokens, int32_t n_tokens, int32_t n_past) {
+    const tl_model_cfg& c = L->model->cfg;
+    if (!tokens) return fail(TL_ERR_ARG, "tokens is null");
+    if (c.vocab <= 0) return fail(TL_ERR_SHAPE, "model was created without embedding / lm_head (vocab = 0)");
+    if (n_tokens < 1 || n_tokens > c.max_tokens - n_past)
+        return fail(TL_ERR_WINDOW, "n_tokens = %d outside [1, %d] (max_tokens = %d, %d cached)", n_tokens, c.max_tokens - n_past, c.max_tokens, n_past);
+    for (int i = 0; i < n_tokens; ++i)
+        if (tokens[i] < 0 || tokens[i] >= c.vocab)
+            return fail(TL_ERR_TOKEN_RANGE, "tokens[%d] = %d outside [0, %d)", i, tokens[i], c.vocab);
     return TL_OK;
 }
 
@@ -956,13 +1028,7 @@ extern "C" tl_status tl_prefill(tl_lora* L, const int32_t* tokens, int32_t n_tok
     if (!next_token) return fail(TL_ERR_ARG, "next_token is null");
     tl_model* m = L->model;
     const tl_model_cfg& c = m->cfg;
-    if (!tokens) return fail(TL_ERR_ARG, "tokens is null");
-    if (c.vocab <= 0) return fail(TL_ERR_SHAPE, "model was created without embedding / lm_head (vocab = 0)");
-    if (n_tokens < 1 || n_tokens > c.max_tokens)
-        return fail(TL_ERR_WINDOW, "n_tokens = %d outside [1, max_tokens = %d]", n_tokens, c.max_tokens);
-    for (int i = 0; i < n_tokens; ++i)
-        if (tokens[i] < 0 || tokens[i] >= c.vocab)
-            return fail(TL_ERR_TOKEN_RANGE, "tokens[%d] = %d outside [0, %d)", i, tokens[i], c.vocab);
+    TLCHK(check_text(L, tokens, n_tokens, 0));
     hipStream_t s = m->stream;
     const int T = n_tokens, d = c.d_model;
     L->kv_len = 0;
@@ -973,11 +1039,157 @@ extern "C" tl_status tl_prefill(tl_lora* L, const int32_t* tokens, int32_t n_tok
     L->pend_n = 0;
     for (int l = 0; l < c.n_layers; ++l) TLCHK(layer_forward(L, l, L->hs[l], L->hs[l + 1], T));
     TLCHK(flush_pending(L));      // the last layer's output rows are read directly below
-    if (L->kv_keep)
+    if (L->kv8)
+        for (int l = 0; l < c.n_layers; ++l) TLCHK(append_8bit(L, l, L->save[l].qkv, T));
+    else if (L->kv_keep)
         for (int l = 0; l < c.n_layers; ++l)
             HIPCHK(hipMemcpyAsync(L->kvbuf[l], L->save[l].qkv, (size_t)T * 3 * d * sizeof(bf16_t), hipMemcpyDeviceToDevice, s));
-    TLCHK(emit_next(L, L->hs[c.n_layers] + (size_t)(T - 1) * d, next_token, logits_out));
+    memcpy(L->text, tokens, (size_t)T * sizeof(int));
+    TLCHK(emit_next(L, L->hs[c.n_layers] + (size_t)(T - 1) * d, T, next_token, logits_out));
     L->kv_len = T;
+    return TL_OK;
+}
+
+extern "C" tl_status tl_extend(tl_lora* L, const int32_t* tokens, int32_t n_tokens, int32_t* next_token, float* logits_out) {
+    LIVE(L, "tl_extend");
+    if (!next_token) return fail(TL_ERR_ARG, "next_token is null");
+    if (!L->kv8) return fail(TL_ERR_ARG, "tl_extend: the cache is not held in 8 bits (tl_cache_8bit)");
+    if (L->kv_len <= 0) return fail(TL_ERR_ARG, "tl_extend: no key/value cache (call tl_prefill first)");
+    tl_model* m = L->model;
+    const tl_model_cfg& c = m->cfg;
+    const int T = n_tokens, past = L->kv_len, d = c.d_model;
+    TLCHK(check_text(L, tokens, T, past));
+    L->drop_on = false;
+    memcpy(L->tok_host, tokens, (size_t)T * sizeof(int));
+    HIPCHK(launch_embed(m->emb, L->tok_host, T, d, L->hs[0], m->stream));
+    L->pend_n = 0;
+    L->kv_len = 0;                // the cache is not what it was from here on, until the call has succeeded
+    for (int l = 0; l < c.n_layers; ++l) TLCHK(layer_forward(L, l, L->hs[l], L->hs[l + 1], T, past));
+    TLCHK(flush_pending(L));
+    memcpy(L->text + past, tokens, (size_t)T * sizeof(int));
+    TLCHK(emit_next(L, L->hs[c.n_layers] + (size_t)(T - 1) * d, past + T, next_token, logits_out));
+    L->kv_len = past + T;
+    return TL_OK;
+}
+
+// ---------------------------------------------------------------- cache in 8 bits
+extern "C" tl_status tl_cache_8bit(tl_lora* L, int32_t on) {
+    LIVE(L, "tl_cache_8bit");
+    tl_model* m = L->model;
+    const tl_model_cfg& c = m->cfg;
+    const size_t d = c.d_model;
+    if (!on) {
+        if (!L->kv8) return TL_OK;
+        if (L->kv_keep && L->kvbuf.empty()) TLCHK(alloc_kvbuf(L));
+        L->kv8 = false;
+        L->kv_len = 0;            // codes do not go back
+        return TL_OK;
+    }
+    if (L->kv8) return TL_OK;
+    if (L->cache8.empty()) {
+        const size_t nb = cdiv(c.max_tokens, 64);
+        std::vector<Cache8> all(c.n_layers);
+        if (!L->ws8) TLCHK(L->pool.alloc(&L->ws8, kWs8Elems));
+        for (Cache8& x : all) {
+            TLCHK(L->pool.alloc(&x.k, nb * 64 * d));
+            TLCHK(L->pool.alloc(&x.v, nb * 64 * d));
+            TLCHK(L->pool.alloc(&x.ks, nb * c.n_heads));
+            TLCHK(L->pool.alloc(&x.vs, nb * c.n_heads));
+            TLCHK(L->pool.alloc(&x.kt, 64 * d));
+            TLCHK(L->pool.alloc(&x.vt, 64 * d));
+            x.heads = c.n_heads, x.d = c.d_head;
+        }
+        L->cache8 = all;
+    }
+    // a cache that exists already moves along
+    for (int l = 0; l < c.n_layers && L->kv_len > 0; ++l) TLCHK(append_8bit(L, l, L->kv_keep ? L->kvbuf[l] : L->save[l].qkv, L->kv_len));
+    HIPCHK(hipStreamSynchronize(m->stream));
+    L->kv8 = true;
+    return TL_OK;
+}
+
+extern "C" tl_status tl_get_kv(tl_lora* L, int32_t layer, int32_t first, int32_t n, float* k_out, float* v_out) {
+    LIVE(L, "tl_get_kv");
+    tl_model* m = L->model;
+    const tl_model_cfg& c = m->cfg;
+    const int d = c.d_model;
+    if (!k_out || !v_out) return fail(TL_ERR_ARG, "tl_get_kv: null pointer");
+    if (layer < 0 || layer >= c.n_layers) return fail(TL_ERR_ARG, "layer %d out of range", layer);
+    if (first < 0 || n < 0 || (int64_t)first + n > L->kv_len) return fail(TL_ERR_WINDOW, "tokens %d + %d of %d cached", first, n, L->kv_len);
+    if (!L->kv8) {                // bf16 rows: widened here
+        std::vector<uint16_t> row;
+        try { row.resize((size_t)n * d); } catch (const std::bad_alloc&) { return fail(TL_ERR_OOM, "host allocation failed"); }
+        HIPCHK(hipStreamSynchronize(m->stream));
+        for (int which = 1; which <= 2 && n > 0; ++which) {
+            const bf16_t* src = (L->kv_keep ? L->kvbuf[layer] : L->save[layer].qkv) + ((size_t)first * 3 + which) * d;
+            HIPCHK(hipMemcpy2D(row.data(), (size_t)d * 2, src, (size_t)d * 6, (size_t)d * 2, n, hipMemcpyDeviceToHost));
+            float* out = which == 1 ? k_out : v_out;
+            for (size_t i = 0; i < (size_t)n * d; ++i) {
+                const uint32_t u = (uint32_t)row[i] << 16;
+                memcpy(out + i, &u, 4);
+            }
+        }
+        return TL_OK;
+    }
+    const int step = std::max(c.max_tokens / 2, 1);        // rows of keys and of values that a temporary of [max_tokens, d] holds
+    for (int i = 0; i < n; i += step) {
+        const int rows = std::min(n - i, step);
+        float *k = L->dhmid, *v = L->dhmid + (size_t)rows * d;
+        HIPCHK(launch_cache8_read(L->cache8[layer], L->kv_len, first + i, rows, k, d, v, d, m->stream));
+        TLCHK(copy_out(L, k_out + (size_t)i * d, k, (size_t)rows * d));
+        TLCHK(copy_out(L, v_out + (size_t)i * d, v, (size_t)rows * d));
+    }
+    return TL_OK;
+}
+
+// ---------------------------------------------------------------- choice of the next token
+static tl_status choice_buffers(tl_lora* L, const char* name) {
+    const int V = L->model->cfg.vocab;
+    if (V <= 0) return fail(TL_ERR_SHAPE, "%s: model was created without embedding / lm_head (vocab = 0)", name);
+    if (!L->counts) TLCHK(L->pool.alloc(&L->counts, (size_t)V));
+    if (!L->bias) TLCHK(L->pool.alloc(&L->bias, (size_t)V));
+    if (!L->allowed) TLCHK(L->pool.alloc(&L->allowed, (size_t)cdiv(V, 32)));
+    if (!L->choose_ws) TLCHK(L->pool.alloc(&L->choose_ws, choose_ws_elems(V)));
+    return TL_OK;
+}
+extern "C" tl_status tl_set_penalties(tl_lora* L, const tl_penalties* p) {
+    LIVE(L, "tl_set_penalties");
+    if (!p) {
+        L->penalties = false;
+        L->pen = {1.f, 0.f, 0.f, 0};
+        return TL_OK;
+    }
+    const tl_penalties c = *p;
+    if (!(c.repetition > 0.f) || !std::isfinite(c.repetition) || !std::isfinite(c.presence) || !std::isfinite(c.frequency) || c.last_n < 0)
+        return fail(TL_ERR_ARG, "tl_set_penalties: repetition %g (above 0), presence %g, frequency %g, last_n %d (0 or more)", c.repetition, c.presence,
+                    c.frequency, c.last_n);
+    TLCHK(choice_buffers(L, "tl_set_penalties"));
+    L->pen = c;
+    L->penalties = true;
+    return TL_OK;
+}
+extern "C" tl_status tl_set_bias(tl_lora* L, const float* bias) {
+    LIVE(L, "tl_set_bias");
+    if (!bias) {
+        L->biased = false;
+        return TL_OK;
+    }
+    TLCHK(choice_buffers(L, "tl_set_bias"));
+    HIPCHK(hipStreamSynchronize(L->model->stream));
+    HIPCHK(hipMemcpy(L->bias, bias, (size_t)L->model->cfg.vocab * sizeof(float), hipMemcpyHostToDevice));
+    L->biased = true;
+    return TL_OK;
+}
+extern "C" tl_status tl_set_allowed(tl_lora* L, const uint32_t* allowed) {
+    LIVE(L, "tl_set_allowed");
+    if (!allowed) {
+        L->masked = false;
+        return TL_OK;
+    }
+    TLCHK(choice_buffers(L, "tl_set_allowed"));
+    HIPCHK(hipStreamSynchronize(L->model->stream));
+    HIPCHK(hipMemcpy(L->allowed, allowed, (size_t)cdiv(L->model->cfg.vocab, 32) * sizeof(unsigned), hipMemcpyHostToDevice));
+    L->masked = true;
     return TL_OK;
 }
 
@@ -991,11 +1203,11 @@ extern "C" tl_status tl_cache_reuse(tl_lora* L, int32_t on) {
         return TL_OK;
     }
     if (L->kv_keep) return TL_OK;
-    if (L->kvbuf.empty()) {
-        std::vector<bf16_t*> bufs(c.n_layers, nullptr);
-        for (int l = 0; l < c.n_layers; ++l) TLCHK(L->pool.alloc(&bufs[l], (size_t)c.max_tokens * 3 * c.d_model));
-        L->kvbuf = bufs;
+    if (L->kv8) {                         // the 8-bit cache has buffers of its own already
+        L->kv_keep = true;
+        return TL_OK;
     }
+    if (L->kvbuf.empty()) TLCHK(alloc_kvbuf(L));
     // a cache that exists already moves along
     for (int l = 0; l < c.n_layers && L->kv_len > 0; ++l)
         HIPCHK(hipMemcpyAsync(L->kvbuf[l], L->save[l].qkv, (size_t)L->kv_len * 3 * c.d_model * sizeof(bf16_t),
@@ -1054,7 +1266,6 @@ extern "C" tl_status tl_decode_step(tl_lora* L, int32_t token, int32_t* next_tok
         const LayerW& W = m->layers[l];
         const float* h_in = L->hs[l];
         float* h_out = L->hs[l + 1];
-        bf16_t* cache = L->kv_keep ? L->kvbuf[l] : sv.qkv;
         const LayerOff& o = L->off[l];
         TLCHK(group_decode_in(L, l, G_QKV, h_in, W.g1));
         // the attention launch finishes q, k and v of the new token, rotates q and k and puts k and v into the cache
@@ -1063,15 +1274,21 @@ extern "C" tl_status tl_decode_step(tl_lora* L, int32_t token, int32_t* next_tok
         fresh.rope = m->rope + (size_t)p * (c.d_head / 2);
         DecodeOut out;
         out.o = sv.o; out.a = L->S + o.A[G_O]; out.r = L->cfg.rank; out.part = L->dec_part;
-        HIPCHK(launch_attention_decode(nullptr, cache + d, cache + 2 * d, 3L * d, p + 1, c.n_heads, c.d_head, out, L->attn_ws,
-                                       L->attn_ws_elems, s, fresh));
+        if (L->kv8) {
+            HIPCHK(launch_decode_cache8(L->cache8[l], p + 1, fresh, out, sv.qkv, L->ws8, kWs8Elems, s));
+        } else {
+            bf16_t* cache = L->kv_keep ? L->kvbuf[l] : sv.qkv;
+            HIPCHK(launch_attention_decode(nullptr, cache + d, cache + 2 * d, 3L * d, p + 1, c.n_heads, c.d_head, out, L->attn_ws,
+                                           L->attn_ws_elems, s, fresh));
+        }
         TLCHK(group_decode_out(L, l, G_O, sv.o, sv.hmid, h_in, c.n_heads));
         TLCHK(group_decode_in(L, l, G_GU, sv.hmid, W.g2));
         HIPCHK(launch_decode_swiglu(L->dec_raw, L->S + o.B[G_GU], L->lora_h, L->cfg.rank, c.d_ffn, sv.act,
                                     L->S + o.A[G_DOWN], L->dec_part, s));
         TLCHK(group_decode_out(L, l, G_DOWN, sv.act, h_out, sv.hmid, cdiv(c.d_ffn, DECODE_SW)));
     }
-    TLCHK(emit_next(L, L->hs[c.n_layers], next_token, logits_out));
+    L->text[p] = token;
+    TLCHK(emit_next(L, L->hs[c.n_layers], p + 1, next_token, logits_out));
     L->kv_len = p + 1;
     return TL_OK;
 }
@@ -1169,16 +1386,6 @@ static tl_status factor_span(tl_lora* L, int layer, int proj, int which, size_t 
     const bool isB = which & 1;
     if (n != (isB ? nb : na)) return fail(TL_ERR_ARG, "size mismatch: expected %zu elements", isB ? nb : na);
     *off = isB ? L->off[layer].B[g] + i * nb : L->off[layer].A[g] + i * na;
-    return TL_OK;
-}
-
-// n floats to the host, behind everything on the model's stream.  One copy on that stream and one wait: 12.3 us for 16 KB into
-// page-locked memory, where a synchronize and hipMemcpy took 14.9.
-static tl_status copy_out(tl_lora* L, float* host_out, const float* src, size_t n) {
-    hipStream_t s = L->model->stream;
-    hipError_t e = hipMemcpyAsync(host_out, src, n * sizeof(float), hipMemcpyDeviceToHost, s);
-    const hipError_t done = hipStreamSynchronize(s);       // (also after an error: nothing may still write to the caller's memory)
-    HIPCHK(e != hipSuccess ? e : done);
     return TL_OK;
 }
 
