@@ -487,7 +487,7 @@ tl_status tl_k_cache8_read(const tl_cache8_mem* cache, int32_t n_cached, int32_t
  * of n_kv_heads; query head j reads key head j / (n_heads / n_kv_heads).  n_rows <= n_keys.
  * workspace: NULL, or device fp32 scratch of workspace_elems floats: with it the keys are cut into up to 64 ranges where the rows are few,
  * n_rows * n_heads * ranges * (d_head + 2) floats are used; contents are undefined before and after, and calls that overlap in time need one
- * each.  tl_k_attention_cache8_plan: the name of the kernel that these sizes get ("columns16", "rows128" or "rows256"), its ranges and the floats that it uses of a
+ * each.  tl_k_attention_cache8_plan: the name of the kernel that these sizes get ("columns16", "columns8", "rows128" or "rows256"), its ranges and the floats that it uses of a
  * workspace of workspace_elems floats (host only). */
 tl_status tl_k_attention_cache8(const tl_cache8_mem* cache, int32_t n_keys, const uint16_t* q, int32_t ldq, int32_t n_rows, int32_t n_heads,
                                 uint16_t* o, int32_t ldo, float* workspace, size_t workspace_elems, void* hip_stream);

@@ -243,8 +243,8 @@ hipError_t launch_cache8_read(const Cache8& c, int n_cached, int first, int n, f
 }
 
 // ---------------------------------------------------------------- attention of a few rows
-// A row of queries and one of the query heads that share a key head make a column; a workgroup has the (up to 16) columns of one key head,
-// and each of its four waves takes every fourth block of the workgroup's range of the cache:
+// A row of queries and one of the query heads that share a key head make a column; a workgroup has the columns of one key head (up to 16 with four
+// waves, up to 8 with eight), and each of its waves takes every fourth (eighth) block of the workgroup's range of the cache:
 //   S^T[key][column] = K q^T   and   O^T[d][column] += V^T P^T     by v_mfma_f32_16x16x32_bf16
 // (lane = 16 g + m:  A: row m, contraction slots 8 g ..;  B: column m, the same slots;  D: column m, rows 4 g .. 4 g + 3).  Codes are
 // whole numbers up to 127, exact in bf16, so the scores are products of what is stored, summed in fp32, and the scales come in behind:
@@ -266,9 +266,8 @@ __device__ __forceinline__ bf16x8_t codes_bf16(unsigned lo, unsigned hi) {
     for (int e = 0; e < 8; ++e) r[e] = (__bf16)(float)(int8_t)((e < 4 ? lo : hi) >> 8 * (e & 3));
     return r;
 }
-// eight bf16 of a tail's value row from slot u0 on, zero from slot `end` on; *odd: whether one that stays is not finite
-__device__ __forceinline__ uint4 tail_values(const bf16_t* row, int u0, int end, bool* odd) {
-    uint4 w = *(const uint4*)(row + u0);
+// eight bf16 of a tail's value row, slots u0 .., zero from slot `end` on; *odd: whether one that stays is not finite
+__device__ __forceinline__ uint4 tail_values(uint4 w, int u0, int end, bool* odd) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         unsigned& x = (&w.x)[e];
@@ -282,12 +281,12 @@ __device__ __forceinline__ uint4 tail_values(const bf16_t* row, int u0, int end,
 // FRESH: the token being decoded, one row of as many query as key heads.  Its q, k and v do not exist as rows yet: every workgroup forms its head's q
 // (while its first codes are on their way), and the one whose range ends with the tail forms k and v and puts them there.  The token must not
 // complete a block.
-template <int D, bool FRESH>
-__global__ __launch_bounds__(256, 2) void attn8_cols_kernel(Cache8 c, int n_keys, const bf16_t* __restrict__ q, long ldq, int n_rows, int group,
+template <int D, int NW, bool FRESH>
+__global__ __launch_bounds__(NW * 64, 8 / NW) void attn8_cols_kernel(Cache8 c, int n_keys, const bf16_t* __restrict__ q, long ldq, int n_rows, int group,
                                                             float scale_log2e, bf16_t* __restrict__ o, long ldo, float* __restrict__ ws,
                                                             int blocks_per_split, DecodeFresh fresh, DecodeOut more) {
-    constexpr int PC = D / 64, NT = D / 16, LDP = D + 4;
-    __shared__ float part[4][16][LDP];                     // a column's output, maximum and sum, wave by wave
+    constexpr int PC = D / 64, NT = D / 16, LDP = D + 4, NCOL = 64 / NW, PART = NCOL * LDP > 1024 ? NCOL * LDP : 1024;
+    __shared__ __align__(16) float part[NW][PART];         // a column's output, maximum and sum, wave by wave
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m16 = lane & 15, g = lane >> 4;
     const int head = blockIdx.x, n_cols = n_rows * group, heads = c.heads * group;
     const int col = min(m16, n_cols - 1), row = col / group, seen = n_keys - n_rows + row + 1;      // keys 0 .. seen - 1
@@ -314,7 +313,7 @@ __global__ __launch_bounds__(256, 2) void attn8_cols_kernel(Cache8 c, int n_keys
         __shared__ __align__(16) bf16_t sq[D];
         __builtin_amdgcn_sched_barrier(0);
         const bool last = b_tail >= b_begin && b_tail < b_end;
-        fresh_rows<D, 256>(fresh, head, last, fr);
+        fresh_rows<D, NW * 64>(fresh, head, last, fr);
         const int which = threadIdx.x / LPK, sub = threadIdx.x % LPK, slot = n_keys - 1 & 63;
         __syncthreads();
         if (which == 0 || (which == 1 && last)) {          // q and k, rotated
@@ -374,7 +373,7 @@ __global__ __launch_bounds__(256, 2) void attn8_cols_kernel(Cache8 c, int n_keys
 #pragma unroll
         for (int t = 0; t < NT; ++t) oacc[t] *= alpha;
     };
-    for (; b < b_full; b += 4) {
+    for (; b < b_full; b += NW) {
         const long at = (long)b * c.heads + head;
 #pragma unroll
         for (int t = 0; t < NT; ++t) vr[t] = load_once(c.v + at * 64 * D + (t * 16 + m16) * 64 + g * 16);
@@ -390,7 +389,7 @@ __global__ __launch_bounds__(256, 2) void attn8_cols_kernel(Cache8 c, int n_keys
             }
             __builtin_amdgcn_sched_barrier(0);             // (widened codes of more than one group would not fit the registers)
         }
-        if (b + 4 < b_full) keys(b + 4);
+        if (b + NW < b_full) keys(b + NW);
         softmax(b, ks, vs);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
@@ -406,31 +405,39 @@ __global__ __launch_bounds__(256, 2) void attn8_cols_kernel(Cache8 c, int n_keys
         const bf16_t *kt = c.kt + (long)head * 64 * D, *vt = c.vt + (long)head * 64 * D;
         const int end = n_keys & 63;
         bool odd = false;
+        uint4 kw[4][2 * PC], vw[NT][2];                    // all of it on its way before the first is used
+#pragma unroll
+        for (int kg = 0; kg < 4; ++kg)
+#pragma unroll
+            for (int st = 0; st < 2 * PC; ++st) kw[kg][st] = *(const uint4*)(kt + (st >> 1) * 4096 + (key0 + kg * 4) * 64 + g * 16 + (st & 1) * 8);
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) (void)tail_values(vt + (t * 16 + m16) * 64, g * 16 + h * 8, end, &odd);
+            for (int h = 0; h < 2; ++h) vw[t][h] = *(const uint4*)(vt + (t * 16 + m16) * 64 + g * 16 + h * 8);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int kg = 0; kg < 4; ++kg) {
             s[kg] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int st = 0; st < 2 * PC; ++st)
-                s[kg] = mfma16(__builtin_bit_cast(bf16x8_t, *(const uint4*)(kt + (st >> 1) * 4096 + (key0 + kg * 4) * 64 + g * 16 + (st & 1) * 8)),
-                               qf[st], s[kg]);
+            for (int st = 0; st < 2 * PC; ++st) s[kg] = mfma16(__builtin_bit_cast(bf16x8_t, kw[kg][st]), qf[st], s[kg]);
         }
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) vw[t][h] = tail_values(vw[t][h], g * 16 + h * 8, end, &odd);
         softmax(b, scale_log2e, 1.f);
         if (!__builtin_amdgcn_ballot_w64(odd)) {
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const bf16x8_t a = __builtin_bit_cast(bf16x8_t, tail_values(vt + (t * 16 + m16) * 64, g * 16 + h * 8, end, &odd));
+                    const bf16x8_t a = __builtin_bit_cast(bf16x8_t, vw[t][h]);
                     oacc[t] = mfma16(a, hi[h], oacc[t]);
                     oacc[t] = mfma16(a, lo[h], oacc[t]);
                 }
         } else {
             // a value that is not finite counts for the columns that see it alone, which a product with zeros does not give
-            float* pl = &part[wave][0][0];
+            float* pl = part[wave];
 #pragma unroll
             for (int i = 0; i < 16; ++i) pl[(g * 16 + i) * 16 + m16] = x[i];
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -447,27 +454,29 @@ __global__ __launch_bounds__(256, 2) void attn8_cols_kernel(Cache8 c, int n_keys
     }
     l += __shfl_xor(l, 16, 64);
     l += __shfl_xor(l, 32, 64);
+    if (m16 < NCOL) {
+        float* mine = part[wave] + m16 * LDP;
 #pragma unroll
-    for (int t = 0; t < NT; ++t) *(f32x4_t*)&part[wave][m16][t * 16 + g * 4] = oacc[t];
-    if (g == 0) { part[wave][m16][D] = m; part[wave][m16][D + 1] = l; }
+        for (int t = 0; t < NT; ++t) *(f32x4_t*)(mine + t * 16 + g * 4) = oacc[t];
+        if (g == 0) { mine[D] = m; mine[D + 1] = l; }
+    }
     uint4 av[4];
     if constexpr (FRESH)
-        if (!ws) head_output_fetch<D, 256>(head, heads, more, av);
+        if (!ws) head_output_fetch<D, NW * 64>(head, heads, more, av);
     __syncthreads();
     float one = 0.f;                                       // FRESH without ranges: this thread's column of the output
-    for (int i = threadIdx.x; i < 16 * D; i += 256) {
+    for (int i = threadIdx.x; i < n_cols * D; i += NW * 64) {
         const int cc = i / D, e = i % D;
-        if (cc >= n_cols) break;
-        float mt = part[0][cc][D];
+        float mt = -INFINITY, lt = 0.f, ot = 0.f;
 #pragma unroll
-        for (int w = 1; w < 4; ++w) mt = fmaxf(mt, part[w][cc][D]);
+        for (int w = 0; w < NW; ++w) mt = fmaxf(mt, part[w][cc * LDP + D]);
         const float base = mt == -INFINITY ? 0.f : mt;     // (of a range that the column sees nothing of)
-        float lt = 0.f, ot = 0.f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const float a = __builtin_amdgcn_exp2f(part[w][cc][D] - base);
-            lt += a * part[w][cc][D + 1];
-            ot += a * part[w][cc][e];
+        for (int w = 0; w < NW; ++w) {
+            const float* p = part[w] + cc * LDP;
+            const float a = __builtin_amdgcn_exp2f(p[D] - base);
+            lt += a * p[D + 1];
+            ot += a * p[e];
         }
         const int r = cc / group, qh = head * group + cc % group;
         if (!ws) {
@@ -480,20 +489,20 @@ __global__ __launch_bounds__(256, 2) void attn8_cols_kernel(Cache8 c, int n_keys
         }
     }
     if constexpr (FRESH)
-        if (!ws) head_output<D, 256>(one, threadIdx.x % D, head, heads, more, av);
+        if (!ws) head_output<D, NW * 64>(one, threadIdx.x % D, head, heads, more, av);
 }
 
-// The ranges of a row and head, one thread a column: lane i holds range i's maximum and sum, and sixteen ranges' columns are asked for before
-// the first is used.
-template <int D>
+// The ranges of a row and head, one thread a column: lane i holds range i's maximum and sum, and NR ranges' columns are asked for before the first is
+// used (6 ranges with NR 8 0.9 us less than with 32).
+template <int D, int NR>
 __global__ __launch_bounds__(D) void attn8_join_kernel(const float* __restrict__ ws, int n_split, int heads, long ldo, DecodeOut out) {
     const int e = threadIdx.x, lane = threadIdx.x & 63, head = blockIdx.x % heads;
     const float* w = ws + (long)blockIdx.x * n_split * (D + 2);
     const int r = min(lane, n_split - 1);
     const float m = w[r * (D + 2) + D], l = w[r * (D + 2) + D + 1];
-    float t[16];
+    float t[NR];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) t[i] = w[min(i, n_split - 1) * (D + 2) + e];
+    for (int i = 0; i < NR; ++i) t[i] = w[min(i, n_split - 1) * (D + 2) + e];
     uint4 av[8];
     head_output_fetch<D, D>(head, heads, out, av);
     __builtin_amdgcn_sched_barrier(0);
@@ -501,13 +510,13 @@ __global__ __launch_bounds__(D) void attn8_join_kernel(const float* __restrict__
     const float a = lane < n_split ? __builtin_amdgcn_exp2f(m - top) : 0.f;      // (one range has keys: top is a number, or all is NaN)
     const float sum = wave_sum(lane < n_split ? a * l : 0.f);
     float acc = 0.f;
-    for (int i0 = 0; i0 < n_split; i0 += 16) {
+    for (int i0 = 0; i0 < n_split; i0 += NR) {
         if (i0) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) t[i] = w[min(i0 + i, n_split - 1) * (D + 2) + e];
+            for (int i = 0; i < NR; ++i) t[i] = w[min(i0 + i, n_split - 1) * (D + 2) + e];
         }
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
+        for (int i = 0; i < NR; ++i) {
             const float ai = __shfl(a, i0 + i, 64);
             acc += i0 + i < n_split ? ai * t[i] : 0.f;
         }
@@ -597,7 +606,8 @@ __global__ __launch_bounds__(NC * 64, 2) void attn8_rows_kernel(Cache8 c, int n_
                 *(uint4*)(st + k_piece_at<D>(key, ch + 1)) = *(const uint4*)(kt + p * 16 + 8);
             } else {
                 const int d = (p - NP) >> 2, ch = (p & 3) * 2, u0 = (p & 3) * 16;
-                const uint4 a = tail_values(vt + d * 64, u0, n_keys & 63, &odd), b = tail_values(vt + d * 64, u0 + 8, n_keys & 63, &odd);
+                const uint4 a = tail_values(*(const uint4*)(vt + d * 64 + u0), u0, n_keys & 63, &odd);
+                const uint4 b = tail_values(*(const uint4*)(vt + d * 64 + u0 + 8), u0 + 8, n_keys & 63, &odd);
                 *(uint4*)(st + TB + v_piece_at(d, ch)) = make_uint4(a.x, a.y, b.x, b.y);
                 *(uint4*)(st + TB + v_piece_at(d, ch + 1)) = make_uint4(a.z, a.w, b.z, b.w);
             }
@@ -731,15 +741,20 @@ static constexpr size_t attn8_rows_lds() {
 }
 
 // Which kernel, and how the keys are cut.
-//   columns16         up to 16 columns of a key head.  us for 2 rows of 32 heads of 128, this and rows128: 300 keys 8.2 and 8.1, 1500 9.5 and 12.5,
-//                     4000 12.2 and 18.6; 17 rows: 300 keys 10.2 and 8.7, 1500 13.3 and 13.2, 4000 19.1 and 15.5
+//   columns16, columns8  up to 16 columns of a key head: four waves for 16 columns, or eight for 8 that share the blocks of a range.  us for 2 rows of 32
+//                     heads of 128, this and rows128: 300 keys 8.2 and 8.1, 1500 9.5 and 12.5, 4000 12.2 and 18.6; 17 rows: 300 keys 10.2 and 8.7,
+//                     1500 13.3 and 13.2, 4000 19.1 and 15.5
 //   rows128, rows256  more columns: 256 to a workgroup where that leaves 16 workgroups or more for a range of the keys (2048 rows of 32 heads over 8192
-//                     keys 286; 200 rows, 4000 keys, 128 and 256: 32 heads 37.2 and 34.5, 4 heads 16.7 and 19.0)
-// Ranges, columns16: none up to 8 blocks (one row of 32 heads, 500 keys: 8.6 without, 8.7 at best; 700 keys 11.0 and 9.0); else two workgroups a CU, of
-// three blocks or more, but one a CU where each has over 16 blocks (131072 keys of 8 heads 52.1 and 50.2, 32768 of 32 52.0 and 49.5).
+//                     keys 257; 200 rows, 4000 keys, 128 and 256: 32 heads 37.2 and 34.5, 4 heads 16.7 and 19.0)
+// Ranges of few columns: none up to 11 blocks, from 5 on with eight waves (one row of 32 heads, 500 keys: 7.8 with four waves, 7.5 with eight, 8.0 cut; 700
+// keys 10.1, 8.4, 8.2 and a launch more; 1000 keys 12.4, 11.9, 8.3).  Else two workgroups a CU, of three blocks or more, but one a CU where each has over
+// 16 blocks (32768 keys of 32 heads 50.9 and 48.2).  Where that is over 16 ranges (few key heads), 16 of up to four blocks
+// (4000 keys of 8 heads: 16 8.9, 21 9.9) or 32 of eight waves (16000 keys of 8 heads: 64 of four
+// waves 14.4, 32 of eight 12.3), from 512 blocks on as many as leave a workgroup for each CU (65536 keys of 2 heads: 32 21.8, 64 16.4; 8000 keys of one: 32
+// 9.1, 42 10.3).
 // Ranges, rows: what costs least of a launch's tiles one after another (1.75 us each with one workgroup of 128 columns on a CU, 2.7 with two; 2.3 of 256
 // columns) and of the join (3 us, and its floats written and read at 3.5 TB/s).
-struct Attn8Plan { int cols, n_split, per; };       // columns a workgroup, ranges, blocks a range
+struct Attn8Plan { int cols, waves, n_split, per; };       // columns and waves a workgroup, ranges, blocks a range
 static Attn8Plan attn8_plan(int n_keys, int n_rows, int heads, int kv_heads, int d, size_t ws_elems) {
     const int nb = cdiv(n_keys, 64);
     const long n_cols = (long)n_rows * (heads / kv_heads);
@@ -747,12 +762,18 @@ static Attn8Plan attn8_plan(int n_keys, int n_rows, int heads, int kv_heads, int
     const long units = kv_heads * (long)cdiv(n_cols, cols), range_elems = (long)n_rows * heads * (d + 2);
     const long most = std::min<long>(std::min<long>(nb, ATTN8_MAX_SPLIT), (long)(ws_elems / (size_t)range_elems));
     long n = 1;
+    int waves = cols == 16 ? 4 : cols / 32;
     if (cols == 16) {
-        if (nb > 8) {
+        if (nb > 11) {
             n = std::min<long>(512 / units, cdiv(nb, 3));
-            if (n > 1 && cdiv(nb, n) > 16) n = 256 / units;
+            if (n > 16 && nb <= 64) n = 16;
+            else if (n > 16 && n_cols <= 8) {
+                waves = 8;
+                n = std::min(n, nb > 512 ? std::max(32l, 256 / units) : 32l);
+            } else if (n > 1 && cdiv(nb, n) > 16) n = 256 / units;
         }
         n = std::min(n, most);
+        if (n < 2 && nb > 4 && n_cols <= 8) waves = 8;
     } else {
         auto cost = [&](long r) {
             const long w = units * r, slots = cols == 128 ? 512 : 256, rest = w % slots;
@@ -762,14 +783,14 @@ static Attn8Plan attn8_plan(int n_keys, int n_rows, int heads, int kv_heads, int
         for (long r = 2; r <= most; ++r)
             if (cost(r) < cost(n)) n = r;
     }
-    if (n < 2) return {cols, 1, nb};
+    if (n < 2) return {cols, waves, 1, nb};
     const int per = cdiv(nb, n);
-    return {cols, cdiv(nb, per), per};
+    return {cols, waves, cdiv(nb, per), per};
 }
 const char* attention_cache8_plan(int n_keys, int n_rows, int heads, int kv_heads, int d, size_t ws_elems, int* n_ranges) {
     const Attn8Plan p = attn8_plan(n_keys, n_rows, heads, kv_heads, d, ws_elems);
     *n_ranges = p.n_split;
-    return p.cols == 16 ? "columns16" : p.cols == 128 ? "rows128" : "rows256";
+    return p.cols == 16 ? (p.waves == 8 ? "columns8" : "columns16") : p.cols == 128 ? "rows128" : "rows256";
 }
 template <int D>
 static hipError_t run_attention_cache8(const Attn8Plan& p, const Cache8& c, int n_keys, const bf16_t* q, long ldq, int n_rows, int group, bf16_t* o,
@@ -788,12 +809,16 @@ static hipError_t run_attention_cache8(const Attn8Plan& p, const Cache8& c, int 
     };
     hipError_t e;
     if (p.cols == 16) {                                    // (one workgroup holds all the columns of a key head)
-        auto kernel = fresh ? attn8_cols_kernel<D, true> : attn8_cols_kernel<D, false>;
-        kernel<<<dim3(c.heads, p.n_split), 256, 0, s>>>(c, n_keys, q, ldq, n_rows, group, scale, o, ldo, w, p.per, fresh ? *fresh : DecodeFresh{}, out);
+        auto cols = [&](auto kernel, int threads) {
+            kernel<<<dim3(c.heads, p.n_split), threads, 0, s>>>(c, n_keys, q, ldq, n_rows, group, scale, o, ldo, w, p.per, fresh ? *fresh : DecodeFresh{}, out);
+        };
+        if (p.waves == 8) fresh ? cols(attn8_cols_kernel<D, 8, true>, 512) : cols(attn8_cols_kernel<D, 8, false>, 512);
+        else fresh ? cols(attn8_cols_kernel<D, 4, true>, 256) : cols(attn8_cols_kernel<D, 4, false>, 256);
         e = hipGetLastError();
     } else e = p.cols == 128 ? rows(std::integral_constant<int, 4>{}) : rows(std::integral_constant<int, 8>{});
     if (e != hipSuccess || !w) return e;
-    attn8_join_kernel<D><<<n_rows * c.heads * group, D, 0, s>>>(w, p.n_split, c.heads * group, ldo, out);
+    auto join = p.n_split <= 8 ? attn8_join_kernel<D, 8> : p.n_split <= 16 ? attn8_join_kernel<D, 16> : attn8_join_kernel<D, 32>;
+    join<<<n_rows * c.heads * group, D, 0, s>>>(w, p.n_split, c.heads * group, ldo, out);
     return hipGetLastError();
 }
 hipError_t launch_attention_cache8(const Cache8& c, int n_keys, const bf16_t* q, long ldq, int n_rows, int heads, bf16_t* o, long ldo,

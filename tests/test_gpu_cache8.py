@@ -147,7 +147,7 @@ def check(api, c, n, k, v, q, heads, kv, workspace=None, p_rounding=None):
     d = c.d_head
     if p_rounding is None:
         name = api.tl_k_attention_cache8_plan(n, q.shape[0], heads, kv, d, 0 if workspace is None else workspace.numel())[0]
-        p_rounding = HI_LO if name == "columns16" else BF16
+        p_rounding = HI_LO if name.startswith("columns") else BF16
     got = attend(api, c, n, q, heads, workspace).double().view(q.shape[0], heads, d)
     want, size, reach = oracle.attention(q, oracle.held(k[:n], kv)[0], oracle.held(v[:n], kv)[0], heads)
     far = (got - want).abs() - oracle.attention_bound(want, size, reach, d, n, p_rounding)
@@ -159,7 +159,7 @@ def queries(seed, rows, width):
 
 
 @pytest.mark.parametrize("heads,kv,d", [(1, 1, 64), (4, 4, 128), (6, 2, 64), (8, 1, 128), (20, 1, 64)])
-@pytest.mark.parametrize("n", [1, 2, 63, 64, 65, 128, 130, 257, 700])
+@pytest.mark.parametrize("n", [1, 2, 63, 64, 65, 128, 130, 257, 512, 700, 705, 1500, 3333])
 def test_one_row(api, n, heads, kv, d):
     k, v = draw(n + heads, n, kv, d)
     c = fill(api, k, v, kv, capacity=n + 70)
@@ -191,9 +191,9 @@ def test_many_columns(api, heads, kv, d, rows, n):
 
 def test_every_kernel_is_reached(api):
     """by the sizes above, with and without ranges"""
-    sizes = [(66, 5, 2, 2, 64), (200, 65, 2, 2, 64), (4000, 11, 3, 1, 64), (2063, 100, 4, 4, 128), (300, 140, 16, 16, 64)]
+    sizes = [(66, 5, 2, 2, 64), (257, 1, 4, 4, 128), (200, 65, 2, 2, 64), (4000, 11, 3, 1, 64), (2063, 100, 4, 4, 128), (300, 140, 16, 16, 64)]
     seen = {api.tl_k_attention_cache8_plan(*s, elems)[0] for s in sizes for elems in (0, 1 << 20)}
-    assert seen == {"columns16", "rows128", "rows256"}
+    assert seen == {"columns8", "columns16", "rows128", "rows256"}
 
 
 def test_ranges_with_nothing_to_see(api):
@@ -247,7 +247,7 @@ def test_scales_far_apart(api):
 
 
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
-@pytest.mark.parametrize("rows", [1, 20, 150])
+@pytest.mark.parametrize("rows", [1, 12, 20, 150])
 @pytest.mark.parametrize("where", ["values", "keys"])
 def test_values_that_are_not_finite(api, bad, rows, where):
     """rows that see them get what the formula gives; those that do not, and other heads, are as without them"""
