@@ -345,3 +345,108 @@ def test_captured_steps(api):
         torch.cuda.synchronize()
         assert torch.equal(out, eager)
         torch.mm(torch.randn(64, 64, device="cuda"), torch.randn(64, 64, device="cuda"))
+
+
+@pytest.mark.parametrize("rows", [1, 40])
+def test_offsets_beyond_32_bits(api, rows):
+    """2^31 bytes of codes and more lie before the last blocks"""
+    heads, d, n = 32, 128, (1 << 19) + 200
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("24 GB of device memory needed")
+    c = api.Cache8.empty(heads, d, n)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    for name, t in c.tensors.items():
+        if t.dtype == torch.int8:
+            t.random_(-127, 128, generator=g)
+        elif t.dtype == torch.float32:
+            t.fill_(0.01)
+    first = (1 << 19) - 64         # the last tokens come through append, over the 2^31-byte mark
+    k, v = draw(21, n - first, heads, d)
+    api.tl_k_cache8_append(c, first, k.cuda(), v.cuda())
+    for x, got in zip((k, v), read(api, c, n, first, n - first)):
+        assert same(got.view(-1, heads, d), oracle.held(x, heads)[0])
+    q = queries(9, rows, heads * d) * 0.3
+    q = q.bfloat16()
+    o = torch.full((rows, heads * d), math.nan, dtype=torch.bfloat16, device="cuda")
+    api.tl_k_attention_cache8(c, n, q.cuda(), o, heads, torch.empty(1 << 22, device="cuda"))
+    full = n // 64
+    for h in (0, 31):
+        kh = (c.tensors["k"][:full, h].double() * c.tensors["k_scale"][:full, h].double()[:, None, None, None]).transpose(1, 2).reshape(-1, d)
+        vh = (c.tensors["v"][:full, h].double() * c.tensors["v_scale"][:full, h].double()[:, None, None]).transpose(1, 2).reshape(-1, d)
+        kh = torch.cat([kh, k[-(n - 64 * full):].view(-1, heads, d)[:, h].double().cuda()])
+        vh = torch.cat([vh, v[-(n - 64 * full):].view(-1, heads, d)[:, h].double().cuda()])
+        for i in {0, rows - 1}:
+            see = n - rows + i + 1
+            qi = q[i].view(heads, d)[h].double().cuda()
+            p = torch.softmax(kh[:see] @ qi / math.sqrt(d), 0)
+            want, size = p @ vh[:see], p @ vh[:see].abs()
+            reach = (kh[:see].abs() @ qi.abs()).max() / math.sqrt(d)
+            far = (o[i].view(heads, d)[h].double() - want).abs() - oracle.attention_bound(want, size, reach, d, n, BF16)
+            assert far.max() <= 0, (h, i, far.max())
+
+
+def test_two_streams_at_once(api):
+    """calls on two streams, each with its cache and workspace, and a stream given by its handle"""
+    heads, d, n = 8, 128, 2000
+    sets = []
+    for i in range(2):
+        k, v = draw(30 + i, n, heads, d)
+        q1, q2 = queries(31 + i, 1, heads * d).cuda(), queries(33 + i, 100, heads * d).cuda()
+        c = fill(api, k, v, heads)
+        ws = torch.empty(1 << 21, device="cuda")
+        want = []
+        for q in (q1, q2):
+            o = torch.empty_like(q)
+            api.tl_k_attention_cache8(c, n, q, o, heads, ws)
+            want.append(o)
+        sets.append((c, q1, q2, ws, want, torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        got = [(torch.empty_like(q1), torch.empty_like(q2)) for _, q1, q2, *_ in sets]
+        torch.cuda.synchronize()
+        for (c, q1, q2, ws, _, s), (o1, o2) in zip(sets, got):
+            api.tl_k_attention_cache8(c, n, q1, o1, heads, ws, stream=s.cuda_stream)
+            api.tl_k_attention_cache8(c, n, q2, o2, heads, ws, stream=s.cuda_stream)
+        torch.cuda.synchronize()
+        for (_, _, _, _, want, _), (o1, o2) in zip(sets, got):
+            assert torch.equal(o1, want[0]) and torch.equal(o2, want[1])
+
+
+@pytest.mark.parametrize("rows,heads,kv", [(1, 4, 4), (30, 4, 2), (300, 16, 16)])
+def test_captured_attention(api, rows, heads, kv):
+    """each kind of kernel, in a graph that is replayed between eager work on the same buffers"""
+    d, n = 64, 1000
+    k, v = draw(40, n, kv, d)
+    c = fill(api, k, v, kv)
+    q = queries(10, rows, heads * d).cuda()
+    o, ws = torch.empty_like(q), torch.empty(1 << 21, device="cuda")
+    g, s = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    api.tl_k_attention_cache8(c, n, q, o, heads, ws)
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s), torch.cuda.graph(g, stream=s):
+        api.tl_k_attention_cache8(c, n, q, o, heads, ws)
+    torch.cuda.current_stream().wait_stream(s)
+    for i in range(3):
+        q.copy_(queries(11 + i, rows, heads * d))
+        api.tl_k_attention_cache8(c, n, q, o, heads, ws)
+        want = o.clone()
+        o.zero_(), ws.fill_(math.nan)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(o, want)
+
+
+def test_rows_behind_the_last_are_left_alone(api):
+    heads, d, n = 2, 64, 130
+    k, v = draw(41, n, heads, d)
+    c = fill(api, k, v, heads, capacity=300)
+    before = {name: t.clone() for name, t in c.tensors.items()}
+    api.tl_k_attention_cache8(c, n, queries(12, 5, heads * d).cuda(), torch.empty(5, heads * d, dtype=torch.bfloat16, device="cuda"), heads)
+    for name, t in c.tensors.items():
+        assert torch.equal(t.view(torch.uint8), before[name].view(torch.uint8)), name
+    x, y = draw(42, 3, heads, d)
+    api.tl_k_cache8_append(c, n, x.cuda(), y.cuda())
+    for name in ("k", "v", "k_scale", "v_scale"):          # no block was completed
+        assert torch.equal(c.tensors[name].view(torch.uint8), before[name].view(torch.uint8)), name
+    kt = c.tensors["k_tail"].view(torch.int16)
+    assert torch.equal(kt[:, :, 5:], before["k_tail"].view(torch.int16)[:, :, 5:]) and torch.equal(kt[:, :, :2], before["k_tail"].view(torch.int16)[:, :, :2])

@@ -19,7 +19,8 @@ def gen(seed):
     return torch.Generator().manual_seed(seed)
 
 
-@pytest.mark.parametrize("rows,n,vocab", [(1, 0, 5), (1, 1, 1), (1, 5000, 32000), (3, 77, 8192), (5, 300, 8193), (2, 1000, 50001), (130, 65, 100)])
+@pytest.mark.parametrize("rows,n,vocab", [(1, 0, 5), (1, 1, 1), (1, 5000, 32000), (3, 77, 8192), (5, 300, 8193), (2, 1000, 50001), (130, 65, 100),
+                                          (64, 4500, 33000), (300, 70, 500), (1, 30000, 9000)])
 def test_counts(api, rows, n, vocab):
     tok = torch.randint(-3, vocab + 3, (rows, n), generator=gen(n + vocab), dtype=torch.int32)
     if n > 4:
@@ -90,7 +91,7 @@ def check(api, logits, counts, bias, allowed, rep, pres, freq, workspace):
             assert c == int((ok & (got[r] == top)).nonzero()[0]), r
 
 
-@pytest.mark.parametrize("rows,vocab", [(1, 1), (1, 31), (1, 33), (1, 1000), (1, 32000), (3, 2048), (3, 2049), (40, 5003), (200, 776)])
+@pytest.mark.parametrize("rows,vocab", [(1, 1), (1, 31), (1, 33), (1, 1000), (1, 32000), (3, 2048), (3, 2049), (40, 5003), (200, 776), (20, 32000), (17, 40001)])
 @pytest.mark.parametrize("shared", [False, True])
 def test_choose(api, rows, vocab, shared):
     logits, counts, bias, allowed = inputs(rows, vocab, rows * vocab, shared)
