@@ -466,7 +466,7 @@ tl_status tl_k_argmax(const float* x, int32_t n, int32_t* out, void* hip_stream)
  *   v      : int8 [n_blocks][n_kv_heads][d_head][64 tokens]
  *   scales : fp32 [n_blocks][n_kv_heads]
  *   tails  : bf16, laid out as one block of k and of v
- * d_head 64 or 128.  The number of tokens cached (n_cached, n_keys) is the caller's to keep: append does not store it.
+ * d_head 64 or 128, up to 4096 heads, capacity up to 2^30.  The number of tokens cached (n_cached, n_keys) is the caller's to keep: append does not store it.
  */
 typedef struct {
     int8_t *k, *v;
@@ -484,7 +484,7 @@ tl_status tl_k_cache8_read(const tl_cache8_mem* cache, int32_t n_cached, int32_t
                            int32_t ldv, void* hip_stream);
 /* Causal attention of the last n_rows of n_keys cached tokens (one row: a decoding step): row i of q (bf16 [n_rows, n_heads * d_head]) sees
  * keys 0 .. n_keys - n_rows + i;  o = softmax(q K^T / sqrt(d_head)) V, bf16, K and V what the cache stands for.  n_heads is a multiple
- * of n_kv_heads; query head j reads key head j / (n_heads / n_kv_heads).  n_rows <= n_keys.
+ * of n_kv_heads; query head j reads key head j / (n_heads / n_kv_heads).  n_rows <= n_keys, n_rows * n_heads <= 2^24.
  * workspace: NULL, or device fp32 scratch of workspace_elems floats: with it the keys are cut into up to 64 ranges where the rows are few,
  * n_rows * n_heads * ranges * (d_head + 2) floats are used; contents are undefined before and after, and calls that overlap in time need one
  * each.  tl_k_attention_cache8_plan: the name of the kernel that these sizes get ("columns16", "columns8", "rows128" or "rows256"), its ranges and the floats that it uses of a
@@ -495,7 +495,7 @@ tl_status tl_k_attention_cache8_plan(int32_t n_keys, int32_t n_rows, int32_t n_h
                                      size_t workspace_elems, char* name_out, size_t name_cap, int32_t* n_ranges_out, size_t* elems_out);
 /* How often each token of the vocabulary is in a row of a text: tokens device int32 [rows, n] (row stride ldt), counts device int32
  * [rows, vocab] (row stride ldc).  add = 0: counts are set; add = 1: added to; add = -1: taken away from (a history that slides).  Ids
- * outside [0, vocab) are passed over, so rows of different lengths are filled up with -1. */
+ * outside [0, vocab) are passed over, so rows of different lengths are filled up with -1.  n and vocab up to 2^30. */
 tl_status tl_k_token_counts(const int32_t* tokens, int32_t ldt, int32_t rows, int32_t n, int32_t vocab, int32_t add, int32_t* counts,
                             int32_t ldc, void* hip_stream);
 /* Penalties, a bias and a mask on logits (fp32 [rows, vocab]), and the greedy choice:  for a token with count > 0

@@ -1805,12 +1805,14 @@ extern "C" tl_status tl_k_argmax(const float* x, int32_t n, int32_t* out, void* 
     HIPCHK(launch_argmax(x, n, out, (hipStream_t)hip_stream));
     return TL_OK;
 }
+// positions, ids and lengths of these calls stay below 2^30, so that no index of 32 bits passes its range
+static constexpr int32_t kMost = 1 << 30;
 // what every call on a cache needs of it
 static tl_status cache8_of(const tl_cache8_mem* m, const char* name, Cache8* out) {
     if (!m || !m->k || !m->v || !m->k_scale || !m->v_scale || !m->k_tail || !m->v_tail) return fail(TL_ERR_ARG, "%s: null pointer", name);
     if (((uintptr_t)m->k | (uintptr_t)m->v | (uintptr_t)m->k_tail | (uintptr_t)m->v_tail) & 15)
         return fail(TL_ERR_ARG, "%s: codes and tails start at multiples of 16 bytes", name);
-    if (m->n_kv_heads < 1 || m->n_kv_heads > 4096 || (m->d_head != 64 && m->d_head != 128) || m->capacity < 1)
+    if (m->n_kv_heads < 1 || m->n_kv_heads > 4096 || (m->d_head != 64 && m->d_head != 128) || m->capacity < 1 || m->capacity > kMost)
         return fail(TL_ERR_ARG, "%s: %d heads of %d, capacity %d", name, m->n_kv_heads, m->d_head, m->capacity);
     *out = Cache8{m->k, m->v, m->k_scale, m->v_scale, m->k_tail, m->v_tail, m->n_kv_heads, m->d_head};
     return TL_OK;
@@ -1850,7 +1852,7 @@ extern "C" tl_status tl_k_attention_cache8(const tl_cache8_mem* cache, int32_t n
 extern "C" tl_status tl_k_attention_cache8_plan(int32_t n_keys, int32_t n_rows, int32_t n_heads, int32_t n_kv_heads, int32_t d_head,
                                                 size_t workspace_elems, char* name_out, size_t name_cap, int32_t* n_ranges_out,
                                                 size_t* elems_out) {
-    KARGS_OK(name_out && name_cap > 0 && n_ranges_out && elems_out && n_keys >= 1 && n_rows >= 1 && n_rows <= n_keys && n_kv_heads >= 1 &&
+    KARGS_OK(name_out && name_cap > 0 && n_ranges_out && elems_out && n_keys >= 1 && n_keys <= kMost && n_rows >= 1 && n_rows <= n_keys && n_kv_heads >= 1 &&
                  n_kv_heads <= 4096 && n_heads >= 1 && n_heads <= 65536 && n_heads % n_kv_heads == 0 && (int64_t)n_rows * n_heads <= 1 << 24 &&
                  (d_head == 64 || d_head == 128), "tl_k_attention_cache8_plan");
     int n = 1;
@@ -1861,7 +1863,7 @@ extern "C" tl_status tl_k_attention_cache8_plan(int32_t n_keys, int32_t n_rows, 
 }
 extern "C" tl_status tl_k_token_counts(const int32_t* tokens, int32_t ldt, int32_t rows, int32_t n, int32_t vocab, int32_t add, int32_t* counts,
                                        int32_t ldc, void* hip_stream) {
-    KARGS_OK((tokens || n == 0 || rows == 0) && (counts || rows == 0) && rows >= 0 && n >= 0 && vocab >= 1 && add >= -1 && add <= 1 &&
+    KARGS_OK((tokens || n == 0 || rows == 0) && (counts || rows == 0) && rows >= 0 && n >= 0 && n <= kMost && vocab >= 1 && vocab <= kMost && add >= -1 && add <= 1 &&
                  (rows <= 1 || (ldt >= n && ldc >= vocab)), "tl_k_token_counts");
     HIPCHK(launch_token_counts(tokens, ldt, rows, n, vocab, add, counts, ldc, (hipStream_t)hip_stream));
     return TL_OK;
@@ -1871,7 +1873,7 @@ extern "C" tl_status tl_k_choose(const float* logits, int32_t ldl, int32_t rows,
                                  int32_t lda, float* out, int32_t ldo, int32_t* choice, float* workspace, size_t workspace_elems,
                                  void* hip_stream) {
     auto row = [&](int32_t ld, int32_t n) { return rows <= 1 || ld == 0 || ld >= n; };      // 0: one row for all
-    KARGS_OK((logits || rows == 0) && rows >= 0 && vocab >= 1 && (rows <= 1 || (ldl >= vocab && (!out || ldo >= vocab))) && (!counts || row(ldc, vocab)) &&
+    KARGS_OK((logits || rows == 0) && rows >= 0 && vocab >= 1 && vocab <= kMost && (rows <= 1 || (ldl >= vocab && (!out || ldo >= vocab))) && (!counts || row(ldc, vocab)) &&
                  (!bias || row(ldb, vocab)) && (!allowed || row(lda, cdiv(vocab, 32))) && (out != logits || rows <= 1 || ldo == ldl),
              "tl_k_choose");
     if (!(repetition > 0.f) || !std::isfinite(repetition) || !std::isfinite(presence) || !std::isfinite(frequency))

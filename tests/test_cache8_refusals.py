@@ -22,7 +22,7 @@ def mem(api, **change):
 
 P = C.c_void_p(1 << 20)
 BAD_MEM = [dict(k=0), dict(v=0), dict(k_scale=0), dict(v_scale=0), dict(k_tail=0), dict(v_tail=0), dict(k=8), dict(v=24), dict(k_tail=2), dict(v_tail=4),
-           dict(n_kv_heads=0), dict(n_kv_heads=-1), dict(n_kv_heads=5000), dict(d_head=96), dict(d_head=0), dict(capacity=0)]
+           dict(n_kv_heads=0), dict(n_kv_heads=-1), dict(n_kv_heads=5000), dict(d_head=96), dict(d_head=0), dict(capacity=0), dict(capacity=2 ** 30 + 1), dict(capacity=-5)]
 
 
 @pytest.mark.parametrize("change", BAD_MEM)
@@ -63,7 +63,7 @@ def test_attention(api, n_keys, q, ldq, rows, heads, o, ldo, status):
     assert api._lib.tl_k_attention_cache8(C.byref(mem(api)), n_keys, q, ldq, rows, heads, o, ldo, None, 0, None) == status
 
 
-@pytest.mark.parametrize("args", [(0, 1, 2, 2, 64), (5, 6, 2, 2, 64), (5, 0, 2, 2, 64), (5, 1, 3, 2, 64), (5, 1, 2, 0, 64), (5, 1, 2, 2, 80)])
+@pytest.mark.parametrize("args", [(0, 1, 2, 2, 64), (2 ** 30 + 1, 1, 2, 2, 64), (5, 6, 2, 2, 64), (5, 0, 2, 2, 64), (5, 1, 3, 2, 64), (5, 1, 2, 0, 64), (5, 1, 2, 2, 80)])
 def test_plan(api, args):
     with pytest.raises(api.TlError):
         api.tl_k_attention_cache8_plan(*args)
@@ -82,7 +82,8 @@ def test_plan_stays_within_the_workspace(api):
 
 @pytest.mark.parametrize("tokens,ldt,rows,n,vocab,add,counts,ldc", [
     (None, 4, 1, 4, 10, 0, P, 10), (P, 4, 1, 4, 10, 0, None, 10), (P, 4, -1, 4, 10, 0, P, 10), (P, 4, 1, -4, 10, 0, P, 10), (P, 4, 1, 4, 0, 0, P, 10),
-    (P, 4, 1, 4, 10, 2, P, 10), (P, 4, 1, 4, 10, -2, P, 10), (P, 3, 2, 4, 10, 0, P, 10), (P, 4, 2, 4, 10, 0, P, 9)])
+    (P, 4, 1, 4, 10, 2, P, 10), (P, 4, 1, 4, 10, -2, P, 10), (P, 3, 2, 4, 10, 0, P, 10), (P, 4, 2, 4, 10, 0, P, 9),
+    (P, 4, 1, 2 ** 30 + 1, 10, 0, P, 10), (P, 4, 1, 4, 2 ** 30 + 1, 0, P, 10)])
 def test_counts(api, tokens, ldt, rows, n, vocab, add, counts, ldc):
     assert api._lib.tl_k_token_counts(tokens, ldt, rows, n, vocab, add, counts, ldc, None) == ARG
 
@@ -92,7 +93,7 @@ GOOD = dict(logits=P, ldl=40, rows=2, vocab=40, counts=P, ldc=40, repetition=1.0
 
 
 @pytest.mark.parametrize("change", [
-    dict(logits=None), dict(ldl=39), dict(rows=-1), dict(vocab=0), dict(ldc=39), dict(ldb=39), dict(lda=1), dict(ldo=39), dict(ldo=0), dict(ldl=41),
+    dict(logits=None), dict(ldl=39), dict(rows=-1), dict(vocab=0), dict(vocab=2 ** 30 + 1, rows=1), dict(ldc=39), dict(ldb=39), dict(lda=1), dict(ldo=39), dict(ldo=0), dict(ldl=41),
     dict(repetition=0.0), dict(repetition=-1.0), dict(repetition=float("nan")), dict(repetition=float("inf")), dict(presence=float("nan")),
     dict(frequency=float("inf"))])
 def test_choose(api, change):
