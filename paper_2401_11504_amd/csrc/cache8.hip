@@ -35,6 +35,8 @@ constexpr int VP = 17;      // words of a value row (64 codes) in LDS: odd, so t
 
 // One workgroup for a block that the new tokens complete and a head's keys or values (block by block, the heads' keys before their
 // values).  Those of the first block also put the rows behind the last complete block into the tail, after they have read the tail.
+// Values are turned round through LDS, as codes, four tokens to a word.  Bytes bound it from some 10^4 tokens of 32 heads of 128 on (32768: 177 us, 4.6
+// TB/s in and out); 333 tokens take 6.2 us, one 2.5: two round trips to memory.
 template <int D>
 __global__ __launch_bounds__(2 * D) void cache8_append_kernel(Cache8 c, int n_cached, const bf16_t* __restrict__ k, long ldk,
                                                               const bf16_t* __restrict__ v, long ldv, int n_new) {
@@ -173,7 +175,8 @@ hipError_t launch_cache8_append(const Cache8& c, int n_cached, const bf16_t* k, 
 }
 
 // Tokens first .. first + n - 1 of a cache that holds n_cached as fp32 rows: code * scale (one rounding), the tail's widened.  A thread
-// writes 4 columns of a row at a time; values are turned round through LDS, as codes.
+// writes 4 columns of a row at a time, past the caches; values are turned round through LDS, as codes.  Bytes bound it: 32768 tokens of 32 heads of
+// 128 228 us, 5.9 TB/s in and out (ordinary stores 242; column pairs straight from memory 620).
 template <int D>
 __global__ __launch_bounds__(2 * D) void cache8_read_kernel(Cache8 c, int n_cached, int first, int n, float* __restrict__ k, long ldk,
                                                             float* __restrict__ v, long ldv) {
@@ -189,7 +192,7 @@ __global__ __launch_bounds__(2 * D) void cache8_read_kernel(Cache8 c, int n_cach
     const long ld = values ? ldv : ldk;
     auto put = [&](int t, float a, float b, float e, float f) {
         const int row = row0 + t;
-        if (row >= 0 && row < n) *(float4*)(out + (long)row * ld) = make_float4(a, b, e, f);
+        if (row >= 0 && row < n) __builtin_nontemporal_store(f32x4_t{a, b, e, f}, (f32x4_t*)(out + (long)row * ld));
     };
     if (in_tail) {
         for (int t = t0; t < 64; t += 8) {
