@@ -747,26 +747,26 @@ static constexpr size_t attn8_rows_lds() {
 //   columns16, columns8  up to 16 columns of a key head: four waves for 16 columns, or eight for 8 that share the blocks of a range.  us for 2 rows of 32
 //                     heads of 128, this and rows128: 300 keys 8.2 and 8.1, 1500 9.5 and 12.5, 4000 12.2 and 18.6; 17 rows: 300 keys 10.2 and 8.7,
 //                     1500 13.3 and 13.2, 4000 19.1 and 15.5
-//   rows128, rows256  more columns: 256 to a workgroup where that leaves 16 workgroups or more for a range of the keys (2048 rows of 32 heads over 8192
-//                     keys 257; 200 rows, 4000 keys, 128 and 256: 32 heads 37.2 and 34.5, 4 heads 16.7 and 19.0)
+//   rows128, rows256  more columns, 128 or 256 to a workgroup (both, 32 heads: 2048 rows, 8192 keys 283 and 262; 1024 rows, 1024 keys 29 and 34; 200 rows,
+//                     4000 keys in 8 ranges 37.2 and 34.5; 200 rows of 4 heads in 16 16.7 and 19.0)
 // Ranges of few columns: none up to 11 blocks, from 5 on with eight waves (one row of 32 heads, 500 keys: 7.8 with four waves, 7.5 with eight, 8.0 cut; 700
 // keys 10.1, 8.4, 8.2 and a launch more; 1000 keys 12.4, 11.9, 8.3).  Else two workgroups a CU, of three blocks or more, but one a CU where each has over
 // 16 blocks (32768 keys of 32 heads 50.9 and 48.2).  Where that is over 16 ranges (few key heads), 16 of up to four blocks
 // (4000 keys of 8 heads: 16 8.9, 21 9.9) or 32 of eight waves (16000 keys of 8 heads: 64 of four
 // waves 14.4, 32 of eight 12.3), from 512 blocks on as many as leave a workgroup for each CU (65536 keys of 2 heads: 32 21.8, 64 16.4; 8000 keys of one: 32
 // 9.1, 42 10.3).
-// Ranges, rows: what costs least of a launch's tiles one after another (1.75 us each with one workgroup of 128 columns on a CU, 2.7 with two; 2.3 of 256
-// columns) and of the join (3 us, and its floats written and read at 3.5 TB/s).
+// Many columns: the workgroup and the ranges that cost least of a launch's tiles one after another (1.75 us each with one workgroup of 128 columns on a
+// CU, 2.7 with two; 2.3 of 256 columns) and of the join (3 us, and its floats written and read at 3.5 TB/s).
 struct Attn8Plan { int cols, waves, n_split, per; };       // columns and waves a workgroup, ranges, blocks a range
 static Attn8Plan attn8_plan(int n_keys, int n_rows, int heads, int kv_heads, int d, size_t ws_elems) {
     const int nb = cdiv(n_keys, 64);
     const long n_cols = (long)n_rows * (heads / kv_heads);
-    const int cols = n_cols <= 16 ? 16 : n_cols <= 128 || kv_heads * (long)cdiv(n_cols, 256) < 16 ? 128 : 256;
-    const long units = kv_heads * (long)cdiv(n_cols, cols), range_elems = (long)n_rows * heads * (d + 2);
+    const long range_elems = (long)n_rows * heads * (d + 2);
     const long most = std::min<long>(std::min<long>(nb, ATTN8_MAX_SPLIT), (long)(ws_elems / (size_t)range_elems));
     long n = 1;
-    int waves = cols == 16 ? 4 : cols / 32;
-    if (cols == 16) {
+    int cols = 16, waves = 4;
+    if (n_cols <= 16) {
+        const long units = kv_heads;
         if (nb > 11) {
             n = std::min<long>(512 / units, cdiv(nb, 3));
             if (n > 16 && nb <= 64) n = 16;
@@ -778,13 +778,18 @@ static Attn8Plan attn8_plan(int n_keys, int n_rows, int heads, int kv_heads, int
         n = std::min(n, most);
         if (n < 2 && nb > 4 && n_cols <= 8) waves = 8;
     } else {
-        auto cost = [&](long r) {
-            const long w = units * r, slots = cols == 128 ? 512 : 256, rest = w % slots;
-            const double tile = cols == 128 ? 2.7 : 2.3, last = rest == 0 ? 0. : cols == 128 && rest <= 256 ? 1.75 : tile;
-            return cdiv(nb, r) * ((double)(w / slots) * tile + last) + (r > 1 ? 3. + 8. * r * range_elems / 3.5e6 : 0.);
-        };
-        for (long r = 2; r <= most; ++r)
-            if (cost(r) < cost(n)) n = r;
+        double best = 0.;
+        for (int c : {128, 256}) {
+            if (c > 128 && n_cols <= 128) break;
+            const long units = kv_heads * (long)cdiv(n_cols, c), slots = c == 128 ? 512 : 256;
+            for (long r = 1; r == 1 || r <= most; ++r) {
+                const long w = units * r, rest = w % slots;
+                const double tile = c == 128 ? 2.7 : 2.3, last = rest == 0 ? 0. : c == 128 && rest <= 256 ? 1.75 : tile;
+                const double cost = cdiv(nb, r) * ((double)(w / slots) * tile + last) + (r > 1 ? 3. + 8. * r * range_elems / 3.5e6 : 0.);
+                if ((c == 128 && r == 1) || cost < best) best = cost, cols = c, n = r;
+            }
+        }
+        waves = cols / 32;
     }
     if (n < 2) return {cols, waves, 1, nb};
     const int per = cdiv(nb, n);

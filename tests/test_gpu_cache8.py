@@ -189,10 +189,31 @@ def test_many_columns(api, heads, kv, d, rows, n):
         check(api, c, n, k, v, q, heads, kv, ws)
 
 
+WIDE = [(600, 520, 64, 64, 64), (1000, 600, 32, 32, 64), (600, 520, 64, 64, 128), (1300, 260, 32, 32, 128)]     # keys, rows, heads, key heads, d
+
+
+@pytest.mark.parametrize("n,rows,heads,kv,d", WIDE)
+@pytest.mark.parametrize("elems", [0, 1 << 22])
+def test_many_columns_of_many_heads(api, n, rows, heads, kv, d, elems):
+    k, v = draw(n + rows, n, kv, d)
+    c = fill(api, k, v, kv, capacity=n + 1)
+    q = queries(n, rows, heads * d)
+    got = attend(api, c, n, q, heads, torch.full((elems,), math.nan, device="cuda") if elems else None).double().view(rows, heads, d).cuda()
+    kh, vh = (oracle.held(x, kv)[0].double().cuda().transpose(0, 1) for x in (k, v))
+    later = torch.arange(n, device="cuda")[None] > torch.arange(rows, device="cuda")[:, None] + n - rows
+    for h in range(heads):
+        qh = q.view(rows, heads, d)[:, h].double().cuda()
+        p = torch.softmax((qh @ kh[h].T / math.sqrt(d)).masked_fill(later, -math.inf), 1)
+        want, size = p @ vh[h], p @ vh[h].abs()
+        reach = (qh.abs() @ kh[h].abs().T).amax(1, keepdim=True) / math.sqrt(d)
+        far = (got[:, h] - want).abs() - oracle.attention_bound(want, size, reach, d, n, BF16)
+        assert far.max() <= 0, (h, far.max())
+
+
 def test_every_kernel_is_reached(api):
     """by the sizes above, with and without ranges"""
-    sizes = [(66, 5, 2, 2, 64), (257, 1, 4, 4, 128), (200, 65, 2, 2, 64), (4000, 11, 3, 1, 64), (2063, 100, 4, 4, 128), (300, 140, 16, 16, 64)]
-    seen = {api.tl_k_attention_cache8_plan(*s, elems)[0] for s in sizes for elems in (0, 1 << 20)}
+    sizes = [(66, 5, 2, 2, 64), (257, 1, 4, 4, 128), (200, 65, 2, 2, 64), (4000, 11, 3, 1, 64), (2063, 100, 4, 4, 128), WIDE[0], WIDE[1]]
+    seen = {api.tl_k_attention_cache8_plan(*s, elems)[0] for s in sizes for elems in (0, 1 << 20, 1 << 22)}
     assert seen == {"columns8", "columns16", "rows128", "rows256"}
 
 
@@ -450,3 +471,25 @@ def test_rows_behind_the_last_are_left_alone(api):
         assert torch.equal(c.tensors[name].view(torch.uint8), before[name].view(torch.uint8)), name
     kt = c.tensors["k_tail"].view(torch.int16)
     assert torch.equal(kt[:, :, 5:], before["k_tail"].view(torch.int16)[:, :, 5:]) and torch.equal(kt[:, :, :2], before["k_tail"].view(torch.int16)[:, :, :2])
+
+
+def test_values_that_are_not_finite_in_wide_workgroups(api):
+    n, rows, heads, _, d = WIDE[0]
+    assert api.tl_k_attention_cache8_plan(n, rows, heads, heads, d)[0] == "rows256"
+    k, v = draw(50, n, heads, d, big=1.0)
+    q = queries(51, rows, heads * d)
+    clean = attend(api, fill(api, k, v, heads), n, q, heads).view(rows, heads, d)
+    v[590, 9] = math.inf               # head 0, the tail (tokens 576 ..)
+    v[300, d + 3] = math.nan           # head 1, block 4
+    got = attend(api, fill(api, k, v, heads), n, q, heads).view(rows, heads, d)
+    at = torch.arange(rows) + n - rows
+    assert torch.equal(got[:, 2:], clean[:, 2:])
+    assert torch.isnan(got[at >= 256, 1]).all() and torch.equal(got[at < 256, 1], clean[at < 256, 1])
+    assert (got[at >= 590, 0, 9] == math.inf).all()
+    assert torch.equal(got[at < 576, 0], clean[at < 576, 0])
+    rest = [e for e in range(d) if e != 9]
+    # the same probabilities, as rounded, times the same values, summed in another order, and rounded to bf16: half a step of either
+    size = v.view(n, heads, d)[:576, 0].float().abs().max()
+    far = (got[:, 0].float() - clean[:, 0].float()).abs()
+    bound = 2.0 ** -7 * clean[:, 0].float().abs() + 600 * 2.0 ** -23 * size
+    assert (far[:, rest] <= bound[:, rest]).all() and (far[at < 590] <= bound[at < 590]).all()
