@@ -540,6 +540,8 @@ template <int D>
 __device__ __forceinline__ unsigned k_piece_at(int key, int c) { return key * D * 2 + ((c ^ (D == 128 ? key & 15 : key >> 1 & 7)) << 4); }
 __device__ __forceinline__ unsigned v_piece_at(int d, int c) { return d * 128 + ((c ^ (d >> 1 & 7)) << 4); }
 
+constexpr int ATTN8_ONE_ROUND = 256;                         // workgroups of eight waves that run at once, one a CU
+
 template <int D, int NC>
 __global__ __launch_bounds__(NC * 64, 2) void attn8_rows_kernel(Cache8 c, int n_keys, const bf16_t* __restrict__ q, long ldq, int n_rows, int group,
                                                              float scale_log2e, bf16_t* __restrict__ o, long ldo, float* __restrict__ ws,
@@ -548,13 +550,17 @@ __global__ __launch_bounds__(NC * 64, 2) void attn8_rows_kernel(Cache8 c, int n_
     constexpr int TB = 64 * D * 2, STAGE = 2 * TB + 16;                                        // a tile's bytes in LDS, K, V and scales
     extern __shared__ __align__(16) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, g = lane >> 5;
-    // the last columns see most: they come first, every head's before any head's second; a head's workgroups are a multiple of
-    // c.heads apart, on one XCD if that is a multiple of eight
-    const int n_cols = n_rows * group, heads = c.heads * group, n_blocks = (n_cols + 32 * NC - 1) / (32 * NC);
-    const int head = blockIdx.x % c.heads, rest = blockIdx.x / c.heads;
-    const int c0 = (n_blocks - 1 - rest % n_blocks) * 32 * NC, split = rest / n_blocks;
-    const int w0 = c0 + 32 * wave, col = min(w0 + l32, n_cols - 1), row = col / group, seen = n_keys - n_rows + row + 1;
-    const int most = n_keys - n_rows + min(c0 + 32 * NC - 1, n_cols - 1) / group + 1;          // keys that the block's last column sees
+    // The last columns see most.  Workgroups that all run at once take 128 columns from the end (waves 0 to 3) and as many from the front (4 to 7, on the
+    // same SIMDs), so that one has about as much to do as another: 2048 rows of 32 heads and 8192 keys 257 -> 246 us, 2048 keys 63.6 -> 50.9.  Of more, one after
+    // another on a CU, those of the last columns come first (4096 rows and keys 146, in pairs 162), as do those of four waves.  A head's workgroups
+    // are a multiple of c.heads apart, on one XCD if that is a multiple of eight.
+    const bool paired = NC == 8 && gridDim.x <= ATTN8_ONE_ROUND;
+    const int n_cols = n_rows * group, heads = c.heads * group, n_parts = (n_cols + 127) / 128, n_blocks = (n_cols + 32 * NC - 1) / (32 * NC);
+    const int head = blockIdx.x % c.heads, rest = blockIdx.x / c.heads, split = rest / n_blocks, at = rest % n_blocks;
+    const int c0 = (paired ? n_parts - 1 - at : (n_blocks - 1 - at) * (NC / 4)) * 128;         // of waves 0 to 3
+    const int w0 = !paired || wave < 4 ? c0 + 32 * wave : 128 * at < c0 ? 128 * at + 32 * (wave - 4) : n_cols;
+    const int col = min(w0 + l32, n_cols - 1), row = col / group, seen = n_keys - n_rows + row + 1;
+    const int most = n_keys - n_rows + min(c0 + (paired ? 127 : 32 * NC - 1), n_cols - 1) / group + 1;          // keys that the block's last column sees
     const int w_most = w0 < n_cols ? n_keys - n_rows + min(w0 + 31, n_cols - 1) / group + 1 : 0;     // the wave's
     const int w_least = n_keys - n_rows + w0 / group + 1;
     const int b_begin = split * blocks_per_split, b_end = min(b_begin + blocks_per_split, (most + 63) >> 6), b_tail = n_keys >> 6;
@@ -747,7 +753,7 @@ static constexpr size_t attn8_rows_lds() {
 //   columns16, columns8  up to 16 columns of a key head: four waves for 16 columns, or eight for 8 that share the blocks of a range.  us for 2 rows of 32
 //                     heads of 128, this and rows128: 300 keys 8.2 and 8.1, 1500 9.5 and 12.5, 4000 12.2 and 18.6; 17 rows: 300 keys 10.2 and 8.7,
 //                     1500 13.3 and 13.2, 4000 19.1 and 15.5
-//   rows128, rows256  more columns, 128 or 256 to a workgroup (both, 32 heads: 2048 rows, 8192 keys 283 and 262; 1024 rows, 1024 keys 29 and 34; 200 rows,
+//   rows128, rows256  more columns, 128 or 256 to a workgroup (both, 32 heads: 2048 rows of 8 key heads, 8192 keys 277 and 246; 1024 rows, 2048 keys 52 and 57; 200 rows,
 //                     4000 keys in 8 ranges 37.2 and 34.5; 200 rows of 4 heads in 16 16.7 and 19.0)
 // Ranges of few columns: none up to 11 blocks, from 5 on with eight waves (one row of 32 heads, 500 keys: 7.8 with four waves, 7.5 with eight, 8.0 cut; 700
 // keys 10.1, 8.4, 8.2 and a launch more; 1000 keys 12.4, 11.9, 8.3).  Else two workgroups a CU, of three blocks or more, but one a CU where each has over
@@ -756,7 +762,7 @@ static constexpr size_t attn8_rows_lds() {
 // waves 14.4, 32 of eight 12.3), from 512 blocks on as many as leave a workgroup for each CU (65536 keys of 2 heads: 32 21.8, 64 16.4; 8000 keys of one: 32
 // 9.1, 42 10.3).
 // Many columns: the workgroup and the ranges that cost least of a launch's tiles one after another (1.75 us each with one workgroup of 128 columns on a
-// CU, 2.7 with two; 2.3 of 256 columns) and of the join (3 us, and its floats written and read at 3.5 TB/s).
+// CU, 2.7 with two; 2.3 of 256 columns, 1.75 where half of them does not see the tile) and of the join (3 us, and its floats written and read at 3.5 TB/s).
 struct Attn8Plan { int cols, waves, n_split, per; };       // columns and waves a workgroup, ranges, blocks a range
 static Attn8Plan attn8_plan(int n_keys, int n_rows, int heads, int kv_heads, int d, size_t ws_elems) {
     const int nb = cdiv(n_keys, 64);
@@ -781,11 +787,12 @@ static Attn8Plan attn8_plan(int n_keys, int n_rows, int heads, int kv_heads, int
         double best = 0.;
         for (int c : {128, 256}) {
             if (c > 128 && n_cols <= 128) break;
-            const long units = kv_heads * (long)cdiv(n_cols, c), slots = c == 128 ? 512 : 256;
+            const long units = kv_heads * (long)cdiv(n_cols, c), slots = c == 128 ? 2 * ATTN8_ONE_ROUND : ATTN8_ONE_ROUND;
             for (long r = 1; r == 1 || r <= most; ++r) {
                 const long w = units * r, rest = w % slots;
-                const double tile = c == 128 ? 2.7 : 2.3, last = rest == 0 ? 0. : c == 128 && rest <= 256 ? 1.75 : tile;
-                const double cost = cdiv(nb, r) * ((double)(w / slots) * tile + last) + (r > 1 ? 3. + 8. * r * range_elems / 3.5e6 : 0.);
+                const double tile = c == 128 ? 2.7 : 2.3, last = rest == 0 ? 0. : c == 128 && rest <= ATTN8_ONE_ROUND ? 1.75 : tile;
+                double cost = cdiv(nb, r) * ((double)(w / slots) * tile + last) + (r > 1 ? 3. + 8. * r * range_elems / 3.5e6 : 0.);
+                if (c > 128 && w <= ATTN8_ONE_ROUND && r == 1) cost -= (2.3 - 1.75) * (n_rows / 64);      // (in pairs: half of the waves has as many fewer)
                 if ((c == 128 && r == 1) || cost < best) best = cost, cols = c, n = r;
             }
         }

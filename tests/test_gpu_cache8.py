@@ -189,7 +189,8 @@ def test_many_columns(api, heads, kv, d, rows, n):
         check(api, c, n, k, v, q, heads, kv, ws)
 
 
-WIDE = [(600, 520, 64, 64, 64), (1000, 600, 32, 32, 64), (600, 520, 64, 64, 128), (1300, 260, 32, 32, 128)]     # keys, rows, heads, key heads, d
+# keys, rows, heads, key heads, d; the last two are more workgroups than run at once
+WIDE = [(600, 520, 64, 64, 64), (1000, 600, 32, 32, 64), (600, 520, 64, 64, 128), (1300, 260, 32, 32, 128), (450, 390, 250, 250, 128), (600, 550, 160, 160, 64)]
 
 
 @pytest.mark.parametrize("n,rows,heads,kv,d", WIDE)
