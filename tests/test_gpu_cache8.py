@@ -494,3 +494,35 @@ def test_values_that_are_not_finite_in_wide_workgroups(api):
     far = (got[:, 0].float() - clean[:, 0].float()).abs()
     bound = 2.0 ** -7 * clean[:, 0].float().abs() + 600 * 2.0 ** -23 * size
     assert (far[:, rest] <= bound[:, rest]).all() and (far[at < 590] <= bound[at < 590]).all()
+
+
+@pytest.mark.parametrize("rows,heads,kv,n", [(1, 2, 2, 300), (1, 4, 2, 900), (12, 4, 4, 2000), (5, 6, 2, 130), (150, 2, 2, 400), (520, 64, 64, 600)])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_a_query_that_is_not_finite(api, rows, heads, kv, n, bad):
+    """is its own row and head's alone"""
+    d = 64
+    k, v = draw(60, n, kv, d)
+    c = fill(api, k, v, kv)
+    q = queries(61, rows, heads * d)
+    ws = torch.full((1 << 20,), math.nan, device="cuda")
+    clean = attend(api, c, n, q, heads, ws).view(rows, heads, d)
+    hit = torch.zeros(rows, heads, dtype=torch.bool)
+    for r, h in ((0, 0), (rows // 2, heads - 1), (rows - 1, heads // 2)):
+        q[r, h * d + 7] = bad
+        hit[r, h] = True
+    got = attend(api, c, n, q, heads, ws).view(rows, heads, d)
+    assert torch.equal(got[~hit], clean[~hit])
+    assert torch.isnan(got[hit]).all()             # infinities among its scores: above all others, of either sign, or times a zero code
+
+
+@pytest.mark.parametrize("n", [64, 128, 192, 193, 199])
+def test_fewer_keys_than_are_cached(api, n):
+    """a multiple of 64, or inside the tail"""
+    heads, d = 2, 64
+    k, v = draw(70, 200, heads, d)
+    c = fill(api, k, v, heads)
+    for rows in (1, 40):
+        check(api, c, n, k, v, queries(rows, rows, heads * d), heads, heads)
+    got = read(api, c, n, 1, n - 1)
+    for x, y in zip((k, v), got):
+        assert same(y.view(n - 1, heads, d), oracle.held(x, heads)[0][1:n])
