@@ -205,7 +205,7 @@ tl_status tl_discard(tl_lora* lora);
  * window, fills the cache, and returns in *next_token the greedy continuation (index of the largest last-position
  * logit; the lowest index wins among equal logits).  logits_out: host fp32[vocab] for the last position, or NULL.
  * tl_decode_step: appends `token` at position kv_length and returns the next greedy token (and its logits).
- * Errors: TL_ERR_ARG (null pointer; decode without a cache), TL_ERR_WINDOW (n_tokens out of range; cache full),
+ * Errors: TL_ERR_ARG (null pointer; decode without a cache; no token to choose, all logits being undefined), TL_ERR_WINDOW (n_tokens out of range; cache full),
  * TL_ERR_TOKEN_RANGE, TL_ERR_SHAPE (vocab = 0), TL_ERR_DISCARDED, TL_ERR_DEVICE.  Outputs written only on TL_OK. */
 tl_status tl_prefill(tl_lora* lora, const int32_t* tokens, int32_t n_tokens, int32_t* next_token, float* logits_out);
 tl_status tl_decode_step(tl_lora* lora, int32_t token, int32_t* next_token, float* logits_out);
@@ -265,8 +265,9 @@ tl_status tl_get_kv(tl_lora* lora, int32_t layer, int32_t first, int32_t n, floa
  *     x = x > 0 ? x / repetition : x * repetition;   x = x - (frequency * count + presence).      NULL: none.
  *   tl_set_bias     : host fp32 [vocab], copied, is added.      NULL: none.
  *   tl_set_allowed  : host uint32 [ceil(vocab / 32)], copied; a token whose bit (bit t % 32 of word t / 32) is 0 is not chosen.  NULL: every token
- *                     may be.  For a grammar: set before each step.  A step that finds no token to choose returns TL_ERR_ARG; a decode step can
- *                     then be made again with another mask.
+ *                     may be.  For a grammar: set before each step.
+ * A step that finds no token to choose (none is allowed, or the values of all allowed ones are undefined) returns TL_ERR_ARG, with any of this set or
+ * none: a decode step can then be made again, tl_prefill and tl_extend leave no cache.
  * They stay until they are set again.  Errors: TL_ERR_ARG, TL_ERR_SHAPE (vocab = 0), TL_ERR_DISCARDED, TL_ERR_OOM, TL_ERR_DEVICE.
  */
 typedef struct {

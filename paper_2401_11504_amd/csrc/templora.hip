@@ -1001,11 +1001,12 @@ static tl_status emit_next(tl_lora* L, const float* h_last, int n_text, int32_t*
     } else {
         HIPCHK(launch_argmax(L->logits, c.vocab, L->next_host, s));
     }
-    if (logits_out)
-        HIPCHK(hipMemcpyAsync(logits_out, L->logits, (size_t)c.vocab * sizeof(float), hipMemcpyDeviceToHost, s));
     HIPCHK(hipStreamSynchronize(s));
-    if (L->next_host[0] < 0) return fail(TL_ERR_ARG, "no token to choose: none is allowed, or the values of all allowed ones are undefined");
-    *next_token = L->next_host[0];
+    // (without a token to choose the argmax leaves its first index beyond the vocabulary, the choice -1)
+    const int next = L->next_host[0];
+    if (next < 0 || next >= c.vocab) return fail(TL_ERR_ARG, "no token to choose: none is allowed, or the values of all allowed ones are undefined");
+    if (logits_out) TLCHK(copy_out(L, logits_out, L->logits, c.vocab));
+    *next_token = next;
     return TL_OK;
 }
 
