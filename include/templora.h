@@ -244,13 +244,15 @@ tl_status tl_cache_reuse(tl_lora* lora, int32_t on);
 
 /* The cache in 8 bits, for long windows.  on != 0: keys and values move to buffers of their own (allocated on the first call: n_layers *
  * max_tokens * 2 d_model bytes and what belongs to them), held as tl_cache8_mem describes with n_heads heads; a cache that exists moves along.
- * tl_prefill fills it (the prompt's own attention works on its bf16 keys and values), tl_decode_step and tl_extend add to it and attend
- * to what it stands for once the new tokens are in.  Whether it survives training-side calls is tl_cache_reuse's to say, as for the bf16 cache.  on == 0
+ * tl_prefill fills it (the prompt's own attention works on its bf16 keys and values), tl_decode_step adds to it and attends to what it stands
+ * for once the new token is in, tl_extend adds to it as well.  Whether it survives training-side calls is tl_cache_reuse's to say, as for the bf16 cache.  on == 0
  * (the initial state): back to the bf16 cache; the cache is dropped.  Errors: TL_ERR_ARG, TL_ERR_DISCARDED, TL_ERR_OOM, TL_ERR_DEVICE. */
 tl_status tl_cache_8bit(tl_lora* lora, int32_t on);
 
-/* n_tokens given tokens at once behind the kv_length cached ones (a text that goes on as it stands, a draft to be checked): what as many
- * tl_decode_step calls would leave in the cache, to within rounding, in one forward pass.  Returns the next token behind the last, as tl_decode_step.
+/* n_tokens given tokens at once behind the kv_length cached ones (a text that goes on as it stands), in one forward pass.  They attend to the blocks
+ * that were complete before the call as the cache holds them, to the tokens behind those and to one another as bf16, as a prompt's tokens do: no token
+ * has part in what those before it become.  (Steps see a block of the new tokens as codes once it is complete; what either way leaves in the cache
+ * differs by that, half a code of an element in what is attended to, and by rounding.)  Returns the next token behind the last, as tl_decode_step.
  * Needs tl_cache_8bit and a cache (TL_ERR_ARG); kv_length + n_tokens <= max_tokens (TL_ERR_WINDOW).  After an error past these checks the cache
  * is dropped.  Other errors as tl_prefill. */
 tl_status tl_extend(tl_lora* lora, const int32_t* tokens, int32_t n_tokens, int32_t* next_token, float* logits_out);

@@ -39,7 +39,7 @@ constexpr int VP = 17;      // words of a value row (64 codes) in LDS: odd, so t
 // TB/s in and out); 333 tokens take 6.2 us, one 2.5: two round trips to memory.
 template <int D>
 __global__ __launch_bounds__(2 * D) void cache8_append_kernel(Cache8 c, int n_cached, const bf16_t* __restrict__ k, long ldk,
-                                                              const bf16_t* __restrict__ v, long ldv, int n_new) {
+                                                              const bf16_t* __restrict__ v, long ldv, int n_new, Cache8Exact exact) {
     using T = Cache8Tile<D>;
     __shared__ int red[4];
     __shared__ unsigned sv[D * VP];
@@ -82,6 +82,20 @@ __global__ __launch_bounds__(2 * D) void cache8_append_kernel(Cache8 c, int n_ca
                         auto get = [&](int e) { return ((i < 2 ? w[e].x : w[e].y) >> 16 * (i & 1)) & 0xffffu; };
                         x[i] = make_uint4(get(0) | get(1) << 16, get(2) | get(3) << 16, get(4) | get(5) << 16, get(6) | get(7) << 16);
                     }
+            }
+        }
+        if (exact.k) {                                     // (uniform) the block as it came as well
+            bf16_t* to = (values ? exact.v : exact.k) + ((long)(block - exact.first) * c.heads + head) * 64 * D;
+            if (!values) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) *(uint4*)(to + (col >> 6) * 4096 + (t0 + i) * 64 + (col & 63)) = x[i];
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {              // four tokens of a column
+                    const unsigned sel = e & 1 ? 0x07060302u : 0x05040100u;
+                    auto pair = [&](int i) { return __builtin_amdgcn_perm((&x[i + 1].x)[e >> 1], (&x[i].x)[e >> 1], sel); };
+                    *(uint2*)(to + (col + e) * 64 + t0) = make_uint2(pair(0), pair(2));
+                }
             }
         }
         int amax = 0;                                      // bf16 bits of the largest magnitude
@@ -159,14 +173,14 @@ __global__ __launch_bounds__(2 * D) void cache8_append_kernel(Cache8 c, int n_ca
     }
 }
 hipError_t launch_cache8_append(const Cache8& c, int n_cached, const bf16_t* k, long ldk, const bf16_t* v, long ldv, int n_new,
-                                hipStream_t s) {
+                                hipStream_t s, const Cache8Exact& exact) {
     // at most 2^19 tokens a launch, for the grid's sake; the cache does not depend on where a text is cut
     for (int i = 0; i < n_new;) {
         const int m = min(n_new - i, 1 << 19), at = n_cached + i, done = ((at + m) >> 6) - (at >> 6);
         const int grid = 2 * c.heads * (done > 1 ? done : 1);
         const bf16_t *ki = k + (long)i * ldk, *vi = v + (long)i * ldv;
-        if (c.d == 128) cache8_append_kernel<128><<<grid, 256, 0, s>>>(c, at, ki, ldk, vi, ldv, m);
-        else cache8_append_kernel<64><<<grid, 128, 0, s>>>(c, at, ki, ldk, vi, ldv, m);
+        if (c.d == 128) cache8_append_kernel<128><<<grid, 256, 0, s>>>(c, at, ki, ldk, vi, ldv, m, exact);
+        else cache8_append_kernel<64><<<grid, 128, 0, s>>>(c, at, ki, ldk, vi, ldv, m, exact);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         i += m;
@@ -284,10 +298,11 @@ __device__ __forceinline__ uint4 tail_values(uint4 w, int u0, int end, bool* odd
 // FRESH: the token being decoded, one row of as many query as key heads.  Its q, k and v do not exist as rows yet: every workgroup forms its head's q
 // (while its first codes are on their way), and the one whose range ends with the tail forms k and v and puts them there.  The token must not
 // complete a block.
-template <int D, int NW, bool FRESH>
+// EXACT: complete blocks are held as they came as well, from exact.first on (a kernel of its own: 252 registers instead of 195).
+template <int D, int NW, bool FRESH, bool EXACT>
 __global__ __launch_bounds__(NW * 64, 8 / NW) void attn8_cols_kernel(Cache8 c, int n_keys, const bf16_t* __restrict__ q, long ldq, int n_rows, int group,
                                                             float scale_log2e, bf16_t* __restrict__ o, long ldo, float* __restrict__ ws,
-                                                            int blocks_per_split, DecodeFresh fresh, DecodeOut more) {
+                                                            int blocks_per_split, DecodeFresh fresh, DecodeOut more, Cache8Exact exact) {
     constexpr int PC = D / 64, NT = D / 16, LDP = D + 4, NCOL = 64 / NW, PART = NCOL * LDP > 1024 ? NCOL * LDP : 1024;
     __shared__ __align__(16) float part[NW][PART];         // a column's output, maximum and sum, wave by wave
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m16 = lane & 15, g = lane >> 4;
@@ -295,7 +310,7 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void attn8_cols_kernel(Cache8 c, i
     const int col = min(m16, n_cols - 1), row = col / group, seen = n_keys - n_rows + row + 1;      // keys 0 .. seen - 1
     const int least = n_keys - n_rows + 1;                                                              // the first column's
     const int b_begin = (int)blockIdx.y * blocks_per_split, b_end = min(b_begin + blocks_per_split, (n_keys + 63) >> 6);
-    const int key0 = (m16 >> 2) * 16 + (m16 & 3), b_tail = n_keys >> 6, b_full = min(b_end, b_tail);
+    const int key0 = (m16 >> 2) * 16 + (m16 & 3), b_tail = n_keys >> 6, b_full = min(b_end, EXACT ? min(b_tail, exact.first) : b_tail);
     // a block's keys are asked for when the block before has used its own, its values when those have been used
     uint4 kr[4][PC], vr[NT];
     float ks_next = 0.f;
@@ -404,9 +419,11 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void attn8_cols_kernel(Cache8 c, i
             if (t & 1) __builtin_amdgcn_sched_barrier(0);
         }
     }
-    if (b == b_tail && b < b_end) {                        // the tail, bf16: one wave's
-        const bf16_t *kt = c.kt + (long)head * 64 * D, *vt = c.vt + (long)head * 64 * D;
-        const int end = n_keys & 63;
+    for (; b < b_end; b += NW) {                           // the tail, one wave's, and blocks as they came: bf16
+        const bool tail = !EXACT || b == b_tail;
+        const long at = (tail ? head : (long)(b - exact.first) * c.heads + head) * 64 * D;
+        const bf16_t *kt = (tail ? c.kt : exact.k) + at, *vt = (tail ? c.vt : exact.v) + at;
+        const int end = tail ? n_keys & 63 : 64;
         bool odd = false;
         uint4 kw[4][2 * PC], vw[NT][2];                    // all of it on its way before the first is used
 #pragma unroll
@@ -454,6 +471,7 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void attn8_cols_kernel(Cache8 c, i
             }
             __builtin_amdgcn_wave_barrier();
         }
+        if (!EXACT) break;
     }
     l += __shfl_xor(l, 16, 64);
     l += __shfl_xor(l, 32, 64);
@@ -542,14 +560,15 @@ __device__ __forceinline__ unsigned v_piece_at(int d, int c) { return d * 128 + 
 
 constexpr int ATTN8_ONE_ROUND = 256;                         // workgroups of eight waves that run at once, one a CU
 
-template <int D, int NC>
+template <int D, int NC, bool EXACT>
 __global__ __launch_bounds__(NC * 64, 2) void attn8_rows_kernel(Cache8 c, int n_keys, const bf16_t* __restrict__ q, long ldq, int n_rows, int group,
                                                              float scale_log2e, bf16_t* __restrict__ o, long ldo, float* __restrict__ ws,
-                                                             int blocks_per_split, int n_split) {
+                                                             int blocks_per_split, int n_split, Cache8Exact exact) {
     constexpr int KS = D / 16, ND = D / 32, NT = NC * 64, NP = 64 * D / 16, PT = 2 * NP / NT;   // pieces of 16 codes: of K, a thread
     constexpr int TB = 64 * D * 2, STAGE = 2 * TB + 16;                                        // a tile's bytes in LDS, K, V and scales
     extern __shared__ __align__(16) unsigned char smem[];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, g = lane >> 5;
+    int tid = threadIdx.x, l32 = tid & 31, g = tid >> 5 & 1;
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     // The last columns see most.  Workgroups that all run at once take 128 columns from the end (waves 0 to 3) and as many from the front (4 to 7, on the
     // same SIMDs), so that one has about as much to do as another: 2048 rows of 32 heads and 8192 keys 257 -> 246 us, 2048 keys 63.6 -> 50.9.  Of more, one after
     // another on a CU, those of the last columns come first (4096 rows and keys 146, in pairs 162), as do those of four waves.  A head's workgroups
@@ -564,6 +583,7 @@ __global__ __launch_bounds__(NC * 64, 2) void attn8_rows_kernel(Cache8 c, int n_
     const int w_most = w0 < n_cols ? n_keys - n_rows + min(w0 + 31, n_cols - 1) / group + 1 : 0;     // the wave's
     const int w_least = n_keys - n_rows + w0 / group + 1;
     const int b_begin = split * blocks_per_split, b_end = min(b_begin + blocks_per_split, (most + 63) >> 6), b_tail = n_keys >> 6;
+    const int b_codes = min(b_end, EXACT ? min(b_tail, exact.first) : b_tail);
 
     bf16x8_t qf[KS];
     const bf16_t* qr = q + (long)row * ldq + (long)(head * group + col % group) * D + g * 8;
@@ -602,9 +622,15 @@ __global__ __launch_bounds__(NC * 64, 2) void attn8_rows_kernel(Cache8 c, int n_
         }
         if (tid < 2) ((float*)(st + 2 * TB))[tid] = tid ? sc : sc * scale_log2e;
     };
-    // the tail as a tile; whether a value of it is not finite
-    auto tail_tile = [&](unsigned char* st) {
-        const bf16_t *kt = c.kt + (long)head * 64 * D, *vt = c.vt + (long)head * 64 * D;
+    // bf16: the values of the tail, or of a block as it came, and how many tokens of it there are
+    auto is_tail = [&](int b) { return !EXACT || b == b_tail; };
+    auto exact_at = [&](int b) { return (is_tail(b) ? head : (long)(b - exact.first) * c.heads + head) * 64 * D; };
+    auto exact_values = [&](int b) { return (is_tail(b) ? c.vt : exact.v) + exact_at(b); };
+    auto exact_tokens = [&](int b) { return is_tail(b) ? n_keys & 63 : 64; };
+    // it as a tile; whether a value of it is not finite
+    auto exact_tile = [&](int b, unsigned char* st) {
+        const bf16_t *kt = (is_tail(b) ? c.kt : exact.k) + exact_at(b), *vt = exact_values(b);
+        const int end = exact_tokens(b);
         bool odd = false;
 #pragma unroll
         for (int i = 0; i < PT; ++i) {
@@ -615,8 +641,8 @@ __global__ __launch_bounds__(NC * 64, 2) void attn8_rows_kernel(Cache8 c, int n_
                 *(uint4*)(st + k_piece_at<D>(key, ch + 1)) = *(const uint4*)(kt + p * 16 + 8);
             } else {
                 const int d = (p - NP) >> 2, ch = (p & 3) * 2, u0 = (p & 3) * 16;
-                const uint4 a = tail_values(*(const uint4*)(vt + d * 64 + u0), u0, n_keys & 63, &odd);
-                const uint4 b = tail_values(*(const uint4*)(vt + d * 64 + u0 + 8), u0 + 8, n_keys & 63, &odd);
+                const uint4 a = tail_values(*(const uint4*)(vt + d * 64 + u0), u0, end, &odd);
+                const uint4 b = tail_values(*(const uint4*)(vt + d * 64 + u0 + 8), u0 + 8, end, &odd);
                 *(uint4*)(st + TB + v_piece_at(d, ch)) = make_uint4(a.x, a.y, b.x, b.y);
                 *(uint4*)(st + TB + v_piece_at(d, ch + 1)) = make_uint4(a.z, a.w, b.z, b.w);
             }
@@ -624,7 +650,7 @@ __global__ __launch_bounds__(NC * 64, 2) void attn8_rows_kernel(Cache8 c, int n_
         if (tid < 2) ((float*)(st + 2 * TB))[tid] = tid ? 1.f : scale_log2e;
         return odd;
     };
-    // probs (bf16 [64][32] of this wave) is set for a tail with values that are not finite
+    // probs (bf16 [64][32] of this wave) is set for a bf16 tile with values that are not finite
     auto tile = [&](int b, const unsigned char* st, unsigned short* probs) {
         const int u0 = b << 6;
         if (u0 >= w_most) return;                            // (uniform) no column of the wave sees it
@@ -679,12 +705,12 @@ __global__ __launch_bounds__(NC * 64, 2) void attn8_rows_kernel(Cache8 c, int n_
             }
         } else {
             // a value that is not finite counts for the columns that see it alone, which a product with zeros does not give
-            const bf16_t* vt = c.vt + (long)head * 64 * D;
+            const bf16_t* vt = exact_values(b);
 #pragma unroll
             for (int v = 0; v < 32; ++v) probs[(32 * (v >> 4) + 8 * (v >> 2 & 3) + 4 * g + (v & 3)) * 32 + l32] = f32_to_bf16(x[v]);
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
-            for (int u = 0; u < (n_keys & 63) && u0 + u < seen; ++u) {
+            for (int u = 0; u < exact_tokens(b) && u0 + u < seen; ++u) {
                 const float p = bf16_to_f32(probs[u * 32 + l32]);
 #pragma unroll
                 for (int dt = 0; dt < ND; ++dt)
@@ -694,7 +720,7 @@ __global__ __launch_bounds__(NC * 64, 2) void attn8_rows_kernel(Cache8 c, int n_
         }
     };
 
-    const int full = min(b_end, b_tail) - b_begin;           // complete blocks
+    const int full = b_codes - b_begin;                      // blocks that are codes
     if (full > 0) {
         fetch(b_begin);
         widen(smem);
@@ -706,12 +732,15 @@ __global__ __launch_bounds__(NC * 64, 2) void attn8_rows_kernel(Cache8 c, int n_
         if (i + 2 < full) fetch(b_begin + i + 2);
         tile(b_begin + i, smem + (i & 1) * STAGE, nullptr);
     }
-    if (b_end > b_tail && b_tail >= b_begin) {
+    for (int b = max(b_begin, b_codes); b < b_end; ++b) {    // blocks as they came, and the tail
+        // (opaque: the places in LDS are worked out tile by tile, or they would be kept beside all else and 130 bytes a lane spilled)
+        if constexpr (EXACT) asm volatile("" : "+v"(tid), "+v"(l32), "+v"(g));
         __syncthreads();
-        const bool odd = tail_tile(smem);
+        const bool odd = exact_tile(b, smem);
         unsigned short* probs = (unsigned short*)(smem + STAGE) + wave * 64 * 32;
-        if (__syncthreads_or(odd)) tile(b_tail, smem, probs);
-        else tile(b_tail, smem, nullptr);
+        if (__syncthreads_or(odd)) tile(b, smem, probs);
+        else tile(b, smem, nullptr);
+        if (!EXACT) break;
     }
     l += __shfl_xor(l, 32, 64);
     if (n_split > 1) {
@@ -809,41 +838,50 @@ const char* attention_cache8_plan(int n_keys, int n_rows, int heads, int kv_head
 }
 template <int D>
 static hipError_t run_attention_cache8(const Attn8Plan& p, const Cache8& c, int n_keys, const bf16_t* q, long ldq, int n_rows, int group, bf16_t* o,
-                                       long ldo, float* ws, hipStream_t s, const DecodeFresh* fresh, const DecodeOut& out) {
+                                       long ldo, float* ws, hipStream_t s, const DecodeFresh* fresh, const DecodeOut& out,
+                                       const Cache8Exact& exact = Cache8Exact{}) {
     const float scale = 1.4426950408889634f / sqrtf((float)D);
     const long n_cols = (long)n_rows * group;
     float* w = p.n_split > 1 || (out.a && !fresh) ? ws : nullptr;       // (the join leaves the shares of A o)
-    auto rows = [&](auto nc) {
+    auto rows = [&](auto nc, auto kernel) {
         constexpr int NC = decltype(nc)::value;
         constexpr size_t lds = attn8_rows_lds<D, NC>();
-        const hipError_t e = hipFuncSetAttribute((const void*)attn8_rows_kernel<D, NC>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e != hipSuccess) return e;
-        attn8_rows_kernel<D, NC><<<c.heads * cdiv(n_cols, 32 * NC) * p.n_split, NC * 64, lds, s>>>(c, n_keys, q, ldq, n_rows, group, scale, o, ldo, w,
-                                                                                             p.per, p.n_split);
+        kernel<<<c.heads * cdiv(n_cols, 32 * NC) * p.n_split, NC * 64, lds, s>>>(c, n_keys, q, ldq, n_rows, group, scale, o, ldo, w,
+                                                                                             p.per, p.n_split, exact);
         return hipGetLastError();
     };
     hipError_t e;
     if (p.cols == 16) {                                    // (one workgroup holds all the columns of a key head)
         auto cols = [&](auto kernel, int threads) {
-            kernel<<<dim3(c.heads, p.n_split), threads, 0, s>>>(c, n_keys, q, ldq, n_rows, group, scale, o, ldo, w, p.per, fresh ? *fresh : DecodeFresh{}, out);
+            kernel<<<dim3(c.heads, p.n_split), threads, 0, s>>>(c, n_keys, q, ldq, n_rows, group, scale, o, ldo, w, p.per, fresh ? *fresh : DecodeFresh{}, out,
+                                                               exact);
         };
-        if (p.waves == 8) fresh ? cols(attn8_cols_kernel<D, 8, true>, 512) : cols(attn8_cols_kernel<D, 8, false>, 512);
-        else fresh ? cols(attn8_cols_kernel<D, 4, true>, 256) : cols(attn8_cols_kernel<D, 4, false>, 256);
+        if (fresh) p.waves == 8 ? cols(attn8_cols_kernel<D, 8, true, false>, 512) : cols(attn8_cols_kernel<D, 4, true, false>, 256);
+        else if (exact.k) p.waves == 8 ? cols(attn8_cols_kernel<D, 8, false, true>, 512) : cols(attn8_cols_kernel<D, 4, false, true>, 256);
+        else p.waves == 8 ? cols(attn8_cols_kernel<D, 8, false, false>, 512) : cols(attn8_cols_kernel<D, 4, false, false>, 256);
         e = hipGetLastError();
-    } else e = p.cols == 128 ? rows(std::integral_constant<int, 4>{}) : rows(std::integral_constant<int, 8>{});
+    } else if (p.cols == 128) {
+        constexpr std::integral_constant<int, 4> nc;
+        e = exact.k ? rows(nc, attn8_rows_kernel<D, 4, true>) : rows(nc, attn8_rows_kernel<D, 4, false>);
+    } else {
+        constexpr std::integral_constant<int, 8> nc;
+        e = exact.k ? rows(nc, attn8_rows_kernel<D, 8, true>) : rows(nc, attn8_rows_kernel<D, 8, false>);
+    }
     if (e != hipSuccess || !w) return e;
     auto join = p.n_split <= 8 ? attn8_join_kernel<D, 8> : p.n_split <= 16 ? attn8_join_kernel<D, 16> : attn8_join_kernel<D, 32>;
     join<<<n_rows * c.heads * group, D, 0, s>>>(w, p.n_split, c.heads * group, ldo, out);
     return hipGetLastError();
 }
 hipError_t launch_attention_cache8(const Cache8& c, int n_keys, const bf16_t* q, long ldq, int n_rows, int heads, bf16_t* o, long ldo,
-                                   float* ws, size_t ws_elems, hipStream_t s) {
+                                   float* ws, size_t ws_elems, hipStream_t s, const Cache8Exact& exact) {
     if (n_rows <= 0) return n_rows == 0 ? hipSuccess : hipErrorInvalidValue;
     const Attn8Plan p = attn8_plan(n_keys, n_rows, heads, c.heads, c.d, ws ? ws_elems : 0);
     DecodeOut out;
     out.o = o;
-    return c.d == 128 ? run_attention_cache8<128>(p, c, n_keys, q, ldq, n_rows, heads / c.heads, o, ldo, ws, s, nullptr, out)
-                      : run_attention_cache8<64>(p, c, n_keys, q, ldq, n_rows, heads / c.heads, o, ldo, ws, s, nullptr, out);
+    return c.d == 128 ? run_attention_cache8<128>(p, c, n_keys, q, ldq, n_rows, heads / c.heads, o, ldo, ws, s, nullptr, out, exact)
+                      : run_attention_cache8<64>(p, c, n_keys, q, ldq, n_rows, heads / c.heads, o, ldo, ws, s, nullptr, out, exact);
 }
 
 // ---------------------------------------------------------------- the token being decoded

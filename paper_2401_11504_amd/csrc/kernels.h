@@ -219,13 +219,20 @@ struct Cache8 {                           // see cache8.hip for the layout
     bf16_t *kt, *vt;                      // the incomplete block: [heads][d / 64][64][64], [heads][d][64]
     int heads, d;
 };
-// tokens n_cached .. n_cached + n_new - 1; k, v: rows of [heads * d]
-hipError_t launch_cache8_append(const Cache8& c, int n_cached, const bf16_t* k, long ldk, const bf16_t* v, long ldv, int n_new, hipStream_t s);
+// complete blocks first, first + 1, .. as they came, bf16, each laid out as a tail is
+struct Cache8Exact {
+    bf16_t *k = nullptr, *v = nullptr;
+    int first = 0x7fffffff;
+};
+// tokens n_cached .. n_cached + n_new - 1; k, v: rows of [heads * d]; exact.k set: blocks that they complete go there as well, first = n_cached / 64
+hipError_t launch_cache8_append(const Cache8& c, int n_cached, const bf16_t* k, long ldk, const bf16_t* v, long ldv, int n_new, hipStream_t s,
+                                const Cache8Exact& exact = Cache8Exact{});
 hipError_t launch_cache8_read(const Cache8& c, int n_cached, int first, int n, float* k, long ldk, float* v, long ldv, hipStream_t s);
-// o = attention of rows of queries, the last n_rows of n_keys tokens; heads a multiple of c.heads, 1 <= n_rows <= n_keys
+// o = attention of rows of queries, the last n_rows of n_keys tokens; heads a multiple of c.heads, 1 <= n_rows <= n_keys; blocks from exact.first on
+// from there instead of from the codes
 constexpr int ATTN8_MAX_SPLIT = 64;
 hipError_t launch_attention_cache8(const Cache8& c, int n_keys, const bf16_t* q, long ldq, int n_rows, int heads, bf16_t* o, long ldo,
-                                   float* ws, size_t ws_elems, hipStream_t s);
+                                   float* ws, size_t ws_elems, hipStream_t s, const Cache8Exact& exact = Cache8Exact{});
 // the newest token of a cache, formed, put in as token n_keys - 1, and its attention: qkv [3 d] and ws (heads * (d + 2) floats or more) are scratch
 hipError_t launch_decode_cache8(const Cache8& c, int n_keys, const DecodeFresh& fresh, const DecodeOut& out, bf16_t* qkv, float* ws, size_t ws_elems,
                                 hipStream_t s);

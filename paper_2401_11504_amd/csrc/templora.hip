@@ -173,6 +173,7 @@ struct tl_lora {
     bool kv8 = false;
     std::vector<Cache8> cache8;
     float* ws8 = nullptr;         // scratch of the attention over it
+    Cache8Exact exact8;           // a layer's blocks that a tl_extend completes, bf16
     // choice of the next token (emit_next): what is set of penalties, bias and mask, and the tokens that the cache holds (pinned, read by the counts)
     bool penalties = false, biased = false, masked = false;
     tl_penalties pen = {1.f, 0.f, 0.f, 0};
@@ -636,7 +637,8 @@ static tl_status group_bwd(tl_lora* L, int l, int g, const bf16_t* dY, const bf1
 }
 
 // ---------------------------------------------------------------- one decoder layer
-// n_past >= 0 (tl_extend): the T tokens follow n_past tokens of the 8-bit cache, which they join, and attend to all of it
+// n_past >= 0 (tl_extend): the T tokens follow n_past tokens of the 8-bit cache, which they join and attend to: to the blocks that were complete as
+// codes, to the others and one another as bf16, because the scale of a block that they complete would tell a token of those behind it
 static tl_status layer_forward(tl_lora* L, int l, const float* h_in, float* h_out, int T, int n_past = -1) {
     tl_model* m = L->model;
     const tl_model_cfg& c = m->cfg;
@@ -648,8 +650,10 @@ static tl_status layer_forward(tl_lora* L, int l, const float* h_in, float* h_ou
     TLCHK(group_fwd(L, l, G_QKV, sv.x1, T, sv.qkv, nullptr, nullptr));
     HIPCHK(launch_rope(sv.qkv, 3L * d, T, 2 * c.n_heads, c.d_head, c.rope_base, std::max(n_past, 0), +1, m->rope, s));  // q and k
     if (n_past >= 0) {
-        HIPCHK(launch_cache8_append(L->cache8[l], n_past, sv.qkv + d, 3L * d, sv.qkv + 2 * d, 3L * d, T, s));
-        HIPCHK(launch_attention_cache8(L->cache8[l], n_past + T, sv.qkv, 3L * d, T, c.n_heads, sv.o, d, L->ws8, kWs8Elems, s));
+        Cache8Exact exact = L->exact8;
+        exact.first = n_past >> 6;
+        HIPCHK(launch_cache8_append(L->cache8[l], n_past, sv.qkv + d, 3L * d, sv.qkv + 2 * d, 3L * d, T, s, exact));
+        HIPCHK(launch_attention_cache8(L->cache8[l], n_past + T, sv.qkv, 3L * d, T, c.n_heads, sv.o, d, L->ws8, kWs8Elems, s, exact));
     } else {
         HIPCHK(launch_attention_fwd(sv.qkv, sv.qkv + d, sv.qkv + 2 * d, 3L * d, T, c.n_heads, c.d_head, sv.o, d, sv.lse, s));
     }
@@ -1091,6 +1095,8 @@ extern "C" tl_status tl_cache_8bit(tl_lora* L, int32_t on) {
         const size_t nb = cdiv(c.max_tokens, 64);
         std::vector<Cache8> all(c.n_layers);
         if (!L->ws8) TLCHK(L->pool.alloc(&L->ws8, kWs8Elems));
+        if (!L->exact8.k) TLCHK(L->pool.alloc(&L->exact8.k, nb * 64 * d));
+        if (!L->exact8.v) TLCHK(L->pool.alloc(&L->exact8.v, nb * 64 * d));
         for (Cache8& x : all) {
             TLCHK(L->pool.alloc(&x.k, nb * 64 * d));
             TLCHK(L->pool.alloc(&x.v, nb * 64 * d));
