@@ -488,7 +488,8 @@ tl_status tl_k_cache8_read(const tl_cache8_mem* cache, int32_t n_cached, int32_t
 /* Causal attention of the last n_rows of n_keys cached tokens (one row: a decoding step): row i of q (bf16 [n_rows, n_heads * d_head]) sees
  * keys 0 .. n_keys - n_rows + i;  o = softmax(q K^T / sqrt(d_head)) V, bf16, K and V what the cache stands for.  n_heads is a multiple
  * of n_kv_heads; query head j reads key head j / (n_heads / n_kv_heads).  n_rows <= n_keys, n_rows * n_heads <= 2^24.  n_keys is all that is
- * cached, or fewer: a multiple of 64 or a number inside the tail (so for reads).  Sums over the keys are fp32: 256 * n_keys * the largest value has to stay below 3e38.
+ * cached, or fewer: a multiple of 64 or a number inside the tail (so for reads).  The scale of a complete block comes from all its tokens: a row in the
+ * middle of one sees the keys before it through a scale that the tokens behind it have part in (append and attend piece by piece where they must not).  Sums over the keys are fp32: 256 * n_keys * the largest value has to stay below 3e38.
  * workspace: NULL, or device fp32 scratch of workspace_elems floats: with it the keys are cut into up to 64 ranges where the rows are few,
  * n_rows * n_heads * ranges * (d_head + 2) floats are used; contents are undefined before and after, and calls that overlap in time need one
  * each.  tl_k_attention_cache8_plan: the name of the kernel that these sizes get ("columns16", "columns8", "rows128" or "rows256"), its ranges and the floats that it uses of a

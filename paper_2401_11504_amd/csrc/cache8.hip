@@ -35,6 +35,7 @@ constexpr int VP = 17;      // words of a value row (64 codes) in LDS: odd, so t
 
 // One workgroup for a block that the new tokens complete and a head's keys or values (block by block, the heads' keys before their
 // values).  Those of the first block also put the rows behind the last complete block into the tail, after they have read the tail.
+// exact.k set: the blocks that are completed go there as they came as well.
 // Values are turned round through LDS, as codes, four tokens to a word.  Bytes bound it from some 10^4 tokens of 32 heads of 128 on (32768: 177 us, 4.6
 // TB/s in and out); 333 tokens take 6.2 us, one 2.5: two round trips to memory.
 template <int D>
@@ -554,6 +555,8 @@ __global__ __launch_bounds__(D) void attn8_join_kernel(const float* __restrict__
 // (times the values' scale) are rounded to bf16, as in the attention of a chunk.  16-byte pieces of a row lie in LDS at a place of
 // their own for each of 16 rows, so that the fragment reads of 16 lanes meet in no bank; a value row's pieces hold the tokens in the
 // order in which a score fragment serves as second operand.
+// EXACT: as in the kernel above; those blocks and the tail are tiles of one buffer, loaded when their turn comes (1024 rows and 1024 keys before
+// them, 32 heads of 128: 33 us more than over codes; the registers for a tile ahead are not there).
 template <int D>
 __device__ __forceinline__ unsigned k_piece_at(int key, int c) { return key * D * 2 + ((c ^ (D == 128 ? key & 15 : key >> 1 & 7)) << 4); }
 __device__ __forceinline__ unsigned v_piece_at(int d, int c) { return d * 128 + ((c ^ (d >> 1 & 7)) << 4); }
