@@ -3,6 +3,7 @@
 #include "../../include/templora.h"
 #include "kernels.h"
 
+#include <algorithm>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -68,10 +69,11 @@ struct Pool {
         *out = (T*)p;
         return TL_OK;
     }
-    void release() {
-        for (void* p : ptrs) (void)hipFree(p);
-        ptrs.clear();
+    // gives back what was allocated since there were n allocations
+    void release_from(size_t n) {
+        for (; ptrs.size() > n; ptrs.pop_back()) (void)hipFree(ptrs.back());
     }
+    void release() { release_from(0); }
 };
 
 // projection groups that share an input: q|k|v, o, gate|up, down
@@ -975,8 +977,15 @@ static tl_status append_8bit(tl_lora* L, int l, const bf16_t* qkv, int n) {
 }
 static tl_status alloc_kvbuf(tl_lora* L) {
     const tl_model_cfg& c = L->model->cfg;
+    const size_t before = L->pool.ptrs.size();
     std::vector<bf16_t*> bufs(c.n_layers, nullptr);
-    for (int l = 0; l < c.n_layers; ++l) TLCHK(L->pool.alloc(&bufs[l], (size_t)c.max_tokens * 3 * c.d_model));
+    for (bf16_t*& b : bufs) {
+        const tl_status st = L->pool.alloc(&b, (size_t)c.max_tokens * 3 * c.d_model);
+        if (st != TL_OK) {
+            L->pool.release_from(before);
+            return st;
+        }
+    }
     L->kvbuf = bufs;
     return TL_OK;
 }
@@ -1078,25 +1087,16 @@ extern "C" tl_status tl_extend(tl_lora* L, const int32_t* tokens, int32_t n_toke
 }
 
 // ---------------------------------------------------------------- cache in 8 bits
-extern "C" tl_status tl_cache_8bit(tl_lora* L, int32_t on) {
-    LIVE(L, "tl_cache_8bit");
-    tl_model* m = L->model;
-    const tl_model_cfg& c = m->cfg;
-    const size_t d = c.d_model;
-    if (!on) {
-        if (!L->kv8) return TL_OK;
-        if (L->kv_keep && L->kvbuf.empty()) TLCHK(alloc_kvbuf(L));
-        L->kv8 = false;
-        L->kv_len = 0;            // codes do not go back
-        return TL_OK;
-    }
-    if (L->kv8) return TL_OK;
-    if (L->cache8.empty()) {
-        const size_t nb = cdiv(c.max_tokens, 64);
-        std::vector<Cache8> all(c.n_layers);
-        if (!L->ws8) TLCHK(L->pool.alloc(&L->ws8, kWs8Elems));
-        if (!L->exact8.k) TLCHK(L->pool.alloc(&L->exact8.k, nb * 64 * d));
-        if (!L->exact8.v) TLCHK(L->pool.alloc(&L->exact8.v, nb * 64 * d));
+static tl_status alloc_cache8(tl_lora* L) {
+    const tl_model_cfg& c = L->model->cfg;
+    const size_t d = c.d_model, nb = cdiv(c.max_tokens, 64), before = L->pool.ptrs.size();
+    std::vector<Cache8> all(c.n_layers);
+    float* ws = nullptr;
+    Cache8Exact exact;
+    auto body = [&]() -> tl_status {
+        TLCHK(L->pool.alloc(&ws, kWs8Elems));
+        TLCHK(L->pool.alloc(&exact.k, nb * 64 * d));
+        TLCHK(L->pool.alloc(&exact.v, nb * 64 * d));
         for (Cache8& x : all) {
             TLCHK(L->pool.alloc(&x.k, nb * 64 * d));
             TLCHK(L->pool.alloc(&x.v, nb * 64 * d));
@@ -1106,8 +1106,29 @@ extern "C" tl_status tl_cache_8bit(tl_lora* L, int32_t on) {
             TLCHK(L->pool.alloc(&x.vt, 64 * d));
             x.heads = c.n_heads, x.d = c.d_head;
         }
-        L->cache8 = all;
+        return TL_OK;
+    };
+    const tl_status st = body();
+    if (st != TL_OK) {
+        L->pool.release_from(before);
+        return st;
     }
+    L->ws8 = ws, L->exact8 = exact, L->cache8 = all;
+    return TL_OK;
+}
+extern "C" tl_status tl_cache_8bit(tl_lora* L, int32_t on) {
+    LIVE(L, "tl_cache_8bit");
+    tl_model* m = L->model;
+    const tl_model_cfg& c = m->cfg;
+    if (!on) {
+        if (!L->kv8) return TL_OK;
+        if (L->kv_keep && L->kvbuf.empty()) TLCHK(alloc_kvbuf(L));
+        L->kv8 = false;
+        L->kv_len = 0;            // codes do not go back
+        return TL_OK;
+    }
+    if (L->kv8) return TL_OK;
+    if (L->cache8.empty()) TLCHK(alloc_cache8(L));
     // a cache that exists already moves along
     for (int l = 0; l < c.n_layers && L->kv_len > 0; ++l) TLCHK(append_8bit(L, l, L->kv_keep ? L->kvbuf[l] : L->save[l].qkv, L->kv_len));
     HIPCHK(hipStreamSynchronize(m->stream));
