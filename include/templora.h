@@ -244,7 +244,7 @@ tl_status tl_cache_reuse(tl_lora* lora, int32_t on);
 
 /* The cache in 8 bits, for long windows: a step reads half the bytes.  on != 0: keys and values move to buffers of their own (allocated on the first
  * call: n_layers * max_tokens * 2 d_model bytes and what belongs to them, beside the activations that the bf16 cache lies in by default; 4 d_model
- * bytes a token for tl_extend), held as tl_cache8_mem describes with n_heads heads; a cache that exists moves along.
+ * bytes a token for tl_extend; the buffers of tl_cache_reuse are given back), held as tl_cache8_mem describes with n_heads heads; a cache that exists moves along.
  * tl_prefill fills it (the prompt's own attention works on its bf16 keys and values), tl_decode_step adds to it and attends to what it stands
  * for once the new token is in, tl_extend adds to it as well.  Whether it survives training-side calls is tl_cache_reuse's to say, as for the bf16 cache.  on == 0
  * (the initial state): back to the bf16 cache; the cache is dropped.  Errors: TL_ERR_ARG, TL_ERR_DISCARDED, TL_ERR_OOM, TL_ERR_DEVICE. */

@@ -74,6 +74,12 @@ struct Pool {
         for (; ptrs.size() > n; ptrs.pop_back()) (void)hipFree(ptrs.back());
     }
     void release() { release_from(0); }
+    void release_one(void* p) {
+        auto it = std::find(ptrs.begin(), ptrs.end(), p);
+        if (it == ptrs.end()) return;
+        (void)hipFree(p);
+        ptrs.erase(it);
+    }
 };
 
 // projection groups that share an input: q|k|v, o, gate|up, down
@@ -1133,6 +1139,8 @@ extern "C" tl_status tl_cache_8bit(tl_lora* L, int32_t on) {
     for (int l = 0; l < c.n_layers && L->kv_len > 0; ++l) TLCHK(append_8bit(L, l, L->kv_keep ? L->kvbuf[l] : L->save[l].qkv, L->kv_len));
     HIPCHK(hipStreamSynchronize(m->stream));
     L->kv8 = true;
+    for (bf16_t* b : L->kvbuf) L->pool.release_one(b);     // (of tl_cache_reuse: allocated again if the bf16 cache comes back)
+    L->kvbuf.clear();
     return TL_OK;
 }
 

@@ -1,4 +1,5 @@
-"""Device memory of the caches: a call that fails for want of it gives back what it had taken."""
+"""Device memory of the caches: a call that fails for want of it gives back what it had taken, and the 8-bit cache takes the place of the
+buffers of tl_cache_reuse."""
 import numpy as np
 import pytest
 
@@ -69,3 +70,28 @@ def test_out_of_memory(api, H, model):
         nxt, logits = api.tl_decode_step(m, text[100], SHAPE.vocab)
         assert np.isfinite(logits).all()
         api.tl_lora_free(m)
+
+
+def test_buffers_of_reuse_are_given_back(api, H, model):
+    a, _ = H.new_lora(model, 6700, b_std=0.01)
+    b, _ = H.new_lora(model, 6700, b_std=0.01)
+    text = synth.zipf_tokens(6700, 200, SHAPE.vocab)
+    api.tl_cache_8bit(b, True)
+    start = free()
+    api.tl_cache_reuse(a, True)
+    assert start - free() >= (8 * 1536 - 64) * MB                 # (less what the allocator had kept of earlier frees)
+    for m in (a, b):
+        api.tl_prefill(m, text[:100])
+    api.tl_cache_8bit(a, True)                                   # the cache moves along
+    assert start - free() <= 8 * 512 * MB + 1200 * MB
+    for i in range(100, 104):
+        xa, xb = api.tl_decode_step(a, text[i], SHAPE.vocab), api.tl_decode_step(b, text[i], SHAPE.vocab)
+        assert xa[0] == xb[0] and np.array_equal(xa[1], xb[1])
+    api.tl_chunk_update(a, text[:32], 0, 1e-3)
+    assert api.tl_kv_length(a) == 104                            # reuse is still on
+    api.tl_cache_8bit(a, False)
+    api.tl_prefill(a, text[:100])
+    api.tl_chunk_update(a, text[:32], 0, 1e-3)
+    assert api.tl_kv_length(a) == 100
+    api.tl_decode_step(a, text[100])
+    api.tl_lora_free(a), api.tl_lora_free(b)
