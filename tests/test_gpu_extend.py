@@ -76,7 +76,8 @@ def far(x, y):
 
 
 @pytest.mark.parametrize("name", ["small", "small128"])
-@pytest.mark.parametrize("n,T,loud", [(5, 59, 62), (5, 70, 63), (40, 200, 127), (70, 58, 127), (130, 9, 135), (112, 16, 127), (60, 300, 188)])
+@pytest.mark.parametrize("n,T,loud", [(5, 59, 62), (5, 70, 63), (40, 200, 127), (70, 58, 127), (130, 9, 135), (112, 16, 127), (60, 300, 188),
+                                      (1530, 10, 1535), (4090, 8, 4095), (1500, 100, 1535)])
 def test_a_later_token_of_the_block(api, H, name, n, T, loud):
     """against a twin that takes the same tokens step by step: the second layer's keys and values of the tokens before the loud one"""
     shape = synth.SHAPES[name]
