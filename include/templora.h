@@ -457,6 +457,7 @@ tl_status tl_k_gemv_pre(const uint16_t* W, int32_t ldw, int32_t N, int32_t K, in
 tl_status tl_k_attention_decode(const uint16_t* q, const uint16_t* k, const uint16_t* v, int32_t ld, int32_t n_keys,
                                 int32_t n_heads, int32_t d_head, uint16_t* o, float* workspace, size_t workspace_elems,
                                 void* hip_stream);
+/* Index of the largest of n floats, the lowest among equals, NaN passed over; 2^31 - 1 if all are NaN. */
 tl_status tl_k_argmax(const float* x, int32_t n, int32_t* out, void* hip_stream);
 /*
  * A key/value cache held in 8 bits, for generation over long texts (caller-owned device memory, 16-byte aligned).
@@ -490,7 +491,8 @@ tl_status tl_k_cache8_read(const tl_cache8_mem* cache, int32_t n_cached, int32_t
  * keys 0 .. n_keys - n_rows + i;  o = softmax(q K^T / sqrt(d_head)) V, bf16, K and V what the cache stands for.  n_heads is a multiple
  * of n_kv_heads; query head j reads key head j / (n_heads / n_kv_heads).  n_rows <= n_keys, n_rows * n_heads <= 2^24.  n_keys is all that is
  * cached, or fewer: a multiple of 64 or a number inside the tail (so for reads).  The scale of a complete block comes from all its tokens: a row in the
- * middle of one sees the keys before it through a scale that the tokens behind it have part in (append and attend piece by piece where they must not).  Sums over the keys are fp32: 256 * n_keys * the largest value has to stay below 3e38.
+ * middle of one sees the keys before it through a scale that the tokens behind it have part in (append and attend piece by piece where they must not).  Sums over the keys are fp32: 256 * n_keys * the largest value has to stay below 3e38, and, scores being
+ * formed over the codes, 127 * the sum of a query's magnitudes as well.
  * workspace: NULL, or device fp32 scratch of workspace_elems floats: with it the keys are cut into up to 64 ranges where the rows are few,
  * n_rows * n_heads * ranges * (d_head + 2) floats are used; contents are undefined before and after, and calls that overlap in time need one
  * each.  tl_k_attention_cache8_plan: the name of the kernel that these sizes get ("columns16", "columns8", "rows128" or "rows256"), its ranges and the floats that it uses of a

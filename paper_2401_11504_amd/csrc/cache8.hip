@@ -36,8 +36,8 @@ constexpr int VP = 17;      // words of a value row (64 codes) in LDS: odd, so t
 // One workgroup for a block that the new tokens complete and a head's keys or values (block by block, the heads' keys before their
 // values).  Those of the first block also put the rows behind the last complete block into the tail, after they have read the tail.
 // exact.k set: the blocks that are completed go there as they came as well.
-// Values are turned round through LDS, as codes, four tokens to a word.  Bytes bound it from some 10^4 tokens of 32 heads of 128 on (32768: 177 us, 4.6
-// TB/s in and out); 333 tokens take 6.2 us, one 2.5: two round trips to memory.
+// Values are turned round through LDS, as codes, four tokens to a word.  Bytes bound it from some 10^4 tokens of 32 heads of 128 on (32768: 160 to 190 us, 4.2
+// to 5 TB/s in and out); 333 tokens take 6.4 to 7.2 us, one 2.5: two round trips to memory.
 template <int D>
 __global__ __launch_bounds__(2 * D) void cache8_append_kernel(Cache8 c, int n_cached, const bf16_t* __restrict__ k, long ldk,
                                                               const bf16_t* __restrict__ v, long ldv, int n_new, Cache8Exact exact) {
