@@ -281,6 +281,22 @@ tl_status tl_set_penalties(tl_lora* lora, const tl_penalties* penalties);
 tl_status tl_set_bias(tl_lora* lora, const float* bias);
 tl_status tl_set_allowed(tl_lora* lora, const uint32_t* allowed);
 
+/*
+ * The next token drawn instead of chosen: from the logits behind penalties, bias and mask, as tl_k_sample defines it.  The i-th draw after this call
+ * (i = 0, 1, ..; tl_prefill, tl_decode_step, tl_extend and each token of tl_generate make one each when they succeed) takes
+ *     u = (mix64(mix64(seed) + i) >> 40) * 2^-24            (mix64 as with the LoRA dropout above)
+ * so that the same calls with the same seed give the same tokens.  temperature 0, the largest; top_k 0, top_p 1, min_p 0: no such limit.  NULL: the
+ * choice is greedy again.  A token whose logit is -infinity is not drawn: a step that finds no other returns TL_ERR_ARG, as above.
+ * vocab up to 2^22.  Errors: TL_ERR_ARG, TL_ERR_SHAPE, TL_ERR_DISCARDED, TL_ERR_OOM, TL_ERR_DEVICE.
+ */
+typedef struct {
+    float temperature; /* 0 or more */
+    int32_t top_k;     /* 0 or more */
+    float top_p, min_p;
+    uint64_t seed;
+} tl_sampling;
+tl_status tl_set_sampling(tl_lora* lora, const tl_sampling* sampling);
+
 /* Release the (discarded or not) handle itself. NULL is accepted. */
 tl_status tl_lora_free(tl_lora* lora);
 
@@ -517,6 +533,75 @@ tl_status tl_k_token_counts(const int32_t* tokens, int32_t ldt, int32_t rows, in
 tl_status tl_k_choose(const float* logits, int32_t ldl, int32_t rows, int32_t vocab, const int32_t* counts, int32_t ldc, float repetition,
                       float presence, float frequency, const float* bias, int32_t ldb, const uint32_t* allowed, int32_t lda, float* out,
                       int32_t ldo, int32_t* choice, float* workspace, size_t workspace_elems, void* hip_stream);
+/*
+ * A token drawn from each row of logits (fp32 [rows, vocab], vocab up to 2^22) by a given number u (fp32 [rows], from [0, 1); below counts as 0).
+ *   params : fp32 [rows, 4], row stride ldp (0: one row for all): temperature, top_k, top_p, min_p
+ *   w_i = round(2^40 exp((x_i - largest) / temperature)): whole numbers, so that sums are exact in any order; NaN and -infinity weigh 0, and where the
+ *   largest is infinity only its equals weigh.  The order: larger logits first, the lowest index among equals.  Kept are
+ *     the first top_k of the order (below 1, or vocab and more: all; fractions are cut off),
+ *     of these, with W the sum of their weights, those before which less than ceil(top_p W) weighs (1 and more, or NaN: all; the first always),
+ *     of these, those that weigh at least ceil(min_p 2^40), min_p taken as 1 at most (0 and below, or NaN: all), and at least 1.
+ *   choice (int32 [rows]): with S the kept weight, the first token in the order of indices up to which more than min(floor(u S), S - 1) is kept;
+ *   -1 where nothing weighs.  kept (int32 [rows], may be NULL): how many tokens are; prob (fp32 [rows], may be NULL): w / S of the chosen one.
+ *   A temperature that is not above 0: the largest logit, the lowest index among equals (kept 1, prob 1).
+ * Products with top_p and u are formed in 64-bit floating point.  params, u: device.  workspace: NULL, or device fp32 scratch of workspace_elems floats (2^18
+ * are enough for any call): with it few rows with many tokens fill the GPU; contents are undefined before and after, calls that overlap in time need one each. */
+tl_status tl_k_sample(const float* logits, int32_t ldl, int32_t rows, int32_t vocab, const float* params, int32_t ldp, const float* u, int32_t* choice,
+                      int32_t* kept, float* prob, float* workspace, size_t workspace_elems, void* hip_stream);
+/*
+ * A key/value cache on pages, for many texts at once and for texts that are cut back (caller-owned device memory).
+ *   k, v  : bf16 [n_pages][n_kv_heads][page_size][d_head], at multiples of 16 bytes; page_size a power of two, 16 to 65536; d_head 64 or 128
+ *   table : int32 [n_seqs][n_table]; slot j of sequence s lies on page table[s][j / page_size] at place j % page_size.  An entry outside [0, n_pages)
+ *           is no page: what would lie there is not written, and passed over when it is read.
+ * A sequence's slots are in use from 0 up to its length, which is the caller's to keep (lengths: device int32 [n_seqs]; below 0 counts as 0, beyond the table as
+ * all of it).  Keys hold their rotation, so that the order of the slots means nothing to attention.  n_seqs up to 65536, n_seqs * n_kv_heads up to 2^24, n_table * page_size and n_pages up to 2^30.
+ * Where the table, lengths, first_row or positions change on the device between two calls, the next call sees it (captured graphs as well).
+ */
+typedef struct {
+    uint16_t *k, *v;
+    const int32_t* table;
+    int32_t n_pages, page_size, n_kv_heads, d_head, n_seqs, n_table;
+} tl_paged_mem;
+/* Keys and values of new tokens, rows of [n_kv_heads * d_head] bf16 (row strides ldk, ldv in elements, first elements anywhere).  first_row: NULL, row s is sequence s's
+ * one new token (n_rows <= n_seqs); or device int32 [n_seqs + 1], not falling: rows first_row[s] .. first_row[s + 1] - 1 are sequence s's, the others nobody's.
+ * The i-th of them goes to slot lengths[s] + i (lengths before the call; slots behind the table's end are not written).
+ * weights (fp32), positions (int32): [n_seqs][n_kv_heads][ldw], each may be NULL: of the new slots (those below ldw) they become 0 and pos[row] (pos: device int32
+ * [n_rows]; NULL: the slot).  A page that two sequences share is written by both. */
+tl_status tl_k_paged_append(const tl_paged_mem* cache, const int32_t* lengths, const uint16_t* k, int32_t ldk, const uint16_t* v, int32_t ldv,
+                            const int32_t* first_row, int32_t n_rows, const int32_t* pos, float* weights, int32_t* positions, int32_t ldw, void* hip_stream);
+/* Attention of one query a sequence over its slots 0 .. lengths[s] - 1 (the new token's among them): o = softmax(q K^T / sqrt(d_head)) V, q and o bf16
+ * [n_seqs, n_heads * d_head]; n_heads a multiple of n_kv_heads, query head j reads key head j / (n_heads / n_kv_heads).  A sequence without a slot on a page gets 0.
+ * max_len: no length is larger (what lies behind is passed over); TL_ERR_WINDOW beyond the table.  n_seqs * n_heads <= 2^24.  Sums over the keys are fp32.
+ * weights_out (fp32 [n_seqs][n_kv_heads][ldw], ldw >= max_len; may be NULL): what each slot got of attention is added up,
+ *     weights_out = weights_in + the sum over the query heads of the key head of the softmax's weight      (weights_in: as large, NULL for 0, or weights_out)
+ * for slots below the length; the others stay as they are.
+ * workspace: device fp32 scratch of workspace_elems floats, or NULL: with it the keys are cut into ranges, so that few sequences fill the GPU.  With weights it
+ * is needed (TL_ERR_SHAPE otherwise).  Contents are undefined before and after; calls that overlap in time need one each.  tl_k_attention_paged_plan: the ranges that
+ * these sizes get with it and the floats that are used (more than workspace_elems: too little for the weights); host only. */
+tl_status tl_k_attention_paged(const tl_paged_mem* cache, const int32_t* lengths, int32_t max_len, const uint16_t* q, int32_t ldq, int32_t n_heads,
+                               uint16_t* o, int32_t ldo, const float* weights_in, float* weights_out, int32_t ldw, float* workspace, size_t workspace_elems,
+                               void* hip_stream);
+tl_status tl_k_attention_paged_plan(int32_t max_len, int32_t n_seqs, int32_t n_heads, int32_t n_kv_heads, int32_t d_head, int32_t weights,
+                                    size_t workspace_elems, int32_t* n_ranges_out, size_t* elems_out);
+/* The same for a prompt: q bf16 [T, n_heads * d_head], k bf16 [T, n_kv_heads * d_head] (both rotated; row strides ldq below 2^25, ldk; first elements anywhere, fastest
+ * at multiples of 4 bytes with ldq even), lse fp32 [n_heads, T] as tl_k_attention_fwd leaves it:
+ *     weights_out[h][u] = weights_in[h][u] + the sum over the query heads of key head h and the rows t >= max(u, first_row) of exp(q_t k_u / sqrt(d_head) - lse_t)
+ * weights fp32 [n_kv_heads, T], row strides ldi, ldo (weights_in NULL for 0, or weights_out); first_row 0: every row counts; n: only the last T - n. */
+tl_status tl_k_attention_weights(const uint16_t* q, int32_t ldq, const uint16_t* k, int32_t ldk, int32_t T, int32_t n_heads, int32_t n_kv_heads,
+                                 int32_t d_head, int32_t first_row, const float* lse, const float* weights_in, int32_t ldi, float* weights_out, int32_t ldo,
+                                 void* hip_stream);
+/* Cuts sequences longer than `budget` slots back to it, each key head by itself: kept are the first `budget` slots of the order
+ *     recent tokens (position > the head's newest position - n_recent) before others, then larger weights (NaN counts as the least), then lower slots;
+ *     slots on no page come after all others.
+ * Kept slots below the budget stay where they are; the i-th slot there that is not kept receives the i-th kept one from behind (key, value, weight, position).
+ *   weights fp32, positions int32 [n_seqs][n_kv_heads][ldw] (slots from ldw on are not looked at: lengths count as ldw at most); weights_out, positions_out: as
+ *   large, or the same; slots below min(length, budget) are written.  lengths_out (int32 [n_seqs], or lengths): min(length, budget).  Pages wholly behind it are free.
+ * workspace: device fp32 scratch of n_seqs * n_kv_heads * (2 * min(budget, longest - budget) + 1) floats or more, longest = min(n_table * page_size, ldw), the
+ * minimum taken as 0 at least (TL_ERR_SHAPE otherwise); calls that overlap in time need one each.  A page that a table holds twice, or that sequences that
+ * are cut back share, ends up with what either wrote. */
+tl_status tl_k_paged_evict(const tl_paged_mem* cache, const int32_t* lengths, int32_t budget, int32_t n_recent, const float* weights, const int32_t* positions,
+                           int32_t ldw, float* weights_out, int32_t* positions_out, int32_t* lengths_out, float* workspace, size_t workspace_elems,
+                           void* hip_stream);
 /* dgu bf16 [T, 2f] from da bf16 [T, f] and gu. */
 tl_status tl_k_swiglu_bwd(const uint16_t* da, const uint16_t* gu, int32_t T, int32_t f, uint16_t* dgu,
                           void* hip_stream);

@@ -61,6 +61,15 @@ class tl_penalties(C.Structure):
     _fields_ = [("repetition", C.c_float), ("presence", C.c_float), ("frequency", C.c_float), ("last_n", C.c_int32)]
 
 
+class tl_sampling(C.Structure):
+    _fields_ = [("temperature", C.c_float), ("top_k", C.c_int32), ("top_p", C.c_float), ("min_p", C.c_float), ("seed", C.c_uint64)]
+
+
+class tl_paged_mem(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("table", C.c_void_p), ("n_pages", C.c_int32), ("page_size", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("d_head", C.c_int32), ("n_seqs", C.c_int32), ("n_table", C.c_int32)]
+
+
 class tl_cache8_mem(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("k_tail", C.c_void_p),
                 ("v_tail", C.c_void_p), ("n_kv_heads", C.c_int32), ("d_head", C.c_int32), ("capacity", C.c_int32)]
@@ -83,6 +92,7 @@ _SIGS = {
     "tl_extend": [_vp, _vp, _i32, C.POINTER(_i32), _vp],
     "tl_get_kv": [_vp, _i32, _i32, _i32, _vp, _vp],
     "tl_set_penalties": [_vp, C.POINTER(tl_penalties)],
+    "tl_set_sampling": [_vp, C.POINTER(tl_sampling)],
     "tl_set_bias": [_vp, _vp],
     "tl_set_allowed": [_vp, _vp],
     "tl_discard": [_vp],
@@ -124,6 +134,12 @@ _SIGS = {
     "tl_k_attention_cache8_plan": [_i32] * 5 + [_sz, C.c_char_p, _sz, C.POINTER(_i32), C.POINTER(_sz)],
     "tl_k_token_counts": [_vp, _i32, _i32, _i32, _i32, _i32, _vp, _i32, _vp],
     "tl_k_choose": [_vp, _i32, _i32, _i32, _vp, _i32, _f32, _f32, _f32, _vp, _i32, _vp, _i32, _vp, _i32, _vp, _vp, _sz, _vp],
+    "tl_k_sample": [_vp, _i32, _i32, _i32, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _sz, _vp],
+    "tl_k_paged_append": [C.POINTER(tl_paged_mem), _vp, _vp, _i32, _vp, _i32, _vp, _i32, _vp, _vp, _vp, _i32, _vp],
+    "tl_k_attention_paged": [C.POINTER(tl_paged_mem), _vp, _i32, _vp, _i32, _i32, _vp, _i32, _vp, _vp, _i32, _vp, _sz, _vp],
+    "tl_k_attention_paged_plan": [_i32] * 6 + [_sz, C.POINTER(_i32), C.POINTER(_sz)],
+    "tl_k_attention_weights": [_vp, _i32, _vp] + [_i32] * 6 + [_vp, _vp, _i32, _vp, _i32, _vp],
+    "tl_k_paged_evict": [C.POINTER(tl_paged_mem), _vp, _i32, _i32, _vp, _vp, _i32, _vp, _vp, _vp, _vp, _sz, _vp],
     "tl_k_attention_fwd": [_vp, _vp, _vp, _i32, _i32, _i32, _i32, _vp, _i32, _vp, _vp],
     "tl_k_attention_bwd": [_vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp],
     "tl_k_cross_entropy": [_vp, _vp, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp],
@@ -288,6 +304,12 @@ def tl_set_penalties(lora, repetition=1.0, presence=0.0, frequency=0.0, last_n=0
     p = tl_penalties(repetition, presence, frequency, last_n)
     off = (repetition, presence, frequency) == (1.0, 0.0, 0.0)
     _chk(_lib.tl_set_penalties(lora, None if off else C.byref(p)))
+
+
+def tl_set_sampling(lora, temperature=None, top_k=0, top_p=1.0, min_p=0.0, seed=0):
+    """tl_set_sampling(lora) goes back to the greedy choice"""
+    p = None if temperature is None else tl_sampling(temperature, top_k, top_p, min_p, seed)
+    _chk(_lib.tl_set_sampling(lora, None if p is None else C.byref(p)))
 
 
 def tl_set_bias(lora, bias, vocab):
@@ -613,6 +635,109 @@ def tl_k_choose(logits, counts, out, choice, repetition=1.0, presence=0.0, frequ
     hp, _ = _row(choice, torch.int32, 1, R)
     wp, n = _ws(workspace)
     _chk(_lib.tl_k_choose(lp, ldl, R, V, cp, ldc, repetition, presence, frequency, bp, ldb, ap, lda, op, ldo, hp, wp, n, _s(stream)))
+
+
+def _vec(t, dtype, n):
+    """address of n elements, or of nothing"""
+    if t is None:
+        return None
+    assert t.is_cuda and t.dtype == dtype and t.numel() == n and t.is_contiguous(), f"{dtype} [{n}] expected"
+    return t.data_ptr()
+
+
+def tl_k_sample(logits, params, u, choice, kept=None, prob=None, workspace=None, stream=None):
+    """logits fp32 [rows, vocab]; params fp32 [rows, 4] or [4]: temperature, top_k, top_p, min_p; u fp32 [rows]; choice, kept int32 [rows], prob fp32 [rows]"""
+    R, V = logits.shape
+    lp, ldl = _row(logits, torch.float32, R, V)
+    pp, ldp = _row(params, torch.float32, R, 4)
+    wp, n = _ws(workspace)
+    _chk(_lib.tl_k_sample(lp, ldl, R, V, pp, ldp, _vec(u, torch.float32, R), _vec(choice, torch.int32, R), _vec(kept, torch.int32, R),
+                          _vec(prob, torch.float32, R), wp, n, _s(stream)))
+
+
+class Paged:
+    """The memory of a key/value cache on pages (tl_paged_mem in the header): three device tensors, kept alive here.
+    k, v bf16 [n_pages, n_kv_heads, page_size, d_head], table int32 [n_seqs, n_table]."""
+
+    def __init__(self, k, v, table):
+        assert k.shape == v.shape and k.dim() == 4 and k.dtype == v.dtype == torch.bfloat16, "k, v: bf16 [n_pages, heads, page_size, d_head] expected"
+        assert table.dim() == 2 and table.dtype == torch.int32, "table: int32 [n_seqs, n_table] expected"
+        for t in (k, v, table):
+            assert t.is_cuda and t.is_contiguous(), "contiguous device tensors expected"
+        self.k, self.v, self.table = k, v, table
+        self.n_pages, self.n_kv_heads, self.page_size, self.d_head = k.shape
+        self.n_seqs, self.n_table = table.shape
+        self.width = self.n_kv_heads * self.d_head
+        self.mem = tl_paged_mem(k.data_ptr(), v.data_ptr(), table.data_ptr(), self.n_pages, self.page_size, self.n_kv_heads, self.d_head, self.n_seqs, self.n_table)
+        self.ref = C.byref(self.mem)
+
+    @classmethod
+    def empty(cls, n_pages, n_kv_heads, page_size, d_head, n_seqs, n_table, device="cuda"):
+        """pages without values, a table without pages"""
+        k, v = (torch.empty(n_pages, n_kv_heads, page_size, d_head, dtype=torch.bfloat16, device=device) for _ in range(2))
+        return cls(k, v, torch.full((n_seqs, n_table), -1, dtype=torch.int32, device=device))
+
+
+def _slots(cache, *tensors):
+    """(addresses, width) of tensors [n_seqs, n_kv_heads, width], None among them; (dtype, tensor) pairs"""
+    width, out = None, []
+    for dtype, t in tensors:
+        if t is None:
+            out.append(None)
+            continue
+        s = t.shape
+        assert t.is_cuda and t.is_contiguous() and t.dtype == dtype and len(s) == 3 and s[:2] == (cache.n_seqs, cache.n_kv_heads), \
+            f"{dtype} [{cache.n_seqs}, {cache.n_kv_heads}, slots] expected"
+        assert width in (None, s[2]), "as many slots each expected"
+        width = s[2]
+        out.append(t.data_ptr())
+    return out, width or 0
+
+
+def tl_k_paged_append(cache, lengths, k, v, first_row=None, pos=None, weights=None, positions=None, stream=None):
+    """k, v bf16 [n_rows, n_kv_heads * d_head] -> slots lengths[s] .. of sequence s = row, or of the rows first_row[s] .. first_row[s + 1] - 1;
+    weights fp32, positions int32 [n_seqs, n_kv_heads, slots]: 0 and pos[row] at the new slots"""
+    kp, ldk, vp, ldv = _rows2(k, v, torch.bfloat16, cache.width)
+    n = k.shape[0]
+    (wp, pp), width = _slots(cache, (torch.float32, weights), (torch.int32, positions))
+    _chk(_lib.tl_k_paged_append(cache.ref, _vec(lengths, torch.int32, cache.n_seqs), kp, ldk, vp, ldv, _vec(first_row, torch.int32, cache.n_seqs + 1), n,
+                                _vec(pos, torch.int32, n), wp, pp, width, _s(stream)))
+
+
+def tl_k_attention_paged(cache, lengths, q, o, n_heads, max_len=None, weights_in=None, weights_out=None, workspace=None, stream=None):
+    """q, o bf16 [n_seqs, n_heads * d_head]; no sequence is longer than max_len (None: than the table has room for);
+    weights_out fp32 [n_seqs, n_kv_heads, slots] = weights_in (or 0) + what each slot got"""
+    qp, ldq, op, ldo = _rows2(q, o, torch.bfloat16, n_heads * cache.d_head)
+    assert q.shape[0] == cache.n_seqs, "one row a sequence expected"
+    (ip, wp), width = _slots(cache, (torch.float32, weights_in), (torch.float32, weights_out))
+    sp, n = _ws(workspace)
+    _chk(_lib.tl_k_attention_paged(cache.ref, _vec(lengths, torch.int32, cache.n_seqs), cache.n_table * cache.page_size if max_len is None else max_len, qp, ldq,
+                                   n_heads, op, ldo, ip, wp, width, sp, n, _s(stream)))
+
+
+def tl_k_attention_paged_plan(max_len, n_seqs, n_heads, n_kv_heads, d_head, weights=False, workspace_elems=0):
+    """-> (ranges of keys, floats of the workspace that are used, or needed where that is more)"""
+    n, elems = _i32(0), _sz(0)
+    _chk(_lib.tl_k_attention_paged_plan(max_len, n_seqs, n_heads, n_kv_heads, d_head, int(weights), workspace_elems, C.byref(n), C.byref(elems)))
+    return n.value, elems.value
+
+
+def tl_k_attention_weights(q, k, n_heads, n_kv_heads, lse, weights_in, weights_out, first_row=0, stream=None):
+    """q bf16 [T, n_heads * d_head], k bf16 [T, n_kv_heads * d_head], lse fp32 [n_heads, T]; weights_in (or None), weights_out fp32 [n_kv_heads, T or more]"""
+    T, d = q.shape[0], q.shape[1] // n_heads
+    assert q.dtype == k.dtype == torch.bfloat16 and q.shape[1] == n_heads * d and tuple(k.shape) == (T, n_kv_heads * d), "bf16 [T, heads * d_head] expected"
+    for w in (weights_in, weights_out):
+        assert w is None or (w.dtype == torch.float32 and w.dim() == 2 and w.shape[0] == n_kv_heads and w.shape[1] >= T), "weights: fp32 [n_kv_heads, T] expected"
+    _chk(_lib.tl_k_attention_weights(_dp(q), q.stride(0), _dp(k), k.stride(0), T, n_heads, n_kv_heads, d, first_row, _vec(lse, torch.float32, n_heads * T),
+                                     _dp(weights_in), weights_in.stride(0) if weights_in is not None else 0, _dp(weights_out), weights_out.stride(0), _s(stream)))
+
+
+def tl_k_paged_evict(cache, lengths, budget, n_recent, weights, positions, weights_out, positions_out, lengths_out, workspace, stream=None):
+    """weights fp32, positions int32 [n_seqs, n_kv_heads, slots] and what they become (or the same tensors); lengths, lengths_out int32 [n_seqs] (or the same)"""
+    (wp, pp, wo, po), width = _slots(cache, (torch.float32, weights), (torch.int32, positions), (torch.float32, weights_out), (torch.int32, positions_out))
+    sp, n = _ws(workspace)
+    _chk(_lib.tl_k_paged_evict(cache.ref, _vec(lengths, torch.int32, cache.n_seqs), budget, n_recent, wp, pp, width, wo, po,
+                               _vec(lengths_out, torch.int32, cache.n_seqs), sp, n, _s(stream)))
 
 
 def tl_k_attention_fwd(q, k, v, n_heads, d_head, o, lse, stream=None):

@@ -17,7 +17,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libtemplora.so")
 SOURCES = ["templora.hip", "gemm_bf16.hip", "gemm_f32.hip", "attention.hip", "elementwise.hip", "decode.hip",
-           "cache8.hip", "choose.hip"]
+           "cache8.hip", "choose.hip", "sample.hip", "paged.hip", "attn_weights.hip"]
 # packed-fp32 VALU forms are switched off for device code on purpose: the compiler otherwise emits v_pk_*_f32
 # forms that have been seen to give wrong results on these machines
 FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950", "-Xclang", "-target-feature", "-Xclang",

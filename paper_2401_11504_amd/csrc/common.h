@@ -59,6 +59,13 @@ __device__ __forceinline__ float block_max(float x, float* red) {
     return t;
 }
 
+// 16 bytes from an address that is a multiple of 2
+struct __attribute__((packed, aligned(2))) any16_t { uint32_t w[4]; };
+__device__ __forceinline__ bf16x8_t load_any16(const bf16_t* p) {
+    const any16_t a = *(const any16_t*)p;
+    return __builtin_bit_cast(bf16x8_t, make_uint4(a.w[0], a.w[1], a.w[2], a.w[3]));
+}
+
 // eight bf16 in a 16-byte word <-> eight floats
 __device__ __forceinline__ void unpack8(uint4 r, float* f) {
     f[0] = bf16_to_f32(r.x & 0xffff); f[1] = bf16_to_f32(r.x >> 16);

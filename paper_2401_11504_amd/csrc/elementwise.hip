@@ -606,6 +606,7 @@ uint64_t dropout_key(uint64_t seed, int64_t step, int layer, int group) {
     const uint64_t stream_id = (1ull << 63) | ((uint64_t)step << 16) | ((uint64_t)layer << 3) | (uint64_t)group;
     return mix64(seed ^ mix64(stream_id));
 }
+uint64_t mix64_host(uint64_t z) { return mix64(z); }
 uint32_t dropout_threshold(float p) {
     const double t = floor((double)p * 4294967296.0);
     return t <= 0.0 ? 0u : (t >= 4294967295.0 ? 4294967295u : (uint32_t)t);

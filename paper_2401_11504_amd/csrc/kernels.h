@@ -250,3 +250,45 @@ struct Choose {
     float repetition, presence, frequency;
 };
 hipError_t launch_choose(const Choose& c, int rows, int vocab, float* ws, size_t ws_elems, hipStream_t s);
+// a token drawn from each row of logits (sample.hip); params [rows][4]: temperature, top-k, top-p, min-p, a stride of 0: one for all
+struct Sample {
+    const float* logits; long ldl;
+    const float* params; long ldp;
+    const float* u;
+    int* choice;
+    int* kept;                            // may be null
+    float* prob;                          // may be null
+    float now[4] = {}, now_u = 0.f;       // the settings and the number where params and u are null
+};
+uint64_t mix64_host(uint64_t z);          // the generator of the dropout masks (elementwise.hip)
+hipError_t launch_sample(const Sample& c, int rows, int vocab, float* ws, size_t ws_elems, hipStream_t s);
+
+// ---------------------------------------------------------------- key/value cache on pages (paged.hip, attn_weights.hip)
+struct Paged {                            // see paged.hip for the layout
+    bf16_t *k, *v;
+    const int* table;                     // [n_seqs][n_table]
+    int n_pages, shift, heads, d, n_seqs, n_table;      // page = 1 << shift
+};
+// row i of sequence s (rows first_row[s] .. first_row[s + 1] - 1; null: row s) into slot lengths[s] + i; weights and positions [n_seqs][heads][ldw], may be null
+hipError_t launch_paged_append(const Paged& c, const int* lengths, const bf16_t* k, long ldk, const bf16_t* v, long ldv, const int* first_row, int n_rows,
+                               const int* pos, float* weights, int* positions, long ldw, hipStream_t s);
+constexpr int PAGED_MAX_RANGES = 128;
+struct PagedWs {                          // scratch of the attention: scores [sequence][query head][ld_scores]; of each range a maximum and a sum, an output
+    float* scores = nullptr;
+    long ld_scores = 0;
+    float2* ml = nullptr;
+    float* o = nullptr;
+};
+struct PagedPlan {
+    int n_ranges = 1, range = 0;
+    size_t elems = 0, ml_at = 0, o_at = 0;
+};
+// elems may be more than ws_elems where weights are asked for: then ws_elems is too little
+PagedPlan attention_paged_plan(int max_len, int n_seqs, int heads, int kv_heads, int d, bool weights, size_t ws_elems);
+hipError_t launch_attention_paged(const Paged& c, const int* lengths, int max_len, const bf16_t* q, long ldq, int heads, bf16_t* o, long ldo, const float* w_in,
+                                  float* w_out, long ldw, float* ws, const PagedPlan& p, hipStream_t s);
+hipError_t launch_attention_weights(const bf16_t* q, long ldq, const bf16_t* k, long ldk, int T, int heads, int kv_heads, int d, int first_row, const float* lse,
+                                    const float* w_in, long ldi, float* w_out, long ldo, hipStream_t s);
+// ws: (2 * min(budget, slots a sequence can have - budget) + 1) ints for each sequence and key head
+hipError_t launch_paged_evict(const Paged& c, const int* lengths, int budget, int n_recent, const float* w_in, const int* p_in, long ldw, float* w_out,
+                              int* p_out, int* lengths_out, int* ws, hipStream_t s);

@@ -1,0 +1,491 @@
+// A key/value cache on pages: tokens of many texts go in, one new token of each attends, heads forget the tokens that got little attention.
+//   k, v [n_pages][heads][page][d] bf16; slot j of sequence s lies on page table[s][j / page] at j % page.  page is a power of two from 16 on, so
+// that 16 slots that begin at a multiple of 16 lie on one page.
+#include "kernels.h"
+
+typedef unsigned u32x2_t __attribute__((ext_vector_type(2)));
+typedef unsigned u32x4_t __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ int page_of(const Paged& c, int seq, int slot) {        // -1: not there
+    const int id = c.table[(long)seq * c.n_table + (slot >> c.shift)];
+    return id >= 0 && id < c.n_pages ? id : -1;
+}
+__device__ __forceinline__ long slot_at(const Paged& c, int id, int head, int slot) {        // of a head's first slot of 16, or any
+    return ((((long)id * c.heads + head) << c.shift) + (slot & ((1 << c.shift) - 1))) * c.d;
+}
+
+// ---------------------------------------------------------------- append
+// One workgroup a row of new tokens: 16 bytes of k and of v a thread at a time.
+__global__ __launch_bounds__(256) void paged_append_kernel(Paged c, const int* __restrict__ lengths, const bf16_t* __restrict__ k, long ldk,
+                                                           const bf16_t* __restrict__ v, long ldv, const int* __restrict__ first_row,
+                                                           const int* __restrict__ pos, float* __restrict__ weights, int* __restrict__ positions, long ldw) {
+    const int row = blockIdx.x;
+    int seq = row, at = 0;
+    if (first_row) {                      // the last sequence that begins at or before the row
+        int lo = 0, hi = c.n_seqs;        // (first_row[lo] <= row < first_row[hi], if it lies in any)
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (first_row[mid] <= row) lo = mid;
+            else hi = mid;
+        }
+        if (first_row[lo] > row || first_row[lo + 1] <= row) return;
+        seq = lo, at = row - first_row[lo];
+    }
+    const long slot = (long)max(lengths[seq], 0) + at;
+    if (slot >= (long)c.n_table << c.shift) return;
+    if (weights || positions) {
+        for (int h = threadIdx.x; h < c.heads && slot < ldw; h += 256) {
+            const long i = ((long)seq * c.heads + h) * ldw + slot;
+            if (weights) weights[i] = 0.f;
+            if (positions) positions[i] = pos ? pos[row] : (int)slot;
+        }
+    }
+    const int id = page_of(c, seq, (int)slot);
+    if (id < 0) return;
+    const int per = c.d >> 3, n = c.heads * per;
+    for (int i = threadIdx.x; i < n; i += 256) {
+        const int h = i / per, e = (i - h * per) * 8;
+        const any16_t kw = *(const any16_t*)(k + (long)row * ldk + h * c.d + e), vw = *(const any16_t*)(v + (long)row * ldv + h * c.d + e);
+        const long to = slot_at(c, id, h, (int)slot) + e;
+        *(uint4*)(c.k + to) = make_uint4(kw.w[0], kw.w[1], kw.w[2], kw.w[3]);
+        *(uint4*)(c.v + to) = make_uint4(vw.w[0], vw.w[1], vw.w[2], vw.w[3]);
+    }
+}
+hipError_t launch_paged_append(const Paged& c, const int* lengths, const bf16_t* k, long ldk, const bf16_t* v, long ldv, const int* first_row, int n_rows,
+                               const int* pos, float* weights, int* positions, long ldw, hipStream_t s) {
+    if (n_rows <= 0) return hipSuccess;
+    paged_append_kernel<<<n_rows, 256, 0, s>>>(c, lengths, k, ldk, v, ldv, first_row, pos, weights, positions, ldw);
+    return hipGetLastError();
+}
+
+// ---------------------------------------------------------------- attention of one new token of each sequence
+// The query heads that share a key head are columns, 16 to a workgroup; its waves take the workgroup's range of the keys in turn, 32 at a time:
+//   S^T[key][column] = K q^T   and   O^T[d][column] += V^T P^T     by v_mfma_f32_16x16x32_bf16
+// (lane = 16 g + m:  A: row m, contraction slots 8 g ..;  B: column m, the same slots;  D: column m, rows 4 g .. 4 g + 3).
+// A lane's scores are those of keys 4 g .. 4 g + 3 of either 16, and these are the slots that it has to bring as the second product's
+// operands, P as it holds it and the values as rows of V: it loads D / 16 neighbouring columns of each of its eight keys, and the matrix
+// product t takes the t-th column of every lane (row m of its result is column m D / 16 + t).  So both K and V come straight from memory as
+// they lie there, nothing goes through LDS, and nothing is exchanged between lanes but the maximum, and that only where it grows by 2^8.
+// Weights are split into two bf16 parts, cut off and rounded, so that they are off by 2^-15 of themselves (the matrix unit has nothing else to do
+// here); the second is above 0, so that an infinite value gives an infinity and not 0 times it.
+__device__ __forceinline__ f32x4_t mfma16(bf16x8_t a, bf16x8_t b, f32x4_t c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+template <int W> struct Words;
+template <> struct Words<4> { typedef u32x4_t type; };
+template <> struct Words<2> { typedef u32x2_t type; };
+
+constexpr int PAGED_NW = 4, PAGED_STEP = 32;
+template <int D, bool SCORES>
+__global__ __launch_bounds__(PAGED_NW * 64, 2) void attn_paged_kernel(Paged c, const int* __restrict__ lengths, int max_len, const bf16_t* __restrict__ q, long ldq,
+                                                                      int group, float scale_log2e, bf16_t* __restrict__ o, long ldo, PagedWs ws, int range,
+                                                                      int n_ranges) {
+    constexpr int NW = PAGED_NW, NST = D / 32, NT = D / 16, NV = D / 32, LDP = D + 4;
+    typedef typename Words<NV>::type vword_t;
+    __shared__ __align__(16) float part[NW][16 * LDP];     // a column's output, maximum and sum, wave by wave
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m16 = lane & 15, g = lane >> 4;
+    const int tiles = (group + 15) >> 4, heads = c.heads * group;
+    int idx = blockIdx.x;
+    const int ht = idx % (c.heads * tiles), head = ht / tiles, c0 = ht % tiles * 16, n_cols = min(16, group - c0);
+    idx /= c.heads * tiles;
+    const int split = idx % n_ranges, seq = idx / n_ranges;
+    const int len = min(max(lengths[seq], 0), max_len), k0 = split * range, kend = min(k0 + range, len);
+    if (k0 >= len && split > 0) return;
+    const long qh0 = (long)seq * heads + head * group + c0;
+
+    bf16x8_t qf[NST];
+    {
+        const bf16_t* qr = q + (long)seq * ldq + (long)(head * group + c0 + min(m16, n_cols - 1)) * D + g * 8;
+#pragma unroll
+        for (int st = 0; st < NST; ++st) qf[st] = load_any16(qr + st * 32);
+    }
+    f32x4_t oacc[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) oacc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, l = 0.f;
+    bool any = false;
+
+    const int n_steps = max(0, (kend - k0 - wave * PAGED_STEP + NW * PAGED_STEP - 1) / (NW * PAGED_STEP));
+    auto key_of = [&](int i) { return k0 + (i * NW + wave) * PAGED_STEP; };
+    int ids = -1;                                          // lane 2 i + t: the page of the wave's 16 keys t of its i-th step of 32 steps
+    auto pages = [&](int i0) {
+        const int key = key_of(i0 + (lane >> 1)) + (lane & 1) * 16;
+        ids = key < kend ? page_of(c, seq, key) : -1;
+    };
+    u32x4_t kr[2][NST];
+    vword_t vr[8];
+    const int k_lane = m16 * D + g * 8, v_lane = g * 4 * D + m16 * NT;
+    int id[2], id_next[2];
+    auto pick = [&](int i) {
+        id_next[0] = __builtin_amdgcn_readlane(ids, 2 * (i & 31));
+        id_next[1] = __builtin_amdgcn_readlane(ids, 2 * (i & 31) + 1);
+    };
+    auto keys = [&](int i) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const bf16_t* p = c.k + slot_at(c, max(id_next[t], 0), head, key_of(i) + 16 * t);
+#pragma unroll
+            for (int st = 0; st < NST; ++st) kr[t][st] = __builtin_nontemporal_load((const u32x4_t*)(p + k_lane + st * 32));
+        }
+    };
+    auto values = [&](int i) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const bf16_t* p = c.v + slot_at(c, max(id_next[t], 0), head, key_of(i) + 16 * t);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) vr[4 * t + e] = __builtin_nontemporal_load((const vword_t*)(p + v_lane + e * D));
+        }
+    };
+    if (n_steps > 0) {
+        pages(0);
+        pick(0);
+        keys(0);
+        values(0);
+    }
+    for (int i = 0; i < n_steps; ++i) {
+        const int key0 = key_of(i);
+        id[0] = id_next[0], id[1] = id_next[1];
+        f32x4_t s[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            s[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int st = 0; st < NST; ++st) s[t] = mfma16(__builtin_bit_cast(bf16x8_t, kr[t][st]), qf[st], s[t]);
+        }
+        if (i + 1 < n_steps) {
+            if ((i + 1 & 31) == 0) pages(i + 1);
+            pick(i + 1);
+            keys(i + 1);
+        }
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = s[e >> 2][e & 3] * scale_log2e;
+        const bool full = key0 + 32 <= kend && id[0] >= 0 && id[1] >= 0;        // (uniform)
+        if (!full) {
+            const vword_t none = {};
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const bool there = key0 + 16 * (e >> 2) + 4 * g + (e & 3) < kend && id[e >> 2] >= 0;
+                x[e] = there ? x[e] : -INFINITY;
+                vr[e] = there ? vr[e] : none;              // (a weight of 0 does not take an infinity or NaN away)
+            }
+            any |= id[0] >= 0 || (id[1] >= 0 && key0 + 16 < kend);
+        } else {
+            any = true;
+        }
+        if constexpr (SCORES) {
+            if (m16 < n_cols) {
+                float* to = ws.scores + (qh0 + m16) * ws.ld_scores + key0 + 4 * g;
+                *(f32x4_t*)to = f32x4_t{x[0], x[1], x[2], x[3]};
+                *(f32x4_t*)(to + 16) = f32x4_t{x[4], x[5], x[6], x[7]};
+            }
+        }
+        float top = x[0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) top = fmaxf(top, x[e]);
+        if (__builtin_amdgcn_ballot_w64(top > m + 8.f)) {
+            top = fmaxf(top, __shfl_xor(top, 16, 64));
+            top = fmaxf(top, __shfl_xor(top, 32, 64));
+            const float mn = fmaxf(m, top), alpha = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+            m = mn;
+            l *= alpha;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) oacc[t] *= alpha;
+        }
+        const float base = m == -INFINITY ? 0.f : m;
+        u32x4_t hi_w;
+        bf16x8_t lo;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            x[e] = __builtin_amdgcn_exp2f(x[e] - base);
+            l += x[e];
+            lo[e] = (__bf16)fmaxf(x[e] - __uint_as_float(__float_as_uint(x[e]) & 0xffff0000u), 0x1p-126f);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) hi_w[e] = __builtin_amdgcn_perm(__float_as_uint(x[2 * e + 1]), __float_as_uint(x[2 * e]), 0x07060302u);
+        const bf16x8_t hi = __builtin_bit_cast(bf16x8_t, hi_w);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            u32x4_t w;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                w[e] = __builtin_amdgcn_perm(vr[2 * e + 1][t >> 1], vr[2 * e][t >> 1], t & 1 ? 0x07060302u : 0x05040100u);
+            const bf16x8_t a = __builtin_bit_cast(bf16x8_t, w);
+            oacc[t] = mfma16(a, hi, oacc[t]);
+            oacc[t] = mfma16(a, lo, oacc[t]);
+        }
+        if (i + 1 < n_steps) values(i + 1);
+    }
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    if (any && m == -INFINITY) l = NAN;                    // keys, and none whose score is above -infinity: 0 / 0
+    if (m16 < n_cols) {
+        float* mine = part[wave] + m16 * LDP;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int t = 0; t < NT; t += 4)
+                *(f32x4_t*)(mine + (4 * g + r) * NT + t) = f32x4_t{oacc[t][r], oacc[t + 1][r], oacc[t + 2][r], oacc[t + 3][r]};
+        if (g == 0) { mine[D] = m; mine[D + 1] = l; }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < n_cols * D; i += NW * 64) {
+        const int cc = i / D, e = i % D;
+        float mt = -INFINITY, lt = 0.f, ot = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) mt = fmaxf(mt, part[w][cc * LDP + D]);
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const float* p = part[w] + cc * LDP;
+            const float a = mt == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(p[D] - mt);
+            if (a != 0.f) lt += a * p[D + 1], ot += a * p[e];
+        }
+        if (n_ranges == 1) o[(long)seq * ldo + (long)(head * group + c0 + cc) * D + e] = f32_to_bf16(lt == 0.f ? 0.f : ot / lt);
+        else ws.o[((qh0 + cc) * n_ranges + split) * D + e] = ot;
+        if (e == 0 && (SCORES || n_ranges > 1)) ws.ml[(qh0 + cc) * n_ranges + split] = make_float2(mt, lt);
+    }
+}
+
+// The largest score and the sum of weights over a query head's live ranges, in every lane of the wave.
+__device__ __forceinline__ float2 join_ml(const float2* ml, int live, int lane) {
+    float top = -INFINITY, sum = 0.f;
+    for (int i = lane; i < live; i += 64) top = fmaxf(top, ml[i].x);
+    top = wave_max(top);
+    for (int i = lane; i < live; i += 64) {
+        const float a = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml[i].x - top);
+        if (a != 0.f) sum += a * ml[i].y;
+    }
+    return make_float2(top, wave_sum(sum));
+}
+// Behind the ranges: the first n_join workgroups join the outputs, 256 / D query heads each, the others add what 1024 slots of a key head got:
+//   weights_out[slot] = weights_in[slot] + the sum over the group's query heads of 2^(x - log2 of the sum of weights)
+template <int D>
+__global__ __launch_bounds__(256) void paged_join_kernel(Paged c, const int* __restrict__ lengths, int max_len, int group, bf16_t* __restrict__ o, long ldo,
+                                                         PagedWs ws, int range, int n_ranges, int n_join, const float* w_in, float* w_out, long ldw, int n_chunks) {
+    const int heads = c.heads * group, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if ((int)blockIdx.x < n_join) {
+        const long qh = (long)blockIdx.x * (256 / D) + threadIdx.x / D;
+        if (qh >= (long)c.n_seqs * heads) return;
+        const int seq = qh / heads, e = threadIdx.x % D, len = min(max(lengths[seq], 0), max_len), live = (len + range - 1) / range;
+        const float2* ml = ws.ml + qh * n_ranges;
+        const float2 all = join_ml(ml, live, lane);
+        float ot = 0.f;
+        for (int i = 0; i < live; ++i) {
+            const float a = all.x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml[i].x - all.x);
+            if (a != 0.f) ot += a * ws.o[(qh * n_ranges + i) * D + e];
+        }
+        o[(long)seq * ldo + qh % heads * D + e] = f32_to_bf16(all.y == 0.f ? 0.f : ot / all.y);
+        return;
+    }
+    int idx = blockIdx.x - n_join;
+    const int chunk = idx % n_chunks, sh = idx / n_chunks, seq = sh / c.heads, head = sh % c.heads;
+    const int len = min(max(lengths[seq], 0), max_len), live = (len + range - 1) / range, key = chunk * 1024 + threadIdx.x * 4;
+    if (chunk * 1024 >= len) return;
+    __shared__ float lse[64];
+    float got[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int g0 = 0; g0 < group; g0 += 64) {
+        const int n = min(64, group - g0);
+        const long qh = (long)seq * heads + head * group + g0;
+        __syncthreads();
+        for (int j = wave; j < n; j += 4) {
+            const float2 all = join_ml(ws.ml + (qh + j) * n_ranges, live, lane);
+            if (lane == 0) lse[j] = all.y == 0.f ? INFINITY : all.x + __log2f(all.y);
+        }
+        __syncthreads();
+        if (key < len) {
+            for (int j = 0; j < n; ++j) {
+                const f32x4_t x = *(const f32x4_t*)(ws.scores + (qh + j) * ws.ld_scores + key);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) got[e] += __builtin_amdgcn_exp2f(x[e] - lse[j]);
+            }
+        }
+    }
+    const long at = ((long)seq * c.heads + head) * ldw + key;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (key + e < len) w_out[at + e] = (w_in ? w_in[at + e] : 0.f) + got[e];
+}
+
+static size_t round4(size_t n) { return (n + 3) & ~(size_t)3; }
+PagedPlan attention_paged_plan(int max_len, int n_seqs, int heads, int kv_heads, int d, bool weights, size_t ws_elems) {
+    const int group = heads / kv_heads, unit = PAGED_NW * PAGED_STEP;
+    const long groups = (long)n_seqs * kv_heads * ((group + 15) / 16), rows = (long)n_seqs * heads;
+    const size_t scores = weights ? (size_t)rows * (size_t)(((long)max_len + 31) & ~31L) : 0;
+    const int most = (int)((max_len + unit - 1L) / unit);
+    PagedPlan p;
+    int n = (int)(1024 / groups < 1 ? 1 : 1024 / groups);
+    if (n_seqs > 1 && n < 4) n = 4;
+    n = n > most ? most : n;
+    n = n > PAGED_MAX_RANGES ? PAGED_MAX_RANGES : n;
+    for (;; --n) {
+        if (n < 1) n = 1;
+        p.range = (int)(((long)max_len + n - 1) / n + unit - 1) / unit * unit;
+        if (p.range < unit) p.range = unit;
+        p.n_ranges = (int)((max_len + (long)p.range - 1) / p.range);
+        if (p.n_ranges < 1) p.n_ranges = 1;
+        const size_t ml = weights || p.n_ranges > 1 ? round4((size_t)rows * p.n_ranges * 2) : 0, part = p.n_ranges > 1 ? (size_t)rows * p.n_ranges * d : 0;
+        p.elems = scores + ml + part;
+        p.ml_at = scores;
+        p.o_at = scores + ml;
+        if (p.elems <= ws_elems || n == 1) return p;
+    }
+}
+hipError_t launch_attention_paged(const Paged& c, const int* lengths, int max_len, const bf16_t* q, long ldq, int heads, bf16_t* o, long ldo, const float* w_in,
+                                  float* w_out, long ldw, float* ws, const PagedPlan& p, hipStream_t s) {
+    const int group = heads / c.heads, tiles = (group + 15) / 16;
+    const float scale = 1.44269504088896340736f / sqrtf((float)c.d);
+    PagedWs w;
+    if (p.elems) {
+        w.scores = ws;
+        w.ld_scores = ((long)max_len + 31) & ~31L;
+        w.ml = (float2*)(ws + p.ml_at);
+        w.o = ws + p.o_at;
+    }
+    const int grid = c.n_seqs * c.heads * tiles * p.n_ranges;
+    auto attend = [&](auto kernel) { kernel<<<grid, PAGED_NW * 64, 0, s>>>(c, lengths, max_len, q, ldq, group, scale, o, ldo, w, p.range, p.n_ranges); };
+    if (c.d == 128) w_out ? attend(attn_paged_kernel<128, true>) : attend(attn_paged_kernel<128, false>);
+    else w_out ? attend(attn_paged_kernel<64, true>) : attend(attn_paged_kernel<64, false>);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || (!w_out && p.n_ranges == 1)) return e;
+    const int n_join = p.n_ranges > 1 ? cdiv((long)c.n_seqs * heads, 256 / c.d) : 0, n_chunks = w_out ? cdiv(max_len, 1024) : 0;
+    auto join = [&](auto kernel) {
+        kernel<<<n_join + c.n_seqs * c.heads * n_chunks, 256, 0, s>>>(c, lengths, max_len, group, o, ldo, w, p.range, p.n_ranges, n_join, w_in, w_out, ldw, n_chunks);
+    };
+    if (c.d == 128) join(paged_join_kernel<128>);
+    else join(paged_join_kernel<64>);
+    return hipGetLastError();
+}
+
+// ---------------------------------------------------------------- eviction
+// One workgroup a sequence and key head: which slots stay.  The order: recent tokens, larger weights, lower slots; the budget-th of it is
+// found digit by digit (11, 11 and 10 bits) by counts of a key that has the same order.  Kept slots below the budget stay where they are; the
+// i-th slot that becomes free there receives the i-th kept one from behind.  The pairs go to ws: [count or ~length][from .., to ..].
+__device__ __forceinline__ unsigned order_key(float w) {
+    const unsigned u = __float_as_uint(w + 0.f);           // (-0 counts as 0)
+    return w != w ? 0u : u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+constexpr int EVICT_NT = 1024;
+__global__ __launch_bounds__(EVICT_NT) void evict_select_kernel(Paged c, const int* __restrict__ lengths, int budget, int n_recent, const float* w_in,
+                                                                const int* p_in, long ldw, float* w_out, int* p_out, int* __restrict__ ws, long ws_ld) {
+    constexpr int NT = EVICT_NT, NWV = NT / 64;
+    __shared__ int hist[2048];
+    __shared__ int sums[3][NWV];
+    __shared__ int found[2];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, seq = blockIdx.x / c.heads;
+    const long row = (long)blockIdx.x * ldw;
+    int* list = ws + (long)blockIdx.x * ws_ld;
+    const int len = (int)min((long)max(lengths[seq], 0), min(ldw, (long)c.n_table << c.shift));
+    if (len <= budget) {
+        if (tid == 0) list[0] = ~len;
+        for (int i = tid; i < len; i += NT) {
+            if (w_out != w_in) w_out[row + i] = w_in[row + i];
+            if (p_out != p_in) p_out[row + i] = p_in[row + i];
+        }
+        return;
+    }
+    int newest = -0x7fffffff - 1;
+    for (int i = tid; i < len; i += NT) newest = max(newest, p_in[row + i]);
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) newest = max(newest, __shfl_xor(newest, off, 64));
+    if (lane == 0) sums[0][wave] = newest;
+    __syncthreads();
+    for (int w = 0; w < NWV; ++w) newest = max(newest, sums[0][w]);
+    const long border = (long)newest - n_recent;
+    auto key_of = [&](int i) -> unsigned {
+        if (page_of(c, seq, i) < 0) return 0u;
+        return (long)p_in[row + i] > border ? 0xffffffffu : order_key(w_in[row + i]);
+    };
+    unsigned prefix = 0;
+    int need = budget;                                     // of the slots whose key begins with the prefix, so many stay
+    for (int d = 0; d < 3; ++d) {
+        const int shift = d == 0 ? 21 : d == 1 ? 10 : 0, bins = d == 2 ? 1024 : 2048;
+        __syncthreads();
+        for (int i = tid; i < 2048; i += NT) hist[i] = 0;
+        __syncthreads();
+        const int above = d == 0 ? 32 : d == 1 ? 21 : 10;
+        for (int i = tid; i < len; i += NT) {
+            const unsigned key = key_of(i);
+            if (d == 0 || key >> above == prefix >> above) atomicAdd(&hist[key >> shift & (bins - 1)], 1);
+        }
+        __syncthreads();
+        // from the top: thread t has the two bins bins - 1 - 2 t and the one below
+        const int hi = bins - 1 - 2 * tid, a = hi >= 0 ? hist[hi] : 0, b = hi >= 1 ? hist[hi - 1] : 0;
+        int run = a + b;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const int o = __shfl_up(run, off, 64);
+            if (lane >= off) run += o;
+        }
+        if (lane == 63) sums[0][wave] = run;
+        __syncthreads();
+        for (int w = 0; w < wave; ++w) run += sums[0][w];
+        const int before = run - a - b;
+        if (a && before < need && need <= before + a) found[0] = hi, found[1] = need - before;
+        if (b && before + a < need && need <= run) found[0] = hi - 1, found[1] = need - before - a;
+        __syncthreads();
+        prefix |= (unsigned)found[0] << shift;
+        need = found[1];
+    }
+    // in the order of the slots: equal keys, slots that become free below the budget, kept ones behind it
+    int n_equal = 0, n_free = 0, n_move = 0;
+    for (int i0 = 0; i0 < len; i0 += NT) {
+        const int i = i0 + tid;
+        const unsigned key = i < len ? key_of(i) : 0u;
+        const bool equal = i < len && key == prefix;
+        const unsigned long long below = (1ull << lane) - 1, eq = __ballot(equal);
+        __syncthreads();
+        if (lane == 0) sums[0][wave] = __popcll(eq);
+        __syncthreads();
+        int rank = n_equal + __popcll(eq & below);
+        for (int w = 0; w < wave; ++w) rank += sums[0][w];
+        const bool keep = i < len && (key > prefix || (equal && rank < need));
+        const bool free = i < len && i < budget && !keep, move = keep && i >= budget;
+        const unsigned long long fr = __ballot(free), mv = __ballot(move);
+        if (lane == 0) sums[1][wave] = __popcll(fr), sums[2][wave] = __popcll(mv);
+        __syncthreads();
+        int f = n_free + __popcll(fr & below), m = n_move + __popcll(mv & below);
+        for (int w = 0; w < wave; ++w) f += sums[1][w], m += sums[2][w];
+        const long most = (ws_ld - 1) >> 1;
+        if (free && f < most) list[1 + most + f] = i;
+        if (move && m < most) list[1 + m] = i;
+        if (i < budget && keep) {
+            if (w_out != w_in) w_out[row + i] = w_in[row + i];
+            if (p_out != p_in) p_out[row + i] = p_in[row + i];
+        }
+        for (int w = 0; w < NWV; ++w) n_equal += sums[0][w], n_free += sums[1][w], n_move += sums[2][w];
+    }
+    __threadfence_block();
+    __syncthreads();
+    const long most = (ws_ld - 1) >> 1;
+    for (int i = tid; i < n_move; i += NT) {               // (as many become free as move)
+        const int from = list[1 + i], to = list[1 + most + i];
+        w_out[row + to] = w_in[row + from];
+        p_out[row + to] = p_in[row + from];
+    }
+    if (tid == 0) list[0] = n_move;
+}
+// The rows of the pairs, D / 8 lanes each for k and for v, 32 pairs a workgroup; and the new lengths.
+__global__ __launch_bounds__(256) void evict_move_kernel(Paged c, int budget, const int* __restrict__ ws, long ws_ld, int* __restrict__ lengths_out, int n_chunks) {
+    const int sh = blockIdx.x / n_chunks, chunk = blockIdx.x % n_chunks, seq = sh / c.heads, head = sh % c.heads;
+    const int* list = ws + (long)sh * ws_ld;
+    const int n = list[0];
+    if (head == 0 && chunk == 0 && threadIdx.x == 0) lengths_out[seq] = n < 0 ? ~n : budget;
+    const long most = (ws_ld - 1) >> 1;
+    const int per = c.d >> 3, pairs = 128 / per, which = threadIdx.x / (2 * per), part = threadIdx.x % (2 * per);
+    bf16_t* at = part < per ? c.k : c.v;
+    const int e = part % per * 8;
+    for (long i0 = chunk * 32L; i0 < n; i0 += n_chunks * 32L) {
+        for (long i = i0 + which; i < min((long)n, i0 + 32); i += pairs) {
+            const int from = list[1 + i], to = list[1 + most + i], a = page_of(c, seq, from), b = page_of(c, seq, to);
+            if (a >= 0 && b >= 0) *(uint4*)(at + slot_at(c, b, head, to) + e) = *(const uint4*)(at + slot_at(c, a, head, from) + e);
+        }
+    }
+}
+hipError_t launch_paged_evict(const Paged& c, const int* lengths, int budget, int n_recent, const float* w_in, const int* p_in, long ldw, float* w_out,
+                              int* p_out, int* lengths_out, int* ws, hipStream_t s) {
+    const long cap = (long)c.n_table << c.shift, width = cap < ldw ? cap : ldw;
+    const long most = width - budget < budget ? (width - budget > 0 ? width - budget : 0) : budget, ld = 1 + 2 * most;
+    evict_select_kernel<<<c.n_seqs * c.heads, EVICT_NT, 0, s>>>(c, lengths, budget, n_recent, w_in, p_in, ldw, w_out, p_out, ws, ld);
+    const long room = (1L << 24) / ((long)c.n_seqs * c.heads);
+    const int n_chunks = most > 0 ? (int)(cdiv(most, 32) < room ? cdiv(most, 32) : room < 1 ? 1 : room) : 1;
+    evict_move_kernel<<<c.n_seqs * c.heads * n_chunks, 256, 0, s>>>(c, budget, ws, ld, lengths_out, n_chunks);
+    return hipGetLastError();
+}

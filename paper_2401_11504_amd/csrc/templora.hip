@@ -190,6 +190,10 @@ struct tl_lora {
     float* bias = nullptr;        // [vocab]
     unsigned* allowed = nullptr;  // [ceil(vocab / 32)]
     float* choose_ws = nullptr;
+    bool sampling = false;
+    tl_sampling smp = {0.f, 0, 1.f, 0.f, 0};
+    uint64_t drawn = 0;           // tokens drawn since tl_set_sampling
+    float* shaped = nullptr;      // [vocab] the logits behind penalties, bias and mask
     float* lora_h = nullptr;      // [3 r] scaled low-rank activations of the projection group in flight
     float* dec_raw = nullptr;     // [max(3 d, 2 f)] frozen part of one token's q|k|v or gate|up
     float* dec_part = nullptr;    // shares of A o (one per head) or A_down act (one per DECODE_SW columns), r each
@@ -974,6 +978,7 @@ static tl_status copy_out(tl_lora* L, float* host_out, const float* src, size_t 
     return TL_OK;
 }
 
+static constexpr int32_t kMostSampled = 1 << 22;      // tokens of a vocabulary that is drawn from: indices and sums of weights fit their bits
 static size_t choose_ws_elems(int vocab) { return (size_t)2 * cdiv(vocab, 1024); }
 // the first n rows of a layer's bf16 cache into its 8-bit one
 static tl_status append_8bit(tl_lora* L, int l, const bf16_t* qkv, int n) {
@@ -1015,9 +1020,17 @@ static tl_status emit_next(tl_lora* L, const float* h_last, int n_text, int32_t*
             HIPCHK(launch_token_counts(L->text + n_text - n, n, 1, n, c.vocab, 0, L->counts, c.vocab, s));
         }
         const Choose ch{L->logits, 0, L->penalties ? L->counts : nullptr, 0, L->biased ? L->bias : nullptr, 0, L->masked ? L->allowed : nullptr, 0,
-                        nullptr, 0, L->next_host, L->pen.repetition, L->pen.presence, L->pen.frequency};
+                        L->sampling ? L->shaped : nullptr, 0, L->sampling ? nullptr : L->next_host, L->pen.repetition, L->pen.presence, L->pen.frequency};
         HIPCHK(launch_choose(ch, 1, c.vocab, L->choose_ws, choose_ws_elems(c.vocab), s));
-    } else {
+    }
+    if (L->sampling) {
+        Sample sm{};
+        sm.logits = L->penalties || L->biased || L->masked ? L->shaped : L->logits;
+        sm.choice = L->next_host;
+        sm.now[0] = L->smp.temperature, sm.now[1] = (float)L->smp.top_k, sm.now[2] = L->smp.top_p, sm.now[3] = L->smp.min_p;
+        sm.now_u = (float)(mix64_host(mix64_host(L->smp.seed) + L->drawn) >> 40) * 0x1p-24f;
+        HIPCHK(launch_sample(sm, 1, c.vocab, nullptr, 0, s));
+    } else if (!(L->penalties || L->biased || L->masked)) {
         HIPCHK(launch_argmax(L->logits, c.vocab, L->next_host, s));
     }
     HIPCHK(hipStreamSynchronize(s));
@@ -1025,6 +1038,7 @@ static tl_status emit_next(tl_lora* L, const float* h_last, int n_text, int32_t*
     const int next = L->next_host[0];
     if (next < 0 || next >= c.vocab) return fail(TL_ERR_ARG, "no token to choose: none is allowed, or the values of all allowed ones are undefined");
     if (logits_out) TLCHK(copy_out(L, logits_out, L->logits, c.vocab));
+    if (L->sampling) ++L->drawn;
     *next_token = next;
     return TL_OK;
 }
@@ -1202,6 +1216,23 @@ extern "C" tl_status tl_set_penalties(tl_lora* L, const tl_penalties* p) {
     TLCHK(choice_buffers(L, "tl_set_penalties"));
     L->pen = c;
     L->penalties = true;
+    return TL_OK;
+}
+extern "C" tl_status tl_set_sampling(tl_lora* L, const tl_sampling* p) {
+    LIVE(L, "tl_set_sampling");
+    if (!p) {
+        L->sampling = false;
+        return TL_OK;
+    }
+    const tl_sampling c = *p;
+    if (!(c.temperature >= 0.f) || !std::isfinite(c.temperature) || c.top_k < 0 || !std::isfinite(c.top_p) || !std::isfinite(c.min_p))
+        return fail(TL_ERR_ARG, "tl_set_sampling: temperature %g (0 or more), top_k %d (0 or more), top_p %g, min_p %g", c.temperature, c.top_k, c.top_p, c.min_p);
+    const int V = L->model->cfg.vocab;
+    if (V <= 0 || V > kMostSampled) return fail(TL_ERR_SHAPE, "tl_set_sampling: vocab = %d outside [1, 2^22]", V);
+    if (!L->shaped) TLCHK(L->pool.alloc(&L->shaped, (size_t)V));
+    L->smp = c;
+    L->sampling = true;
+    L->drawn = 0;
     return TL_OK;
 }
 extern "C" tl_status tl_set_bias(tl_lora* L, const float* bias) {
@@ -1916,6 +1947,95 @@ extern "C" tl_status tl_k_choose(const float* logits, int32_t ldl, int32_t rows,
         return fail(TL_ERR_ARG, "tl_k_choose: repetition %g (above 0), presence %g, frequency %g", repetition, presence, frequency);
     const Choose c{logits, ldl, counts, ldc, bias, ldb, allowed, lda, out, ldo, choice, repetition, presence, frequency};
     HIPCHK(launch_choose(c, rows, vocab, workspace, workspace_elems, (hipStream_t)hip_stream));
+    return TL_OK;
+}
+extern "C" tl_status tl_k_sample(const float* logits, int32_t ldl, int32_t rows, int32_t vocab, const float* params, int32_t ldp, const float* u,
+                                 int32_t* choice, int32_t* kept, float* prob, float* workspace, size_t workspace_elems, void* hip_stream) {
+    KARGS_OK(((logits && params && u && choice) || rows == 0) && rows >= 0 && vocab >= 1 && vocab <= kMostSampled && (rows <= 1 || ldl >= vocab) &&
+                 (rows <= 1 || ldp == 0 || ldp >= 4), "tl_k_sample");
+    Sample c{};
+    c.logits = logits, c.ldl = ldl, c.params = params, c.ldp = ldp, c.u = u, c.choice = choice, c.kept = kept, c.prob = prob;
+    HIPCHK(launch_sample(c, rows, vocab, workspace, workspace ? workspace_elems : 0, (hipStream_t)hip_stream));
+    return TL_OK;
+}
+// what every call on a cache on pages needs of it
+static tl_status paged_of(const tl_paged_mem* m, const char* name, Paged* out) {
+    if (!m || !m->k || !m->v || !m->table) return fail(TL_ERR_ARG, "%s: null pointer", name);
+    if (((uintptr_t)m->k | (uintptr_t)m->v) & 15) return fail(TL_ERR_ARG, "%s: pages start at multiples of 16 bytes", name);
+    const int32_t page = m->page_size;
+    if (m->n_kv_heads < 1 || m->n_kv_heads > 4096 || (m->d_head != 64 && m->d_head != 128) || page < 16 || page > 65536 || (page & (page - 1)) || m->n_pages < 1 ||
+        m->n_pages > kMost || m->n_seqs < 0 || m->n_seqs > 65536 || (int64_t)m->n_seqs * m->n_kv_heads > 1 << 24 || m->n_table < 1 || (int64_t)m->n_table * page > kMost)
+        return fail(TL_ERR_ARG, "%s: %d heads of %d, %d pages of %d, %d sequences of up to %d", name, m->n_kv_heads, m->d_head, m->n_pages, page, m->n_seqs, m->n_table);
+    int shift = 4;
+    while (1 << shift < page) ++shift;
+    *out = Paged{m->k, m->v, m->table, m->n_pages, shift, m->n_kv_heads, m->d_head, m->n_seqs, m->n_table};
+    return TL_OK;
+}
+extern "C" tl_status tl_k_paged_append(const tl_paged_mem* cache, const int32_t* lengths, const uint16_t* k, int32_t ldk, const uint16_t* v, int32_t ldv,
+                                       const int32_t* first_row, int32_t n_rows, const int32_t* pos, float* weights, int32_t* positions, int32_t ldw,
+                                       void* hip_stream) {
+    Paged c;
+    TLCHK(paged_of(cache, "tl_k_paged_append", &c));
+    const int64_t width = (int64_t)c.heads * c.d;
+    KARGS_OK(n_rows >= 0 && n_rows <= kMost && ((lengths && k && v) || n_rows == 0) && (n_rows <= 1 || (ldk >= width && ldv >= width)) &&
+                 (first_row ? c.n_seqs > 0 || n_rows == 0 : n_rows <= c.n_seqs) && ((!weights && !positions) || ldw >= 1), "tl_k_paged_append");
+    HIPCHK(launch_paged_append(c, lengths, k, ldk, v, ldv, first_row, n_rows, pos, weights, positions, ldw, (hipStream_t)hip_stream));
+    return TL_OK;
+}
+// sizes of an attention over pages
+static bool attention_paged_ok(int64_t max_len, int64_t n_seqs, int64_t n_heads, int64_t n_kv_heads) {
+    return max_len >= 1 && max_len <= kMost && n_seqs >= 0 && n_seqs <= 65536 && n_heads >= 1 && n_heads <= 65536 && n_heads % n_kv_heads == 0 &&
+           n_seqs * n_heads <= 1 << 24;
+}
+extern "C" tl_status tl_k_attention_paged(const tl_paged_mem* cache, const int32_t* lengths, int32_t max_len, const uint16_t* q, int32_t ldq, int32_t n_heads,
+                                          uint16_t* o, int32_t ldo, const float* weights_in, float* weights_out, int32_t ldw, float* workspace,
+                                          size_t workspace_elems, void* hip_stream) {
+    Paged c;
+    TLCHK(paged_of(cache, "tl_k_attention_paged", &c));
+    KARGS_OK(((lengths && q && o) || c.n_seqs == 0) && attention_paged_ok(max_len, c.n_seqs, n_heads, c.heads) &&
+                 (c.n_seqs <= 1 || ((int64_t)ldq >= (int64_t)n_heads * c.d && (int64_t)ldo >= (int64_t)n_heads * c.d)) && (weights_out || !weights_in) &&
+                 (!weights_out || ldw >= max_len), "tl_k_attention_paged");
+    if (max_len > (int64_t)c.n_table << c.shift) return fail(TL_ERR_WINDOW, "tl_k_attention_paged: %d keys, room for %d pages of %d", max_len, c.n_table, 1 << c.shift);
+    if (c.n_seqs == 0) return TL_OK;
+    const PagedPlan p = attention_paged_plan(max_len, c.n_seqs, n_heads, c.heads, c.d, weights_out != nullptr, workspace ? workspace_elems : 0);
+    if (p.elems > (workspace ? workspace_elems : 0))
+        return fail(TL_ERR_SHAPE, "tl_k_attention_paged: weights need a workspace of %zu floats at least", p.elems);
+    HIPCHK(launch_attention_paged(c, lengths, max_len, q, ldq, n_heads, o, ldo, weights_in, weights_out, ldw, workspace, p, (hipStream_t)hip_stream));
+    return TL_OK;
+}
+extern "C" tl_status tl_k_attention_paged_plan(int32_t max_len, int32_t n_seqs, int32_t n_heads, int32_t n_kv_heads, int32_t d_head, int32_t weights,
+                                               size_t workspace_elems, int32_t* n_ranges_out, size_t* elems_out) {
+    KARGS_OK(n_ranges_out && elems_out && n_kv_heads >= 1 && n_kv_heads <= 4096 && attention_paged_ok(max_len, n_seqs, n_heads, n_kv_heads) && n_seqs >= 1 &&
+                 (d_head == 64 || d_head == 128), "tl_k_attention_paged_plan");
+    const PagedPlan p = attention_paged_plan(max_len, n_seqs, n_heads, n_kv_heads, d_head, weights != 0, workspace_elems);
+    *n_ranges_out = p.n_ranges;
+    *elems_out = p.elems;
+    return TL_OK;
+}
+extern "C" tl_status tl_k_attention_weights(const uint16_t* q, int32_t ldq, const uint16_t* k, int32_t ldk, int32_t T, int32_t n_heads, int32_t n_kv_heads,
+                                            int32_t d_head, int32_t first_row, const float* lse, const float* weights_in, int32_t ldi, float* weights_out,
+                                            int32_t ldo, void* hip_stream) {
+    KARGS_OK(T >= 0 && T <= kMost && ((q && k && lse && weights_out) || T == 0) && n_kv_heads >= 1 && n_kv_heads <= 4096 && n_heads >= 1 && n_heads <= 65536 &&
+                 n_heads % n_kv_heads == 0 && (d_head == 64 || d_head == 128) && first_row >= 0 && ldq < 1 << 25 &&
+                 (T <= 1 || ((int64_t)ldq >= (int64_t)n_heads * d_head && (int64_t)ldk >= (int64_t)n_kv_heads * d_head)) &&
+                 (n_kv_heads == 1 || (ldo >= T && (!weights_in || ldi >= T))) && (weights_in != weights_out || !weights_in || n_kv_heads == 1 || ldi == ldo),
+             "tl_k_attention_weights");
+    HIPCHK(launch_attention_weights(q, ldq, k, ldk, T, n_heads, n_kv_heads, d_head, first_row, lse, weights_in, ldi, weights_out, ldo, (hipStream_t)hip_stream));
+    return TL_OK;
+}
+extern "C" tl_status tl_k_paged_evict(const tl_paged_mem* cache, const int32_t* lengths, int32_t budget, int32_t n_recent, const float* weights,
+                                      const int32_t* positions, int32_t ldw, float* weights_out, int32_t* positions_out, int32_t* lengths_out,
+                                      float* workspace, size_t workspace_elems, void* hip_stream) {
+    Paged c;
+    TLCHK(paged_of(cache, "tl_k_paged_evict", &c));
+    KARGS_OK(((lengths && weights && positions && weights_out && positions_out && lengths_out) || c.n_seqs == 0) && budget >= 1 && n_recent >= 0 && ldw >= 1,
+             "tl_k_paged_evict");
+    const int64_t cap = (int64_t)c.n_table << c.shift, width = std::min<int64_t>(cap, ldw), most = std::max<int64_t>(0, std::min<int64_t>(budget, width - budget));
+    const size_t need = (size_t)c.n_seqs * c.heads * (2 * most + 1);
+    if (c.n_seqs == 0) return TL_OK;
+    if (!workspace || workspace_elems < need) return fail(TL_ERR_SHAPE, "tl_k_paged_evict: needs a workspace of %zu floats", need);
+    HIPCHK(launch_paged_evict(c, lengths, budget, n_recent, weights, positions, ldw, weights_out, positions_out, lengths_out, (int*)workspace,
+                              (hipStream_t)hip_stream));
     return TL_OK;
 }
 extern "C" tl_status tl_k_swiglu_bwd(const uint16_t* da, const uint16_t* gu, int32_t T, int32_t f, uint16_t* dgu,
