@@ -272,7 +272,7 @@ struct Paged {                            // see paged.hip for the layout
 // row i of sequence s (rows first_row[s] .. first_row[s + 1] - 1; null: row s) into slot lengths[s] + i; weights and positions [n_seqs][heads][ldw], may be null
 hipError_t launch_paged_append(const Paged& c, const int* lengths, const bf16_t* k, long ldk, const bf16_t* v, long ldv, const int* first_row, int n_rows,
                                const int* pos, float* weights, int* positions, long ldw, hipStream_t s);
-constexpr int PAGED_MAX_RANGES = 128;
+constexpr int PAGED_MAX_RANGES = 64;         // (a wave joins them, one a lane)
 struct PagedWs {                          // scratch of the attention: scores [sequence][query head][ld_scores]; of each range a maximum and a sum, an output
     float* scores = nullptr;
     long ld_scores = 0;

@@ -1,6 +1,8 @@
 // A key/value cache on pages: tokens of many texts go in, one new token of each attends, heads forget the tokens that got little attention.
 //   k, v [n_pages][heads][page][d] bf16; slot j of sequence s lies on page table[s][j / page] at j % page.  page is a power of two from 16 on, so
 // that 16 slots that begin at a multiple of 16 lie on one page.
+#include <algorithm>
+
 #include "kernels.h"
 
 typedef unsigned u32x2_t __attribute__((ext_vector_type(2)));
@@ -244,20 +246,18 @@ __global__ __launch_bounds__(PAGED_NW * 64, 2) void attn_paged_kernel(Paged c, c
     }
 }
 
-// The largest score and the sum of weights over a query head's live ranges, in every lane of the wave.
-__device__ __forceinline__ float2 join_ml(const float2* ml, int live, int lane) {
-    float top = -INFINITY, sum = 0.f;
-    for (int i = lane; i < live; i += 64) top = fmaxf(top, ml[i].x);
-    top = wave_max(top);
-    for (int i = lane; i < live; i += 64) {
-        const float a = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml[i].x - top);
-        if (a != 0.f) sum += a * ml[i].y;
-    }
-    return make_float2(top, wave_sum(sum));
+// Of a query head's live ranges: lane i < live has its factor 2^(its largest score - the largest of all) in a, every lane what all weigh; returns the largest.
+__device__ __forceinline__ float join_ranges(const float2* ml, int live, int lane, float* a, float* sum) {
+    const float2 mine = lane < live ? ml[lane] : make_float2(-INFINITY, 0.f);
+    const float top = wave_max(mine.x);
+    *a = lane >= live ? 0.f : top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mine.x - top);
+    *sum = wave_sum(*a != 0.f ? *a * mine.y : 0.f);
+    return top;
 }
-// Behind the ranges: the first n_join workgroups join the outputs, 256 / D query heads each, the others add what 1024 slots of a key head got:
+// Behind the ranges: the first n_join workgroups join the outputs, 256 / D query heads each, NR ranges' columns asked for at a time, the others add what
+// 1024 slots of a key head got:
 //   weights_out[slot] = weights_in[slot] + the sum over the group's query heads of 2^(x - log2 of the sum of weights)
-template <int D>
+template <int D, int NR>
 __global__ __launch_bounds__(256) void paged_join_kernel(Paged c, const int* __restrict__ lengths, int max_len, int group, bf16_t* __restrict__ o, long ldo,
                                                          PagedWs ws, int range, int n_ranges, int n_join, const float* w_in, float* w_out, long ldw, int n_chunks) {
     const int heads = c.heads * group, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -265,43 +265,61 @@ __global__ __launch_bounds__(256) void paged_join_kernel(Paged c, const int* __r
         const long qh = (long)blockIdx.x * (256 / D) + threadIdx.x / D;
         if (qh >= (long)c.n_seqs * heads) return;
         const int seq = qh / heads, e = threadIdx.x % D, len = min(max(lengths[seq], 0), max_len), live = (len + range - 1) / range;
-        const float2* ml = ws.ml + qh * n_ranges;
-        const float2 all = join_ml(ml, live, lane);
-        float ot = 0.f;
-        for (int i = 0; i < live; ++i) {
-            const float a = all.x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml[i].x - all.x);
-            if (a != 0.f) ot += a * ws.o[(qh * n_ranges + i) * D + e];
+        const float* part = ws.o + qh * n_ranges * D + e;
+        float t[NR], a, sum, ot = 0.f;
+        auto fetch = [&](int i0) {
+#pragma unroll
+            for (int i = 0; i < NR; ++i) t[i] = part[(long)min(i0 + i, n_ranges - 1) * D];
+        };
+        fetch(0);
+        join_ranges(ws.ml + qh * n_ranges, live, lane, &a, &sum);
+        for (int i0 = 0; i0 < live; i0 += NR) {
+            if (i0) fetch(i0);
+#pragma unroll
+            for (int i = 0; i < NR; ++i) {
+                const float ai = __shfl(a, (i0 + i) & 63, 64);
+                ot += i0 + i < live && ai != 0.f ? ai * t[i] : 0.f;      // (a range that weighs nothing, or is none, may hold anything)
+            }
         }
-        o[(long)seq * ldo + qh % heads * D + e] = f32_to_bf16(all.y == 0.f ? 0.f : ot / all.y);
+        o[(long)seq * ldo + qh % heads * D + e] = f32_to_bf16(sum == 0.f ? 0.f : ot / sum);
         return;
     }
     int idx = blockIdx.x - n_join;
     const int chunk = idx % n_chunks, sh = idx / n_chunks, seq = sh / c.heads, head = sh % c.heads;
     const int len = min(max(lengths[seq], 0), max_len), live = (len + range - 1) / range, key = chunk * 1024 + threadIdx.x * 4;
     if (chunk * 1024 >= len) return;
-    __shared__ float lse[64];
-    float got[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int g0 = 0; g0 < group; g0 += 64) {
-        const int n = min(64, group - g0);
+    constexpr int NH = 8;                                  // query heads at a time
+    __shared__ float lse[NH];
+    const long at = ((long)seq * c.heads + head) * ldw + key;
+    float was[4] = {0.f, 0.f, 0.f, 0.f}, got[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (w_in && key + e < len) was[e] = w_in[at + e];
+    for (int g0 = 0; g0 < group; g0 += NH) {
+        const int n = min(NH, group - g0);
         const long qh = (long)seq * heads + head * group + g0;
-        __syncthreads();
+        f32x4_t x[NH];
+#pragma unroll
+        for (int j = 0; j < NH; ++j)
+            if (j < n && key < len) x[j] = *(const f32x4_t*)(ws.scores + (qh + j) * ws.ld_scores + key);
+        if (g0) __syncthreads();
         for (int j = wave; j < n; j += 4) {
-            const float2 all = join_ml(ws.ml + (qh + j) * n_ranges, live, lane);
-            if (lane == 0) lse[j] = all.y == 0.f ? INFINITY : all.x + __log2f(all.y);
+            float a, sum;
+            const float top = join_ranges(ws.ml + (qh + j) * n_ranges, live, lane, &a, &sum);
+            if (lane == 0) lse[j] = sum == 0.f ? INFINITY : top + __log2f(sum);
         }
         __syncthreads();
-        if (key < len) {
-            for (int j = 0; j < n; ++j) {
-                const f32x4_t x = *(const f32x4_t*)(ws.scores + (qh + j) * ws.ld_scores + key);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) got[e] += __builtin_amdgcn_exp2f(x[e] - lse[j]);
+        for (int j = 0; j < NH; ++j) {
+            if (j < n) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) got[e] += __builtin_amdgcn_exp2f(x[j][e] - lse[j]);
             }
         }
     }
-    const long at = ((long)seq * c.heads + head) * ldw + key;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-        if (key + e < len) w_out[at + e] = (w_in ? w_in[at + e] : 0.f) + got[e];
+        if (key + e < len) w_out[at + e] = was[e] + got[e];
 }
 
 static size_t round4(size_t n) { return (n + 3) & ~(size_t)3; }
@@ -311,8 +329,12 @@ PagedPlan attention_paged_plan(int max_len, int n_seqs, int heads, int kv_heads,
     const size_t scores = weights ? (size_t)rows * (size_t)(((long)max_len + 31) & ~31L) : 0;
     const int most = (int)((max_len + unit - 1L) / unit);
     PagedPlan p;
-    int n = (int)(1024 / groups < 1 ? 1 : 1024 / groups);
-    if (n_seqs > 1 && n < 4) n = 4;
+    // Ranges of 512 keys where sequences differ in length, and no fewer workgroups than CUs; a range alone needs no second launch.  us, by ranges:
+    // 131072 keys of 8 key heads 16 / 24 / 32 / 48 / 64: 136 / 102 / 89 / 107 / 90; 3800 of 32 heads 4 / 8 / 16: 27 / 21 / 21; 64 texts of up to
+    // 4096, 8 key heads 1 / 2 / 4 / 6 / 8 / 16 / 32: 130 / 149 / 140 / 124 / 127 / 131 / 148; 33 of up to 2000 1 / 2 / 4 / 8: 74 / 64 / 57 / 52; 64 of up to 500
+    // 1 / 2 / 4: 23 / 28 / 30; one of 200 1 / 2: 14.5 / 17.3 (the launches bound the last two).
+    int n = 1;
+    if (max_len > 512) n = (int)std::max(256 / groups, n_seqs > 1 ? ((long)max_len + 511) / 512 : 1L);
     n = n > most ? most : n;
     n = n > PAGED_MAX_RANGES ? PAGED_MAX_RANGES : n;
     for (;; --n) {
@@ -349,8 +371,8 @@ hipError_t launch_attention_paged(const Paged& c, const int* lengths, int max_le
     auto join = [&](auto kernel) {
         kernel<<<n_join + c.n_seqs * c.heads * n_chunks, 256, 0, s>>>(c, lengths, max_len, group, o, ldo, w, p.range, p.n_ranges, n_join, w_in, w_out, ldw, n_chunks);
     };
-    if (c.d == 128) join(paged_join_kernel<128>);
-    else join(paged_join_kernel<64>);
+    if (c.d == 128) p.n_ranges <= 8 ? join(paged_join_kernel<128, 8>) : join(paged_join_kernel<128, 32>);
+    else p.n_ranges <= 8 ? join(paged_join_kernel<64, 8>) : join(paged_join_kernel<64, 32>);
     return hipGetLastError();
 }
 

@@ -3,33 +3,39 @@
 // The order is that of the logits, the lowest index first among equals.  Kept are the first top_k of it, of these the ones that less than top_p of
 // their weight lies before, of these the ones with at least min_p of the largest weight.  With S the kept weight, the token is the first in the order
 // of the indices up to which more than floor(u S) is kept.
+#include <type_traits>
+
 #include "kernels.h"
 
 typedef unsigned long long u64;
 constexpr u64 SAMPLE_ONE = 1ull << 40;
-constexpr int SAMPLE_NT = 1024, SAMPLE_NW = SAMPLE_NT / 64, SAMPLE_BINS = 2048, SAMPLE_LIST = 4096;
+constexpr int SAMPLE_BINS = 2048;
+constexpr float SAMPLE_REACH = 1846.f;     // 64 units of the bins to one of (largest - x) / temperature: what lies further than 28.84 weighs less than half a unit
 
-// 2^y in units of 2^-40, y <= 0, rounded to the nearest: 2^n e^(f ln 2) with y = n + f, |f| <= 1/2, the exponential by its series up to the 13th power
-// (the first term left out is below 2^-57).  Adding 2^52 rounds to a whole number and leaves it in the mantissa's low bits.
+// 2^y in units of 2^-40, y <= 0 (NaN: 0), rounded to the nearest: 2^n e^(f ln 2) with y = n + f, |f| <= 1/2, the exponential by its series up to the 13th
+// power (the first term left out is below 2^-57).  n goes into the exponent; adding 2^52 rounds to a whole number and leaves it in the mantissa's low bits.
 __device__ __forceinline__ u64 weight_of(double y) {
-    if (!(y > -41.5)) return 0;
-    const double n = rint(y), t = (y - n) * 0.693147180559945309417;
-    double p = 1.0 / 6227020800.0;
-    p = fma(p, t, 1.0 / 479001600.0);
-    p = fma(p, t, 1.0 / 39916800.0);
-    p = fma(p, t, 1.0 / 3628800.0);
-    p = fma(p, t, 1.0 / 362880.0);
-    p = fma(p, t, 1.0 / 40320.0);
-    p = fma(p, t, 1.0 / 5040.0);
-    p = fma(p, t, 1.0 / 720.0);
-    p = fma(p, t, 1.0 / 120.0);
-    p = fma(p, t, 1.0 / 24.0);
-    p = fma(p, t, 1.0 / 6.0);
-    p = fma(p, t, 0.5);
-    p = fma(p, t, 1.0);
-    p = fma(p, t, 1.0);
-    const double scale = __longlong_as_double((long long)((int)n + 40 + 1023) << 52);
-    return (u64)__double_as_longlong(fma(p, scale, 4503599627370496.0)) & 0xfffffffffffffull;
+    constexpr double L = 0.693147180559945309417;
+    y = fmax(y, -60.0);
+    const double n = rint(y), f = y - n;
+    constexpr double l2 = L * L, l3 = l2 * L, l4 = l3 * L, l5 = l4 * L, l6 = l5 * L, l7 = l6 * L, l8 = l7 * L, l9 = l8 * L, l10 = l9 * L, l11 = l10 * L, l12 = l11 * L,
+                     l13 = l12 * L;
+    double p = l13 / 6227020800.0;
+    p = fma(p, f, l12 / 479001600.0);
+    p = fma(p, f, l11 / 39916800.0);
+    p = fma(p, f, l10 / 3628800.0);
+    p = fma(p, f, l9 / 362880.0);
+    p = fma(p, f, l8 / 40320.0);
+    p = fma(p, f, l7 / 5040.0);
+    p = fma(p, f, l6 / 720.0);
+    p = fma(p, f, l5 / 120.0);
+    p = fma(p, f, l4 / 24.0);
+    p = fma(p, f, l3 / 6.0);
+    p = fma(p, f, l2 / 2.0);
+    p = fma(p, f, L);
+    p = fma(p, f, 1.0);
+    p = __hiloint2double(__double2hiint(p) + (((int)n + 40) << 20), __double2loint(p)) + 4503599627370496.0;
+    return (u64)__double_as_longlong(p) & 0xfffffffffffffull;
 }
 // larger for larger x, the same for 0 and -0
 __device__ __forceinline__ unsigned key_of_logit(float x) {
@@ -37,97 +43,71 @@ __device__ __forceinline__ unsigned key_of_logit(float x) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 __device__ __forceinline__ float logit_of_key(unsigned k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
+// a place in the order, larger: earlier
+__device__ __forceinline__ u64 composite(float v, int i) { return (u64)key_of_logit(v) << 22 | (unsigned)(0x3fffff - i); }
+__device__ __forceinline__ float logit_of(u64 e) { return logit_of_key((unsigned)(e >> 22)); }
+__device__ __forceinline__ int index_of(u64 e) { return 0x3fffff - (int)(e & 0x3fffff); }
 
-struct SampleRow {
-    float top, bins;                      // the largest logit; bins of a unit of x
-    double per;                           // log2(e) / temperature
-    __device__ __forceinline__ u64 weight(float x) const { return x == top ? SAMPLE_ONE : weight_of(((double)x - (double)top) * per); }
-    // a coarse place in the order, 0 for the largest: monotone, as every step of it is
-    __device__ __forceinline__ int bin(float x) const { return x == top ? 0 : (int)fminf((top - x) * bins, (float)(SAMPLE_BINS - 1)); }
-    __device__ __forceinline__ bool counts(float x) const { return x == top || ((double)x - (double)top) * per > -41.5; }       // may weigh something (NaN: no)
-};
-
-// f(x[i], i) for first <= i < end, the workgroup's (or a wave's) lanes side by side
-template <int LANES, int U, class F>
-__device__ __forceinline__ void each_logit(const float* x, int first, int end, int lane, F&& f) {
-    for (int i0 = first; i0 < end; i0 += 4 * LANES * U) {
-        float4 v[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int i = i0 + (u * LANES + lane) * 4;
-            if (i + 4 <= end) v[u] = *(const float4*)(x + i);
-            else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) (&v[u].x)[e] = i + e < end ? x[i + e] : -INFINITY;
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int i = i0 + (u * LANES + lane) * 4;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (i + e < end) f((&v[u].x)[e], i + e);
-        }
-    }
-}
-
+template <int NT, int LIST>
 struct SampleLds {
     u64 sum[SAMPLE_BINS];
     int count[SAMPLE_BINS];
-    u64 list[SAMPLE_LIST];
-    u64 wave_sum[SAMPLE_NW];
-    int wave_count[SAMPLE_NW];
+    u64 list[LIST];
+    u64 wave_sum[NT / 64];
     u64 found_sum, found_before_sum, lowest;
     int found, found_count, found_before, n_list;
 };
 // inclusive sums over the threads of the workgroup; the total to *all
-__device__ __forceinline__ u64 block_scan(SampleLds& s, u64 v, u64* all) {
+template <class S, class N>
+__device__ __forceinline__ N block_scan(S& s, N v, N* all) {
+    constexpr int NW = sizeof(s.wave_sum) / sizeof(u64);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) {
-        const u64 o = __shfl_up(v, off, 64);
+        const N o = __shfl_up(v, off, 64);
         if (lane >= off) v += o;
     }
     __syncthreads();
-    if (lane == 63) s.wave_sum[wave] = v;
+    if (lane == 63) s.wave_sum[wave] = (u64)v;
     __syncthreads();
-    u64 total = 0;
+    N total = 0;
 #pragma unroll
-    for (int w = 0; w < SAMPLE_NW; ++w) {
-        if (w < wave) v += s.wave_sum[w];
-        total += s.wave_sum[w];
+    for (int w = 0; w < NW; ++w) {
+        const N o = (N)s.wave_sum[w];
+        if (w < wave) v += o;
+        total += o;
     }
     *all = total;
     return v;
 }
-__device__ __forceinline__ int block_count(SampleLds& s, int v) {
-    u64 all;
-    block_scan(s, (u64)v, &all);
-    return (int)all;
-}
-__device__ __forceinline__ void clear_bins(SampleLds& s) {
-    for (int i = threadIdx.x; i < SAMPLE_BINS; i += SAMPLE_NT) s.sum[i] = 0, s.count[i] = 0;
-    __syncthreads();
-}
 // the bin in which the count (by_count) or the weight, summed up from bin 0 and on top of before_*, first reaches `limit`: s.found (-1: none does), its own
-// count and sum, and those before it
-__device__ __forceinline__ void find_bin(SampleLds& s, bool by_count, u64 limit, int before_count, u64 before_sum) {
-    const int b = 2 * threadIdx.x;
-    u64 all;
-    __syncthreads();
+// count and sum, and those before it.  SUMS: else the counts alone are there and wanted.
+template <int NT, bool SUMS, class S>
+__device__ __forceinline__ void find_bin(S& s, bool by_count, u64 limit, int before_count, u64 before_sum) {
+    constexpr int N = SAMPLE_BINS / NT;
+    const int b = N * threadIdx.x;
+    int c[N], cs = 0;
+    u64 w[N], ws = 0, all;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        c[i] = s.count[b + i], cs += c[i];
+        w[i] = SUMS ? s.sum[b + i] : 0, ws += w[i];
+    }
     if (threadIdx.x == 0) s.found = -1;
-    const int c0 = s.count[b], c1 = s.count[b + 1];
-    const u64 w0 = s.sum[b], w1 = s.sum[b + 1];
-    const int c = (int)block_scan(s, (u64)(c0 + c1), &all) + before_count;
-    const u64 w = block_scan(s, w0 + w1, &all) + before_sum;
-    auto take = [&](int at, int n, u64 x, int nb, u64 xb) { s.found = at, s.found_count = n, s.found_sum = x, s.found_before = nb, s.found_before_sum = xb; };
-    const u64 end = by_count ? (u64)c : w, mid = by_count ? (u64)(c - c1) : w - w1, start = by_count ? (u64)(c - c0 - c1) : w - w0 - w1;
-    if (start < limit && limit <= mid) take(b, c0, w0, c - c0 - c1, w - w0 - w1);
-    if (mid < limit && limit <= end) take(b + 1, c1, w1, c - c1, w - w1);
+    int all_c;
+    cs = block_scan(s, cs, &all_c) - cs + before_count;
+    if (SUMS) ws = block_scan(s, ws, &all) - ws + before_sum;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const u64 start = by_count ? (u64)cs : ws, end = by_count ? (u64)(cs + c[i]) : ws + w[i];
+        if (start < limit && limit <= end) s.found = b + i, s.found_count = c[i], s.found_sum = w[i], s.found_before = cs, s.found_before_sum = ws;
+        cs += c[i], ws += w[i];
+    }
     __syncthreads();
 }
-// one value a thread, the largest in thread 0
-__device__ __forceinline__ u64 block_sort(SampleLds& s, u64 v, int n) {
+// one value a thread, the largest in thread 0; n of them are not 0
+template <class S>
+__device__ __forceinline__ u64 block_sort(S& s, u64 v, int n) {
     int size = 64;
     while (size < n) size <<= 1;
     const int t = threadIdx.x;
@@ -148,8 +128,16 @@ __device__ __forceinline__ u64 block_sort(SampleLds& s, u64 v, int n) {
     return v;
 }
 
-__global__ __launch_bounds__(SAMPLE_NT) void sample_kernel(Sample c, int vocab) {
-    __shared__ SampleLds s;
+// One workgroup a row.  HELD: the row stays in LDS from its one reading on; else every pass over it reads it again.
+//   pass 1  the largest logit
+//   pass 2  with top_k or top_p: how many tokens (top_k), or how much weight (top_p), lies in each of 2048 ranges of (largest - x) / temperature, 64 to a unit
+//   pass 3  what lies in the ranges up to the one with the cut is listed; up to a token a thread, the list is sorted, cut and drawn from
+//   else    the cut is found digit by digit among the tokens of its range (from a list if they fit one), and a last pass draws
+template <int NT, int LIST, bool HELD>
+__global__ __launch_bounds__(NT) void sample_kernel(Sample c, int vocab) {
+    constexpr int NW = NT / 64;
+    __shared__ SampleLds<NT, LIST> s;
+    extern __shared__ __align__(16) float held[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const long r = blockIdx.x;
     const float* x = c.logits + r * c.ldl;
@@ -160,114 +148,181 @@ __global__ __launch_bounds__(SAMPLE_NT) void sample_kernel(Sample c, int vocab) 
         if (c.kept) c.kept[r] = kept;
         if (c.prob) c.prob[r] = prob;
     };
+    bool infinite = false;                                 // the largest is infinity: its equals count as 0, all others as -infinity
+    auto from_memory = [&](int i) -> float4 {              // (behind the row: -infinity, which weighs nothing)
+        float4 v;
+        if (i + 4 <= vocab) v = *(const float4*)(x + i);
+        else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) (&v.x)[e] = i + e < vocab ? x[i + e] : -INFINITY;
+        }
+        return v;
+    };
+    // f(x[i], i), the lanes side by side, from the first on to the end, both multiples of 4
+    auto each = [&](auto lanes, int first, int end, int at, auto&& f) {
+        constexpr int LANES = decltype(lanes)::value, U = HELD ? 1 : 4;
+        for (int i0 = first; i0 < end; i0 += 4 * LANES * U) {
+            float4 v[U];
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                const int i = i0 + (k * LANES + at) * 4;
+                if (i >= end) v[k] = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+                else if (HELD) v[k] = *(const float4*)(held + i);
+                else v[k] = from_memory(i);
+            }
+            if (!HELD && infinite) {
+#pragma unroll
+                for (int k = 0; k < U; ++k)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) (&v[k].x)[e] = (&v[k].x)[e] == INFINITY ? 0.f : -INFINITY;
+            }
+#pragma unroll
+            for (int k = 0; k < U; ++k)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) f((&v[k].x)[e], i0 + (k * LANES + at) * 4 + e);
+        }
+    };
+    const int padded = (vocab + 3) & ~3;
+    auto all_of = [&](auto&& f) { each(std::integral_constant<int, NT>{}, 0, padded, tid, f); };
 
-    // the largest, and its lowest index for the choice without a temperature
     float m = -INFINITY;
-    int at = 0x7fffffff;
-    const bool greedy = !(temperature > 0.f);
-    if (greedy) each_logit<SAMPLE_NT, 4>(x, 0, vocab, tid, [&](float v, int i) { if (v > m) m = v, at = i; });
-    else each_logit<SAMPLE_NT, 4>(x, 0, vocab, tid, [&](float v, int) { m = fmaxf(m, v); });
+    if (HELD) {
+        for (int i0 = 0; i0 < padded; i0 += 16 * NT) {
+            float4 v[4];
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) {
-        const float o = __shfl_xor(m, off, 64);
-        const int oi = __shfl_xor(at, off, 64);
-        if (o > m || (o == m && oi < at)) m = o, at = oi;
+            for (int k = 0; k < 4; ++k) {
+                const int i = i0 + (k * NT + tid) * 4;
+                if (i < padded) v[k] = from_memory(i);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int i = i0 + (k * NT + tid) * 4;
+                if (i >= padded) continue;
+                *(float4*)(held + i) = v[k];
+                m = fmaxf(m, fmaxf(fmaxf(v[k].x, v[k].y), fmaxf(v[k].z, v[k].w)));
+            }
+        }
+    } else {
+        all_of([&](float v, int) { m = fmaxf(m, v); });
     }
-    if (lane == 0) s.wave_sum[wave] = (u64)key_of_logit(m) << 32 | (unsigned)~at;
+    m = wave_max(m);
+    if (lane == 0) s.wave_sum[wave] = __float_as_uint(m);
+    if (tid == 0) s.n_list = 0, s.lowest = 0;
+    for (int i = tid; i < SAMPLE_BINS; i += NT) s.sum[i] = 0, s.count[i] = 0;
     __syncthreads();
-    u64 best = 0;
+    float top = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < SAMPLE_NW; ++w) best = best > s.wave_sum[w] ? best : s.wave_sum[w];
-    __syncthreads();
-    SampleRow row;
-    row.top = logit_of_key((unsigned)(best >> 32));
-    if (row.top == -INFINITY) {
+    for (int w = 0; w < NW; ++w) top = fmaxf(top, __uint_as_float((unsigned)s.wave_sum[w]));
+    if (top == -INFINITY) {
         if (tid == 0) out(-1, 0, 0.f);
         return;
     }
-    if (greedy) {
-        if (tid == 0) out((int)~(unsigned)best, 1, 1.f);
+    if (!(temperature > 0.f)) {                            // the lowest index of the largest
+        all_of([&](float v, int i) { if (v == top) atomicMax(&s.lowest, composite(0.f, i)); });
+        __syncthreads();
+        if (tid == 0) out(index_of(s.lowest), 1, 1.f);
         return;
     }
-    row.per = 1.0 / (double)temperature * 1.44269504088896340736;
-    row.bins = 64.f / temperature;
+    infinite = top == INFINITY;
+    if (infinite) {
+        top = 0.f;
+        if (HELD) {
+            for (int i = tid; i < padded; i += NT) held[i] = held[i] == INFINITY ? 0.f : -INFINITY;
+            __syncthreads();
+        }
+    }
+    const double per = 1.0 / (double)temperature * 1.44269504088896340736, top64 = (double)top;
+    const float to_bins = 64.f / temperature;
+    auto weight = [&](float v) -> u64 { return weight_of(((double)v - top64) * per); };
+    auto place = [&](float v) -> float { return v == top ? 0.f : (top - v) * to_bins; };      // monotone, as each step of it is; its whole part is the bin
 
     const int k = top_k >= 1.f && top_k < (float)vocab ? (int)top_k : 0;
     const bool p_on = top_p < 1.f;
     u64 least = 1;
     if (min_p > 0.f) least = min_p >= 1.f ? SAMPLE_ONE : (u64)ceil((double)min_p * (double)SAMPLE_ONE);
     auto limit_of = [&](u64 sum) -> u64 { return top_p > 0.f ? (u64)ceil((double)top_p * (double)sum) : 1ull; };
-    auto composite = [&](float v, int i) -> u64 { return (u64)key_of_logit(v) << 22 | (unsigned)(0x3fffff - i); };        // larger: earlier in the order
-    u64 threshold = 0;                                     // kept: composites from here on
+    auto place_in = [&](u64 all) -> u64 {
+        const u64 t = (u64)floor((double)fminf(fmaxf(u, 0.f), 1.f) * (double)all);
+        return t < all ? t : all - 1;
+    };
+    u64 cut = 0;                                           // kept: composites from here on
     if (k || p_on) {
-        clear_bins(s);
-        each_logit<SAMPLE_NT, 4>(x, 0, vocab, tid, [&](float v, int) {
-            if (!row.counts(v)) return;
-            const int b = row.bin(v);
-            atomicAdd(&s.count[b], 1);
-            if (p_on) atomicAdd(&s.sum[b], row.weight(v));
-        });
-        __syncthreads();
+        auto clear = [&]() {
+            __syncthreads();
+            for (int i = tid; i < SAMPLE_BINS; i += NT) s.sum[i] = 0, s.count[i] = 0;
+            __syncthreads();
+        };
+        auto weigh_bins = [&]() {
+            all_of([&](float v, int i) {
+                const float b = place(v);
+                if (!(b < SAMPLE_REACH) || (cut && composite(v, i) < cut)) return;
+                atomicAdd(&s.count[(int)b], 1);
+                atomicAdd(&s.sum[(int)b], weight(v));
+            });
+            __syncthreads();
+        };
         u64 total = 0;
         bool by_count = k > 0;
         if (by_count) {
-            find_bin(s, true, (u64)k, 0, 0);
+            all_of([&](float v, int) {
+                const float b = place(v);
+                if (b < SAMPLE_REACH) atomicAdd(&s.count[(int)b], 1);
+            });
+            __syncthreads();
+            find_bin<NT, false>(s, true, (u64)k, 0, 0);
             by_count = s.found >= 0;
+            if (!by_count && p_on) clear();
         }
         if (!by_count && p_on) {
-            block_scan(s, s.sum[2 * tid] + s.sum[2 * tid + 1], &total);
-            find_bin(s, false, limit_of(total), 0, 0);
+            weigh_bins();
+            u64 mine = 0;
+            for (int i = tid; i < SAMPLE_BINS; i += NT) mine += s.sum[i];
+            block_scan(s, mine, &total);
+            find_bin<NT, true>(s, false, limit_of(total), 0, 0);
         }
         if (by_count || p_on) {
             const int few = s.found_before + s.found_count;
-            if (few <= SAMPLE_NT) {
-                // all that can be kept fits one token a thread
-                const int b = s.found;
-                if (tid == 0) s.n_list = 0;
-                __syncthreads();
-                each_logit<SAMPLE_NT, 4>(x, 0, vocab, tid, [&](float v, int i) {
-                    if (row.counts(v) && row.bin(v) <= b) s.list[atomicAdd(&s.n_list, 1)] = composite(v, i);
-                });
+            if (few <= NT) {
+                const float end = (float)(s.found + 1);
+                all_of([&](float v, int i) { if (place(v) < end) s.list[atomicAdd(&s.n_list, 1)] = composite(v, i); });
                 __syncthreads();
                 u64 e = tid < few ? s.list[tid] : 0;
                 e = block_sort(s, e, few);
-                const int i = 0x3fffff - (int)(e & 0x3fffff);
-                u64 w = tid < few ? row.weight(logit_of_key((unsigned)(e >> 22))) : 0, all;
-                if (by_count && tid >= k) w = 0;
+                u64 w = tid < few && !(by_count && tid >= k) ? weight(logit_of(e)) : 0, all;
                 const u64 before = block_scan(s, w, &all) - w;
                 if (by_count) total = all;
                 const bool keep = w >= least && (!p_on || tid == 0 || before < limit_of(total));
-                const int kept = block_count(s, keep);
-                u64 o = keep ? ~((u64)i << 41 | w) : 0;    // (weights have 41 bits, indices 22)
+                int kept;
+                block_scan(s, (int)keep, &kept);
+                u64 o = keep ? ~((u64)index_of(e) << 41 | w) : 0;    // (weights have 41 bits, indices 22)
                 o = block_sort(s, o, few);
                 w = o ? ~o & ((1ull << 41) - 1) : 0;
-                const u64 upto = block_scan(s, w, &all);
-                u64 t = (u64)floor((double)fminf(fmaxf(u, 0.f), 1.f) * (double)all);
-                t = t < all ? t : all - 1;
+                const u64 upto = block_scan(s, w, &all), t = place_in(all);
                 if (upto - w <= t && t < upto) out((int)(~o >> 41), kept, (float)((double)w / (double)all));
                 return;
             }
-            // the place of a cut inside bin b of the coarse order: digit by digit of the composite; its elements from the list if they fit one
-            auto cut = [&](bool count_mode, u64 limit, u64* sum_upto) -> u64 {
-                const int b = s.found, n = s.found_count;
+            // the last composite that is kept, the cut lying in the bin that was found: digit by digit, among the tokens of the bin, from the list if they fit
+            auto find_cut = [&](bool count_mode, u64 limit, u64* sum_upto) -> u64 {
+                const float b = (float)s.found;
+                const int n = s.found_count;
                 int before = s.found_before;
                 u64 before_sum = s.found_before_sum;
-                const bool listed = n <= SAMPLE_LIST;
+                const bool listed = n <= LIST;
                 __syncthreads();
-                if (tid == 0) s.n_list = 0;
+                if (tid == 0) s.n_list = 0, s.lowest = ~0ull;
                 __syncthreads();
-                if (listed) {
-                    each_logit<SAMPLE_NT, 4>(x, 0, vocab, tid, [&](float v, int i) {
-                        if (row.counts(v) && row.bin(v) == b && composite(v, i) >= threshold) s.list[atomicAdd(&s.n_list, 1)] = composite(v, i);
+                auto of_bin = [&](auto&& f) {
+                    all_of([&](float v, int i) {
+                        const float at = place(v);
+                        if (at >= b && at < b + 1.f && (!cut || composite(v, i) >= cut)) f(composite(v, i));
                     });
-                }
-                auto each = [&](auto&& f) {
+                };
+                if (listed) of_bin([&](u64 e) { s.list[atomicAdd(&s.n_list, 1)] = e; });
+                auto members = [&](auto&& f) {
                     if (listed) {
-                        for (int i = tid; i < n; i += SAMPLE_NT) f(s.list[i]);
+                        for (int i = tid; i < n; i += NT) f(s.list[i]);
                     } else {
-                        each_logit<SAMPLE_NT, 4>(x, 0, vocab, tid, [&](float v, int i) {
-                            if (row.counts(v) && row.bin(v) == b && composite(v, i) >= threshold) f(composite(v, i));
-                        });
+                        of_bin(f);
                     }
                     __syncthreads();
                 };
@@ -276,86 +331,91 @@ __global__ __launch_bounds__(SAMPLE_NT) void sample_kernel(Sample c, int vocab) 
                 for (int d = 0; d < 5; ++d) {
                     const int bits = d == 2 ? 10 : 11, above = shift;
                     shift -= bits;
-                    clear_bins(s);
-                    each([&](u64 e) {
+                    clear();
+                    members([&](u64 e) {
                         if (d > 0 && e >> above != prefix >> above) return;
                         const int bin = (SAMPLE_BINS - 1) - (int)(e >> shift & ((1 << bits) - 1));
                         atomicAdd(&s.count[bin], 1);
-                        atomicAdd(&s.sum[bin], row.weight(logit_of_key((unsigned)(e >> 22))));
+                        atomicAdd(&s.sum[bin], weight(logit_of(e)));
                     });
-                    find_bin(s, count_mode, limit, before, before_sum);
+                    find_bin<NT, true>(s, count_mode, limit, before, before_sum);
                     prefix |= (u64)(SAMPLE_BINS - 1 - s.found) << shift;
                     before = s.found_before, before_sum = s.found_before_sum;
                     *sum_upto = before_sum + s.found_sum;
                     if (s.found_count == 1 || (count_mode && (u64)(before + s.found_count) == limit)) break;       // all of the bin
                 }
-                // (other coarse bins may lie above the prefix: the cut is the last composite that is kept)
-                if (tid == 0) s.lowest = ~0ull;
-                __syncthreads();
-                each([&](u64 e) { if (e >> shift == prefix >> shift) atomicMin(&s.lowest, e); });
+                members([&](u64 e) { if (e >> shift == prefix >> shift) atomicMin(&s.lowest, e); });       // (tokens of other bins may lie above the prefix)
                 return s.lowest;
             };
             if (by_count) {
-                threshold = cut(true, (u64)k, &total);
-                if (p_on) {
-                    // the cut by weight lies before the one by count: its bin is found over the coarse bins again
-                    clear_bins(s);
-                    each_logit<SAMPLE_NT, 4>(x, 0, vocab, tid, [&](float v, int i) {
-                        if (!row.counts(v) || composite(v, i) < threshold) return;
-                        const int b = row.bin(v);
-                        atomicAdd(&s.count[b], 1);
-                        atomicAdd(&s.sum[b], row.weight(v));
-                    });
-                    __syncthreads();
-                    find_bin(s, false, limit_of(total), 0, 0);
+                clear();
+                weigh_bins();
+                find_bin<NT, true>(s, true, (u64)k, 0, 0);
+                cut = find_cut(true, (u64)k, &total);
+                if (p_on) {                                // the cut by weight lies before the one by count
+                    clear();
+                    weigh_bins();
+                    find_bin<NT, true>(s, false, limit_of(total), 0, 0);
                 }
             }
             if (p_on) {
                 u64 unused;
-                const u64 limit = limit_of(total), other = cut(false, limit, &unused);
-                threshold = threshold > other ? threshold : other;
+                const u64 other = find_cut(false, limit_of(total), &unused);
+                cut = cut > other ? cut : other;
             }
         }
     }
-    // what is kept, a 16th of the row a wave; then the 16th that holds the place, a stretch of it a thread
-    const int stretch = ((vocab + SAMPLE_NW - 1) / SAMPLE_NW + 255) & ~255;
-    auto weight = [&](float v, int i) -> u64 {
-        if (threshold && composite(v, i) < threshold) return 0;
-        const u64 w = row.weight(v);
+    // what is kept, a share of the row a wave; then the share that holds the place, a stretch of it a thread.  `bar`: nothing below it is kept (for min_p with a
+    // margin for the roundings of its own; the weight decides).
+    const float cut_at = cut ? logit_of(cut) : -INFINITY;
+    const int cut_index = cut ? index_of(cut) : 0;
+    float bar = cut_at;
+    if (least > 1) {
+        const float low = top - 1.0001f * temperature * (0.001f - __logf(fminf(min_p, 1.f))) - 1e-6f * fabsf(top);
+        if (low <= top) bar = fmaxf(bar, low);
+    }
+    auto kept_weight = [&](float v, int i) -> u64 {
+        if (!(v >= bar) || (v == cut_at && i > cut_index)) return 0;
+        const u64 w = weight(v);
         return w >= least ? w : 0;
     };
+    const int stretch = ((vocab + NW - 1) / NW + 255) & ~255;
     u64 sum = 0;
     int n = 0;
     const int mine = wave * stretch;
-    each_logit<64, 4>(x, mine, min(mine + stretch, vocab), lane, [&](float v, int i) {
-        const u64 w = weight(v, i);
+    each(std::integral_constant<int, 64>{}, mine, min(mine + stretch, padded), lane, [&](float v, int i) {
+        const u64 w = kept_weight(v, i);
         sum += w;
         n += w != 0;
     });
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
-    const int kept = block_count(s, n);
+    int kept;
+    block_scan(s, n, &kept);
     __syncthreads();
     if (lane == 0) s.wave_sum[wave] = sum;
     __syncthreads();
     u64 all = 0;
 #pragma unroll
-    for (int w = 0; w < SAMPLE_NW; ++w) all += s.wave_sum[w];
-    u64 t = (u64)floor((double)fminf(fmaxf(u, 0.f), 1.f) * (double)all);
-    t = t < all ? t : all - 1;
+    for (int w = 0; w < NW; ++w) all += s.wave_sum[w];
+    const u64 t = place_in(all);
     int part = 0;
     u64 before = 0;
-    for (; part < SAMPLE_NW - 1 && before + s.wave_sum[part] <= t; ++part) before += s.wave_sum[part];
-    const int first = part * stretch, end = min(first + stretch, vocab), per = stretch / SAMPLE_NT + (stretch % SAMPLE_NT != 0);
-    const int a = min(first + tid * per, end), b = min(a + per, end);
-    u64 own = 0;
-    for (int i = a; i < b; ++i) own += weight(x[i], i);
+    for (; part < NW - 1 && before + s.wave_sum[part] <= t; ++part) before += s.wave_sum[part];
+    const int first = part * stretch, end = min(first + stretch, vocab), own = (stretch + NT - 1) / NT;
+    const int a = min(first + tid * own, end), b = min(a + own, end);
+    auto at = [&](int i) -> float {
+        const float v = HELD ? held[i] : x[i];
+        return HELD || !infinite ? v : v == INFINITY ? 0.f : -INFINITY;
+    };
+    u64 here = 0;
+    for (int i = a; i < b; ++i) here += kept_weight(at(i), i);
     u64 unused;
-    u64 upto = block_scan(s, own, &unused) + before;
-    if (upto - own <= t && t < upto) {
-        upto -= own;
+    u64 upto = block_scan(s, here, &unused) + before;
+    if (upto - here <= t && t < upto) {
+        upto -= here;
         for (int i = a; i < b; ++i) {
-            const u64 w = weight(x[i], i);
+            const u64 w = kept_weight(at(i), i);
             upto += w;
             if (t < upto) {
                 out(i, kept, (float)((double)w / (double)all));
@@ -364,9 +424,17 @@ __global__ __launch_bounds__(SAMPLE_NT) void sample_kernel(Sample c, int vocab) 
         }
     }
 }
+constexpr int SAMPLE_HELD = 32512;         // logits that fit LDS beside the bins
 hipError_t launch_sample(const Sample& c, int rows, int vocab, float* ws, size_t ws_elems, hipStream_t s) {
     if (rows <= 0) return hipSuccess;
     (void)ws, (void)ws_elems;
-    sample_kernel<<<rows, SAMPLE_NT, 0, s>>>(c, vocab);
+    if (vocab <= SAMPLE_HELD && rows <= 256) {
+        const int lds = ((vocab + 3) & ~3) * 4;
+        const hipError_t e = hipFuncSetAttribute((const void*)sample_kernel<1024, 1024, true>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        if (e != hipSuccess) return e;
+        sample_kernel<1024, 1024, true><<<rows, 1024, lds, s>>>(c, vocab);
+    } else {
+        sample_kernel<512, 2048, false><<<rows, 512, 0, s>>>(c, vocab);
+    }
     return hipGetLastError();
 }
