@@ -71,7 +71,7 @@ __device__ __forceinline__ N block_scan(S& s, N v, N* all) {
     if (lane == 63) s.wave_sum[wave] = (u64)v;
     __syncthreads();
     N total = 0;
-#pragma unroll
+#pragma unroll 4
     for (int w = 0; w < NW; ++w) {
         const N o = (N)s.wave_sum[w];
         if (w < wave) v += o;
@@ -134,7 +134,7 @@ __device__ __forceinline__ u64 block_sort(S& s, u64 v, int n) {
 //   pass 3  what lies in the ranges up to the one with the cut is listed; up to a token a thread, the list is sorted, cut and drawn from
 //   else    the cut is found digit by digit among the tokens of its range (from a list if they fit one), and a last pass draws
 template <int NT, int LIST, bool HELD>
-__global__ __launch_bounds__(NT) void sample_kernel(Sample c, int vocab) {
+__global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab) {
     constexpr int NW = NT / 64;
     __shared__ SampleLds<NT, LIST> s;
     extern __shared__ __align__(16) float held[];
@@ -149,7 +149,7 @@ __global__ __launch_bounds__(NT) void sample_kernel(Sample c, int vocab) {
         if (c.prob) c.prob[r] = prob;
     };
     bool infinite = false;                                 // the largest is infinity: its equals count as 0, all others as -infinity
-    auto from_memory = [&](int i) -> float4 {              // (behind the row: -infinity, which weighs nothing)
+    auto from_memory = [&](int i) __attribute__((always_inline)) -> float4 {              // (behind the row: -infinity, which weighs nothing)
         float4 v;
         if (i + 4 <= vocab) v = *(const float4*)(x + i);
         else {
@@ -158,18 +158,24 @@ __global__ __launch_bounds__(NT) void sample_kernel(Sample c, int vocab) {
         }
         return v;
     };
-    // f(x[i], i), the lanes side by side, from the first on to the end, both multiples of 4
-    auto each = [&](auto lanes, int first, int end, int at, auto&& f) {
-        constexpr int LANES = decltype(lanes)::value, U = HELD ? 1 : 4;
-        for (int i0 = first; i0 < end; i0 += 4 * LANES * U) {
-            float4 v[U];
+    // f(x[i], i), the lanes side by side, from the first on to the end, both multiples of 4; U times four a lane at a time, the next on their way
+    auto each = [&](auto lanes, int first, int end, int at, auto&& f) __attribute__((always_inline)) {
+        constexpr int LANES = decltype(lanes)::value, U = HELD ? 1 : 2;
+        float4 v[U], next[U];
+        auto fetch = [&](int i0) __attribute__((always_inline)) {
 #pragma unroll
             for (int k = 0; k < U; ++k) {
                 const int i = i0 + (k * LANES + at) * 4;
-                if (i >= end) v[k] = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-                else if (HELD) v[k] = *(const float4*)(held + i);
-                else v[k] = from_memory(i);
+                if (i >= end) next[k] = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+                else if (HELD) next[k] = *(const float4*)(held + i);
+                else next[k] = from_memory(i);
             }
+        };
+        fetch(first);
+        for (int i0 = first; i0 < end; i0 += 4 * LANES * U) {
+#pragma unroll
+            for (int k = 0; k < U; ++k) v[k] = next[k];
+            fetch(i0 + 4 * LANES * U);
             if (!HELD && infinite) {
 #pragma unroll
                 for (int k = 0; k < U; ++k)
@@ -179,13 +185,18 @@ __global__ __launch_bounds__(NT) void sample_kernel(Sample c, int vocab) {
 #pragma unroll
             for (int k = 0; k < U; ++k)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) f((&v[k].x)[e], i0 + (k * LANES + at) * 4 + e);
+                for (int e = 0; e < 4; ++e) {
+                    f((&v[k].x)[e], i0 + (k * LANES + at) * 4 + e);
+                    if (e & 1) __builtin_amdgcn_sched_barrier(0);        // (more than two weights at a time would not fit the registers)
+                }
         }
     };
     const int padded = (vocab + 3) & ~3;
-    auto all_of = [&](auto&& f) { each(std::integral_constant<int, NT>{}, 0, padded, tid, f); };
+    auto all_of = [&](auto&& f) __attribute__((always_inline)) { each(std::integral_constant<int, NT>{}, 0, padded, tid, f); };
 
+    const bool greedy = !(temperature > 0.f);
     float m = -INFINITY;
+    int lowest = 0;
     if (HELD) {
         for (int i0 = 0; i0 < padded; i0 += 16 * NT) {
             float4 v[4];
@@ -202,9 +213,12 @@ __global__ __launch_bounds__(NT) void sample_kernel(Sample c, int vocab) {
                 m = fmaxf(m, fmaxf(fmaxf(v[k].x, v[k].y), fmaxf(v[k].z, v[k].w)));
             }
         }
+    } else if (greedy) {
+        all_of([&](float v, int i) { if (v > m) m = v, lowest = i; });
     } else {
         all_of([&](float v, int) { m = fmaxf(m, v); });
     }
+    const float own_top = m;
     m = wave_max(m);
     if (lane == 0) s.wave_sum[wave] = __float_as_uint(m);
     if (tid == 0) s.n_list = 0, s.lowest = 0;
@@ -217,8 +231,9 @@ __global__ __launch_bounds__(NT) void sample_kernel(Sample c, int vocab) {
         if (tid == 0) out(-1, 0, 0.f);
         return;
     }
-    if (!(temperature > 0.f)) {                            // the lowest index of the largest
-        all_of([&](float v, int i) { if (v == top) atomicMax(&s.lowest, composite(0.f, i)); });
+    if (greedy) {                                          // the lowest index of the largest
+        if (HELD) all_of([&](float v, int i) { if (v == top) atomicMax(&s.lowest, composite(0.f, i)); });
+        else if (own_top == top) atomicMax(&s.lowest, composite(0.f, lowest));
         __syncthreads();
         if (tid == 0) out(index_of(s.lowest), 1, 1.f);
         return;
@@ -232,9 +247,9 @@ __global__ __launch_bounds__(NT) void sample_kernel(Sample c, int vocab) {
         }
     }
     const double per = 1.0 / (double)temperature * 1.44269504088896340736, top64 = (double)top;
-    const float to_bins = 64.f / temperature;
-    auto weight = [&](float v) -> u64 { return weight_of(((double)v - top64) * per); };
-    auto place = [&](float v) -> float { return v == top ? 0.f : (top - v) * to_bins; };      // monotone, as each step of it is; its whole part is the bin
+    const float to_bins = fminf(64.f / temperature, 3e38f);
+    auto weight = [&](float v) __attribute__((always_inline)) -> u64 { return weight_of(((double)v - top64) * per); };
+    auto place = [&](float v) -> float { return (top - v) * to_bins; };      // monotone, as each step of it is; its whole part is the bin
 
     const int k = top_k >= 1.f && top_k < (float)vocab ? (int)top_k : 0;
     const bool p_on = top_p < 1.f;
@@ -247,12 +262,12 @@ __global__ __launch_bounds__(NT) void sample_kernel(Sample c, int vocab) {
     };
     u64 cut = 0;                                           // kept: composites from here on
     if (k || p_on) {
-        auto clear = [&]() {
+        auto clear = [&]() __attribute__((always_inline)) {
             __syncthreads();
             for (int i = tid; i < SAMPLE_BINS; i += NT) s.sum[i] = 0, s.count[i] = 0;
             __syncthreads();
         };
-        auto weigh_bins = [&]() {
+        auto weigh_bins = [&]() __attribute__((always_inline)) {
             all_of([&](float v, int i) {
                 const float b = place(v);
                 if (!(b < SAMPLE_REACH) || (cut && composite(v, i) < cut)) return;
@@ -261,8 +276,53 @@ __global__ __launch_bounds__(NT) void sample_kernel(Sample c, int vocab) {
             });
             __syncthreads();
         };
+        // tokens of the bins up to b, listed as far as there is room
+        auto list_upto = [&](int b) __attribute__((always_inline)) {
+            const float end = (float)(b + 1);
+            all_of([&](float v, int i) {
+                if (place(v) < end) {
+                    const int at = atomicAdd(&s.n_list, 1);
+                    if (at < LIST) s.list[at] = composite(v, i);
+                }
+            });
+            __syncthreads();
+        };
+        // the list, one token a thread, holds all that can be kept: sorted, cut, sorted by index and drawn from
+        auto draw_listed = [&](int n, bool by_count, u64 total) __attribute__((always_inline)) {
+            u64 e = tid < n ? s.list[tid] : 0;
+            e = block_sort(s, e, n);
+            u64 w = tid < n && !(by_count && tid >= k) ? weight(logit_of(e)) : 0, all;
+            const u64 before = block_scan(s, w, &all) - w;
+            if (by_count) total = all;
+            const bool keep = w >= least && (!p_on || tid == 0 || before < limit_of(total));
+            const int kept = __syncthreads_count(keep);
+            u64 o = keep ? ~((u64)index_of(e) << 41 | w) : 0;    // (weights have 41 bits, indices 22)
+            o = block_sort(s, o, by_count ? min(n, k) : n);
+            w = o ? ~o & ((1ull << 41) - 1) : 0;
+            const u64 upto = block_scan(s, w, &all), t = place_in(all);
+            if (upto - w <= t && t < upto) out((int)(~o >> 41), kept, (float)((double)w / (double)all));
+        };
         u64 total = 0;
         bool by_count = k > 0;
+        // The top_k-th largest of the threads' own largest is no larger than the top_k-th of all: with few wanted, what lies from its bin on is listed without
+        // counting all tokens, and most often fits the list.
+        if (by_count && k <= NT / 4) {
+            const float b = place(infinite ? (own_top == INFINITY ? 0.f : -INFINITY) : own_top);
+            if (b < SAMPLE_REACH) atomicAdd(&s.count[(int)b], 1);
+            __syncthreads();
+            find_bin<NT, false>(s, true, (u64)k, 0, 0);
+            const int found = s.found;
+            if (found >= 0) {
+                list_upto(found);
+                const int n = s.n_list;
+                if (n <= NT) {
+                    draw_listed(n, true, 0);
+                    return;
+                }
+            }
+            clear();
+            if (tid == 0) s.n_list = 0;
+        }
         if (by_count) {
             all_of([&](float v, int) {
                 const float b = place(v);
@@ -283,26 +343,12 @@ __global__ __launch_bounds__(NT) void sample_kernel(Sample c, int vocab) {
         if (by_count || p_on) {
             const int few = s.found_before + s.found_count;
             if (few <= NT) {
-                const float end = (float)(s.found + 1);
-                all_of([&](float v, int i) { if (place(v) < end) s.list[atomicAdd(&s.n_list, 1)] = composite(v, i); });
-                __syncthreads();
-                u64 e = tid < few ? s.list[tid] : 0;
-                e = block_sort(s, e, few);
-                u64 w = tid < few && !(by_count && tid >= k) ? weight(logit_of(e)) : 0, all;
-                const u64 before = block_scan(s, w, &all) - w;
-                if (by_count) total = all;
-                const bool keep = w >= least && (!p_on || tid == 0 || before < limit_of(total));
-                int kept;
-                block_scan(s, (int)keep, &kept);
-                u64 o = keep ? ~((u64)index_of(e) << 41 | w) : 0;    // (weights have 41 bits, indices 22)
-                o = block_sort(s, o, few);
-                w = o ? ~o & ((1ull << 41) - 1) : 0;
-                const u64 upto = block_scan(s, w, &all), t = place_in(all);
-                if (upto - w <= t && t < upto) out((int)(~o >> 41), kept, (float)((double)w / (double)all));
+                list_upto(s.found);
+                draw_listed(few, by_count, total);
                 return;
             }
             // the last composite that is kept, the cut lying in the bin that was found: digit by digit, among the tokens of the bin, from the list if they fit
-            auto find_cut = [&](bool count_mode, u64 limit, u64* sum_upto) -> u64 {
+            auto find_cut = [&](bool count_mode, u64 limit, u64* sum_upto) __attribute__((always_inline)) -> u64 {
                 const float b = (float)s.found;
                 const int n = s.found_count;
                 int before = s.found_before;
@@ -311,14 +357,14 @@ __global__ __launch_bounds__(NT) void sample_kernel(Sample c, int vocab) {
                 __syncthreads();
                 if (tid == 0) s.n_list = 0, s.lowest = ~0ull;
                 __syncthreads();
-                auto of_bin = [&](auto&& f) {
+                auto of_bin = [&](auto&& f) __attribute__((always_inline)) {
                     all_of([&](float v, int i) {
                         const float at = place(v);
                         if (at >= b && at < b + 1.f && (!cut || composite(v, i) >= cut)) f(composite(v, i));
                     });
                 };
                 if (listed) of_bin([&](u64 e) { s.list[atomicAdd(&s.n_list, 1)] = e; });
-                auto members = [&](auto&& f) {
+                auto members = [&](auto&& f) __attribute__((always_inline)) {
                     if (listed) {
                         for (int i = tid; i < n; i += NT) f(s.list[i]);
                     } else {
@@ -326,6 +372,18 @@ __global__ __launch_bounds__(NT) void sample_kernel(Sample c, int vocab) {
                     }
                     __syncthreads();
                 };
+                if (n <= NT) {
+                    __syncthreads();
+                    u64 e = tid < n ? s.list[tid] : 0, all;
+                    e = block_sort(s, e, n);
+                    const u64 w = tid < n ? weight(logit_of(e)) : 0, upto = block_scan(s, w, &all) + before_sum;
+                    const bool keep = tid < n && (count_mode ? (u64)(before + tid) < limit : tid == 0 || upto - w < limit);
+                    const int kept = __syncthreads_count(keep);
+                    if (tid == kept - 1) s.lowest = e, s.found_sum = upto;
+                    __syncthreads();
+                    *sum_upto = s.found_sum;
+                    return s.lowest;
+                }
                 u64 prefix = 0;
                 int shift = 54;
                 for (int d = 0; d < 5; ++d) {
@@ -374,35 +432,49 @@ __global__ __launch_bounds__(NT) void sample_kernel(Sample c, int vocab) {
         const float low = top - 1.0001f * temperature * (0.001f - __logf(fminf(min_p, 1.f))) - 1e-6f * fabsf(top);
         if (low <= top) bar = fmaxf(bar, low);
     }
-    auto kept_weight = [&](float v, int i) -> u64 {
+    auto kept_weight = [&](float v, int i) __attribute__((always_inline)) -> u64 {
         if (!(v >= bar) || (v == cut_at && i > cut_index)) return 0;
         const u64 w = weight(v);
         return w >= least ? w : 0;
     };
-    const int stretch = ((vocab + NW - 1) / NW + 255) & ~255;
-    u64 sum = 0;
+    // chunks of a wave's share, so that a thread has few tokens to go through where the place is
+    constexpr int UNIT = HELD ? 256 : 512, CHUNKS = HELD ? 1 : SAMPLE_BINS / NW;
+    const int per_wave = (vocab + NW - 1) / NW, chunk = ((per_wave + CHUNKS - 1) / CHUNKS + UNIT - 1) / UNIT * UNIT, n_chunks = (per_wave + chunk - 1) / chunk;
+    const int mine = wave * n_chunks * chunk;
     int n = 0;
-    const int mine = wave * stretch;
-    each(std::integral_constant<int, 64>{}, mine, min(mine + stretch, padded), lane, [&](float v, int i) {
-        const u64 w = kept_weight(v, i);
-        sum += w;
-        n += w != 0;
-    });
+    __syncthreads();
+    for (int j = 0; j < n_chunks; ++j) {
+        u64 sum = 0;
+        each(std::integral_constant<int, 64>{}, mine + j * chunk, min(mine + (j + 1) * chunk, padded), lane, [&](float v, int i) {
+            const u64 w = kept_weight(v, i);
+            sum += w;
+            n += w != 0;
+        });
+        if (__builtin_amdgcn_ballot_w64(sum != 0)) {
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
+            for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
+        }
+        if (lane == 0) s.sum[wave * n_chunks + j] = sum;
+    }
     int kept;
+    u64 all;
     block_scan(s, n, &kept);
     __syncthreads();
-    if (lane == 0) s.wave_sum[wave] = sum;
-    __syncthreads();
-    u64 all = 0;
+    // the chunk that holds the place
+    constexpr int PER = SAMPLE_BINS / NT;
+    u64 own_sum[PER], mass = 0;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) all += s.wave_sum[w];
+    for (int j = 0; j < PER; ++j) mass += own_sum[j] = tid * PER + j < NW * n_chunks ? s.sum[tid * PER + j] : 0;
+    u64 before = block_scan(s, mass, &all) - mass;
     const u64 t = place_in(all);
-    int part = 0;
-    u64 before = 0;
-    for (; part < NW - 1 && before + s.wave_sum[part] <= t; ++part) before += s.wave_sum[part];
-    const int first = part * stretch, end = min(first + stretch, vocab), own = (stretch + NT - 1) / NT;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        if (before <= t && t < before + own_sum[j]) s.found = tid * PER + j, s.found_before_sum = before;
+        before += own_sum[j];
+    }
+    __syncthreads();
+    before = s.found_before_sum;
+    const int first = s.found * chunk, end = min(first + chunk, vocab), own = (chunk + NT - 1) / NT;
     const int a = min(first + tid * own, end), b = min(a + own, end);
     auto at = [&](int i) -> float {
         const float v = HELD ? held[i] : x[i];
