@@ -2,9 +2,11 @@
 //   k, v [n_pages][heads][page][d] bf16; slot j of sequence s lies on page table[s][j / page] at j % page.  page is a power of two from 16 on, so
 // that 16 slots that begin at a multiple of 16 lie on one page.
 #include <algorithm>
+#include <type_traits>
 
 #include "kernels.h"
 
+typedef int i32x4_t __attribute__((ext_vector_type(4)));
 typedef unsigned u32x2_t __attribute__((ext_vector_type(2)));
 typedef unsigned u32x4_t __attribute__((ext_vector_type(4)));
 
@@ -384,8 +386,203 @@ __device__ __forceinline__ unsigned order_key(float w) {
     const unsigned u = __float_as_uint(w + 0.f);           // (-0 counts as 0)
     return w != w ? 0u : u & 0x80000000u ? ~u : u | 0x80000000u;
 }
+// the bin, from the last down, in which the count first reaches `need`: *bin, and what of `need` is left for it (hist: BINS counts)
+template <int NT, int BINS>
+__device__ __forceinline__ void find_from_top(const int* hist, int* sums, int* found, int need, int* bin, int* left) {
+    constexpr int N = 2048 / NT;                           // bins a thread (with 1024 bins half the threads have none)
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, hi = BINS - 1 - N * threadIdx.x;
+    int c[N], all = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) c[i] = hi - i >= 0 ? hist[hi - i] : 0, all += c[i];
+    int run = all;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const int o = __shfl_up(run, off, 64);
+        if (lane >= off) run += o;
+    }
+    if (lane == 63) sums[wave] = run;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) run += sums[w];
+    run -= all;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if (run < need && need <= run + c[i]) found[0] = hi - i, found[1] = need - run;
+        run += c[i];
+    }
+    __syncthreads();
+    *bin = found[0];
+    *left = found[1];
+}
+// Up to 32 slots a thread: weights, positions and then keys stay in registers from their one reading on.  Thread t has slots 4 (k NT + t) + e for k < K,
+// e = 0 .. 3, as bits 4 k + e of a mask.  32768 slots of 32 heads: 146 us where every pass read them again, with two barriers and three counts over
+// the waves for each 1024 slots.
+template <int NT, int K>
+__global__ __launch_bounds__(NT, 4) void evict_select_kernel(Paged c, const int* __restrict__ lengths, int budget, int n_recent, const float* w_in, const int* p_in,
+                                                          long ldw, float* w_out, int* p_out, int* __restrict__ ws, long ws_ld) {
+    constexpr int NWV = NT / 64;
+    __shared__ int hist[2048];
+    __shared__ int sums[NWV], counts[K * NWV], found[2];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), seq = blockIdx.x / c.heads;
+    const long row = (long)blockIdx.x * ldw;
+    int* list = ws + (long)blockIdx.x * ws_ld;
+    const int len = (int)min((long)max(lengths[seq], 0), min(ldw, (long)c.n_table << c.shift));
+    if (len <= budget) {
+        if (tid == 0) list[0] = ~len;
+        for (int i = tid; i < len; i += NT) {
+            if (w_out != w_in) w_out[row + i] = w_in[row + i];
+            if (p_out != p_in) p_out[row + i] = p_in[row + i];
+        }
+        return;
+    }
+    f32x4_t w[K];
+    i32x4_t p[K];
+    int id[K];
+    const float* wr = w_in + row;
+    const int* pr = p_in + row;
+    const int* tr = c.table + (long)seq * c.n_table;
+    constexpr int NEVER = -0x7fffffff - 1;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const unsigned i = 4 * (k * NT + tid);
+        w[k] = f32x4_t{0.f, 0.f, 0.f, 0.f}, p[k] = i32x4_t{NEVER, NEVER, NEVER, NEVER};
+        if (i + 4 <= (unsigned)len) w[k] = *(const f32x4_t*)(wr + i), p[k] = *(const i32x4_t*)(pr + i);
+        id[k] = i < (unsigned)len ? tr[i >> c.shift] : -1;
+    }
+    if ((len & 3) && tid == (len >> 2) % NT) {             // the last slots, fewer than four
+        f32x4_t wt = {0.f, 0.f, 0.f, 0.f};
+        i32x4_t pt = {NEVER, NEVER, NEVER, NEVER};
+        for (int i = len & ~3, e = 0; e < 3; ++e)
+            if (i + e < len) wt[e] = wr[i + e], pt[e] = pr[i + e];
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            if (k == (len >> 2) / NT) w[k] = wt, p[k] = pt;
+    }
+    for (int i = tid; i < 2048; i += NT) hist[i] = 0;
+    int newest = -0x7fffffff - 1;
+#pragma unroll
+    for (int k = 0; k < K; ++k) newest = max(newest, max(max(p[k][0], p[k][1]), max(p[k][2], p[k][3])));
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) newest = max(newest, __shfl_xor(newest, off, 64));
+    if (lane == 0) sums[wave] = newest;
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < NWV; ++x) newest = max(newest, sums[x]);
+    const long border = (long)newest - n_recent;
+    unsigned key[K][4];
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) key[k][e] = id[k] < 0 || id[k] >= c.n_pages ? 0u : (long)p[k][e] > border ? 0xffffffffu : order_key(w[k][e]);
+    __builtin_amdgcn_sched_barrier(0);
+    unsigned prefix = 0;
+    int need = budget;                                     // of the slots whose key begins with the prefix, so many stay
+    auto digit = [&](auto shift_of, auto above_of) {
+        constexpr int SHIFT = decltype(shift_of)::value, ABOVE = decltype(above_of)::value, BINS = 1 << (ABOVE - SHIFT);
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (4 * (k * NT + tid) + e < len && (ABOVE == 32 || key[k][e] >> (ABOVE & 31) == prefix >> (ABOVE & 31))) atomicAdd(&hist[key[k][e] >> SHIFT & (BINS - 1)], 1);
+        __syncthreads();
+        int bin;
+        find_from_top<NT, BINS>(hist, sums, found, need, &bin, &need);
+        prefix |= (unsigned)bin << SHIFT;
+        if (SHIFT) {
+            for (int i = tid; i < 2048; i += NT) hist[i] = 0;
+            __syncthreads();
+        }
+    };
+    using std::integral_constant;
+    digit(integral_constant<int, 21>{}, integral_constant<int, 32>{});
+    digit(integral_constant<int, 10>{}, integral_constant<int, 21>{});
+    digit(integral_constant<int, 0>{}, integral_constant<int, 10>{});
+    const int n_equal = hist[prefix & 1023];
+    // f(bit, how many bits are set for slots before it) for each set bit; returns how many there are
+    auto in_order = [&](unsigned mask, auto&& f) -> int {
+        int below[K];
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            int before = 0, all = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const unsigned long long b = __ballot(mask >> (4 * k + e) & 1);
+                before += __popcll(b & ((1ull << lane) - 1));
+                all += __popcll(b);
+            }
+            below[k] = before;
+            if (lane == 0) counts[k * NWV + wave] = all;
+            __builtin_amdgcn_sched_barrier(0);             // (the masks of all eight would not fit the registers)
+        }
+        __syncthreads();
+        constexpr int PER = K * NWV / 64 > 0 ? K * NWV / 64 : 1;      // counts a lane, in order
+        int c2[PER], mine = 0;
+#pragma unroll
+        for (int x = 0; x < PER; ++x) c2[x] = lane * PER + x < K * NWV ? counts[lane * PER + x] : 0, mine += c2[x];
+        int run = mine;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const int o = __shfl_up(run, off, 64);
+            if (lane >= off) run += o;
+        }
+        const int total = __shfl(run, 63, 64);
+        run -= mine;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int at = k * NWV + wave;                 // (uniform)
+            int base = 0, upto = run;
+#pragma unroll
+            for (int x = 0; x < PER; ++x) {
+                const int here = __shfl(upto, at / PER, 64);
+                if (at % PER == x) base = here;
+                upto += c2[x];
+            }
+            int rank = base + below[k];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (mask >> (4 * k + e) & 1) f(4 * k + e, rank++);
+        }
+        return total;
+    };
+    unsigned keep = 0, equal = 0;
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const bool there = 4 * (k * NT + tid) + e < len;
+            if (there && key[k][e] > prefix) keep |= 1u << (4 * k + e);
+            if (there && key[k][e] == prefix) equal |= 1u << (4 * k + e);
+        }
+    if (n_equal == need) keep |= equal;                    // (uniform)
+    else {
+        in_order(equal, [&](int bit, int rank) { if (rank < need) keep |= 1u << bit; });
+        __syncthreads();
+    }
+    // slots that become free and, behind them in the order of the slots, as many that move there
+    unsigned marked = 0;
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int i = 4 * (k * NT + tid) + e;
+            if (i < len && (keep >> (4 * k + e) & 1) == (i >= budget)) marked |= 1u << (4 * k + e);
+        }
+    const int n = in_order(marked, [&](int bit, int rank) { if (rank < ws_ld - 1) list[1 + rank] = 4 * ((bit >> 2) * NT + tid) + (bit & 3); });
+    if (tid == 0) list[0] = n >> 1;
+    if (w_out == w_in && p_out == p_in) return;
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int i = 4 * (k * NT + tid) + e;
+            if (i < budget && keep >> (4 * k + e) & 1) {
+                if (w_out != w_in) w_out[row + i] = w_in[row + i];
+                if (p_out != p_in) p_out[row + i] = p_in[row + i];
+            }
+        }
+}
+// The same for any number of slots, which are read again by every pass; the slots that move there lie `most` behind those that become free.
 constexpr int EVICT_NT = 1024;
-__global__ __launch_bounds__(EVICT_NT) void evict_select_kernel(Paged c, const int* __restrict__ lengths, int budget, int n_recent, const float* w_in,
+__global__ __launch_bounds__(EVICT_NT) void evict_select_long_kernel(Paged c, const int* __restrict__ lengths, int budget, int n_recent, const float* w_in,
                                                                 const int* p_in, long ldw, float* w_out, int* p_out, int* __restrict__ ws, long ws_ld) {
     constexpr int NT = EVICT_NT, NWV = NT / 64;
     __shared__ int hist[2048];
@@ -428,23 +625,10 @@ __global__ __launch_bounds__(EVICT_NT) void evict_select_kernel(Paged c, const i
             if (d == 0 || key >> above == prefix >> above) atomicAdd(&hist[key >> shift & (bins - 1)], 1);
         }
         __syncthreads();
-        // from the top: thread t has the two bins bins - 1 - 2 t and the one below
-        const int hi = bins - 1 - 2 * tid, a = hi >= 0 ? hist[hi] : 0, b = hi >= 1 ? hist[hi - 1] : 0;
-        int run = a + b;
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            const int o = __shfl_up(run, off, 64);
-            if (lane >= off) run += o;
-        }
-        if (lane == 63) sums[0][wave] = run;
-        __syncthreads();
-        for (int w = 0; w < wave; ++w) run += sums[0][w];
-        const int before = run - a - b;
-        if (a && before < need && need <= before + a) found[0] = hi, found[1] = need - before;
-        if (b && before + a < need && need <= run) found[0] = hi - 1, found[1] = need - before - a;
-        __syncthreads();
-        prefix |= (unsigned)found[0] << shift;
-        need = found[1];
+        int bin;
+        if (d == 2) find_from_top<NT, 1024>(hist, sums[0], found, need, &bin, &need);
+        else find_from_top<NT, 2048>(hist, sums[0], found, need, &bin, &need);
+        prefix |= (unsigned)bin << shift;
     }
     // in the order of the slots: equal keys, slots that become free below the budget, kept ones behind it
     int n_equal = 0, n_free = 0, n_move = 0;
@@ -466,37 +650,34 @@ __global__ __launch_bounds__(EVICT_NT) void evict_select_kernel(Paged c, const i
         int f = n_free + __popcll(fr & below), m = n_move + __popcll(mv & below);
         for (int w = 0; w < wave; ++w) f += sums[1][w], m += sums[2][w];
         const long most = (ws_ld - 1) >> 1;
-        if (free && f < most) list[1 + most + f] = i;
-        if (move && m < most) list[1 + m] = i;
+        if (free && f < most) list[1 + f] = i;
+        if (move && m < most) list[1 + most + m] = i;
         if (i < budget && keep) {
             if (w_out != w_in) w_out[row + i] = w_in[row + i];
             if (p_out != p_in) p_out[row + i] = p_in[row + i];
         }
         for (int w = 0; w < NWV; ++w) n_equal += sums[0][w], n_free += sums[1][w], n_move += sums[2][w];
     }
-    __threadfence_block();
-    __syncthreads();
-    const long most = (ws_ld - 1) >> 1;
-    for (int i = tid; i < n_move; i += NT) {               // (as many become free as move)
-        const int from = list[1 + i], to = list[1 + most + i];
-        w_out[row + to] = w_in[row + from];
-        p_out[row + to] = p_in[row + from];
-    }
     if (tid == 0) list[0] = n_move;
 }
-// The rows of the pairs, D / 8 lanes each for k and for v, 32 pairs a workgroup; and the new lengths.
-__global__ __launch_bounds__(256) void evict_move_kernel(Paged c, int budget, const int* __restrict__ ws, long ws_ld, int* __restrict__ lengths_out, int n_chunks) {
+// The rows of the pairs, d / 8 lanes each for k and for v, 32 pairs a workgroup at a time, their weights and positions, and the new lengths.  apart: how far behind
+// the first free slot of a list the first one that moves lies (0: as many as there are).
+__global__ __launch_bounds__(256) void evict_move_kernel(Paged c, int budget, const int* __restrict__ ws, long ws_ld, long apart, const float* w_in, const int* p_in,
+                                                         long ldw, float* w_out, int* p_out, int* __restrict__ lengths_out, int n_chunks) {
     const int sh = blockIdx.x / n_chunks, chunk = blockIdx.x % n_chunks, seq = sh / c.heads, head = sh % c.heads;
     const int* list = ws + (long)sh * ws_ld;
     const int n = list[0];
     if (head == 0 && chunk == 0 && threadIdx.x == 0) lengths_out[seq] = n < 0 ? ~n : budget;
-    const long most = (ws_ld - 1) >> 1;
+    const int* froms = list + 1 + (apart ? apart : n);
+    const long row = (long)sh * ldw;
     const int per = c.d >> 3, pairs = 128 / per, which = threadIdx.x / (2 * per), part = threadIdx.x % (2 * per);
     bf16_t* at = part < per ? c.k : c.v;
     const int e = part % per * 8;
     for (long i0 = chunk * 32L; i0 < n; i0 += n_chunks * 32L) {
         for (long i = i0 + which; i < min((long)n, i0 + 32); i += pairs) {
-            const int from = list[1 + i], to = list[1 + most + i], a = page_of(c, seq, from), b = page_of(c, seq, to);
+            const int from = froms[i], to = list[1 + i], a = page_of(c, seq, from), b = page_of(c, seq, to);
+            if (part == 0) w_out[row + to] = w_in[row + from];
+            else if (part == 1) p_out[row + to] = p_in[row + from];
             if (a >= 0 && b >= 0) *(uint4*)(at + slot_at(c, b, head, to) + e) = *(const uint4*)(at + slot_at(c, a, head, from) + e);
         }
     }
@@ -505,9 +686,18 @@ hipError_t launch_paged_evict(const Paged& c, const int* lengths, int budget, in
                               int* p_out, int* lengths_out, int* ws, hipStream_t s) {
     const long cap = (long)c.n_table << c.shift, width = cap < ldw ? cap : ldw;
     const long most = width - budget < budget ? (width - budget > 0 ? width - budget : 0) : budget, ld = 1 + 2 * most;
-    evict_select_kernel<<<c.n_seqs * c.heads, EVICT_NT, 0, s>>>(c, lengths, budget, n_recent, w_in, p_in, ldw, w_out, p_out, ws, ld);
+    const int rows = c.n_seqs * c.heads;
+    // Many threads a row, few slots a thread: latency bounds these kernels.  us, 64 sequences of 8 heads and 2112 slots with 256 threads of up to 32 / 16 slots,
+    // 512 of 8, 1024 of 4: 25.5 / 20.5 / 18.3 / 17.2 for the call
+    auto select = [&](auto kernel, int threads) { kernel<<<rows, threads, 0, s>>>(c, lengths, budget, n_recent, w_in, p_in, ldw, w_out, p_out, ws, ld); };
+    if (width <= 1024) select(evict_select_kernel<256, 1>, 256);
+    else if (width <= 4096) select(evict_select_kernel<1024, 1>, 1024);
+    else if (width <= 8192) select(evict_select_kernel<1024, 2>, 1024);
+    else if (width <= 16384) select(evict_select_kernel<1024, 4>, 1024);
+    else if (width <= 32768) select(evict_select_kernel<1024, 8>, 1024);
+    else select(evict_select_long_kernel, EVICT_NT);
     const long room = (1L << 24) / ((long)c.n_seqs * c.heads);
     const int n_chunks = most > 0 ? (int)(cdiv(most, 32) < room ? cdiv(most, 32) : room < 1 ? 1 : room) : 1;
-    evict_move_kernel<<<c.n_seqs * c.heads * n_chunks, 256, 0, s>>>(c, budget, ws, ld, lengths_out, n_chunks);
+    evict_move_kernel<<<c.n_seqs * c.heads * n_chunks, 256, 0, s>>>(c, budget, ws, ld, width <= 32 * 1024 ? 0 : most, w_in, p_in, ldw, w_out, p_out, lengths_out, n_chunks);
     return hipGetLastError();
 }

@@ -309,3 +309,38 @@ def test_evict_pages_that_are_not_there_and_short_rows(api):
     check_evict(api, k.clone(), v.clone(), table, ints([400, 390, 250]), 200, 50, w, p, False)
     # weights for fewer slots than the table has room for: lengths count as that
     check_evict(api, k, v, table, ints([400, 390, 250]), 200, 50, w[:, :, :300].contiguous(), p[:, :, :300].contiguous(), True)
+
+
+@pytest.mark.parametrize("n,budget", [(8191, 3000), (8192, 100), (8193, 5000), (8195, 8194), (20001, 4096), (32768, 4096), (32769, 9000), (40003, 39000)])
+def test_evict_of_many_slots(api, n, budget):
+    """slots held by 256 and by 1024 threads, and read again; with many equal weights"""
+    g = gen(n)
+    kv, page, d = 2, 64, 64
+    n_table = -(-n // page)
+    k, v = (bf16(g, n_table, kv, page, d) for _ in range(2))
+    table = torch.randperm(n_table, generator=g)[None].int()
+    w = torch.rand(1, kv, n, generator=g)
+    w[0, 1] = (w[0, 1] * 4).floor()
+    p = torch.randperm(n, generator=g)[None, None].expand(1, kv, n).int().contiguous()
+    cache = on_gpu(api, k, v, table)
+    for recent in (0, budget // 3):
+        key = torch.where(p > p.max() - recent, math.inf, w)
+        order = torch.sort(key, dim=2, descending=True, stable=True).indices[0, :, :budget]
+        wo, po = torch.zeros(1, kv, n, device="cuda"), torch.zeros(1, kv, n, dtype=torch.int32, device="cuda")
+        c = on_gpu(api, k, v, table)
+        L = torch.zeros(1, dtype=torch.int32, device="cuda")
+        most = max(0, min(budget, min(n, n_table * page) - budget))
+        api.tl_k_paged_evict(c, ints([n]).cuda(), budget, recent, w.cuda(), p.cuda(), wo, po, L, torch.empty(kv * (2 * most + 1), device="cuda"))
+        assert L.tolist() == [budget]
+        for h in range(kv):
+            kept = torch.zeros(n, dtype=torch.bool)
+            kept[order[h]] = True
+            now = torch.arange(budget)
+            now[~kept[:budget]] = budget + kept[budget:].nonzero()[:, 0]
+            assert torch.equal(wo[0, h, :budget].cpu(), w[0, h, now]) and torch.equal(po[0, h, :budget].cpu(), p[0, h, now])
+            slots = torch.arange(n)
+            slots[:budget] = now
+            for x, y in ((c.k, k), (c.v, v)):
+                at = table[0].long()
+                got = x.cpu()[at, h].reshape(-1, d)[:n]
+                assert torch.equal(got, y[at, h].reshape(-1, d)[slots])
