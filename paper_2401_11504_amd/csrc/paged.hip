@@ -662,6 +662,7 @@ __global__ __launch_bounds__(EVICT_NT) void evict_select_long_kernel(Paged c, co
 }
 // The rows of the pairs, d / 8 lanes each for k and for v, 32 pairs a workgroup at a time, their weights and positions, and the new lengths.  apart: how far behind
 // the first free slot of a list the first one that moves lies (0: as many as there are).
+template <int D>
 __global__ __launch_bounds__(256) void evict_move_kernel(Paged c, int budget, const int* __restrict__ ws, long ws_ld, long apart, const float* w_in, const int* p_in,
                                                          long ldw, float* w_out, int* p_out, int* __restrict__ lengths_out, int n_chunks) {
     const int sh = blockIdx.x / n_chunks, chunk = blockIdx.x % n_chunks, seq = sh / c.heads, head = sh % c.heads;
@@ -670,15 +671,34 @@ __global__ __launch_bounds__(256) void evict_move_kernel(Paged c, int budget, co
     if (head == 0 && chunk == 0 && threadIdx.x == 0) lengths_out[seq] = n < 0 ? ~n : budget;
     const int* froms = list + 1 + (apart ? apart : n);
     const long row = (long)sh * ldw;
-    const int per = c.d >> 3, pairs = 128 / per, which = threadIdx.x / (2 * per), part = threadIdx.x % (2 * per);
-    bf16_t* at = part < per ? c.k : c.v;
-    const int e = part % per * 8;
+    constexpr int PER = D >> 3, PAIRS = 128 / PER, U = 32 / PAIRS;      // lanes of a row, pairs at a time, times
+    const int which = threadIdx.x / (2 * PER), part = threadIdx.x % (2 * PER);
+    bf16_t* at = (part < PER ? c.k : c.v) + part % PER * 8;
     for (long i0 = chunk * 32L; i0 < n; i0 += n_chunks * 32L) {
-        for (long i = i0 + which; i < min((long)n, i0 + 32); i += pairs) {
-            const int from = froms[i], to = list[1 + i], a = page_of(c, seq, from), b = page_of(c, seq, to);
-            if (part == 0) w_out[row + to] = w_in[row + from];
-            else if (part == 1) p_out[row + to] = p_in[row + from];
-            if (a >= 0 && b >= 0) *(uint4*)(at + slot_at(c, b, head, to) + e) = *(const uint4*)(at + slot_at(c, a, head, from) + e);
+        int from[U], to[U], a[U], b[U];
+        u32x4_t x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const long i = min(i0 + u * PAIRS + which, (long)n - 1);        // (behind the last pair: that one again)
+            from[u] = froms[i], to[u] = list[1 + i];
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) a[u] = page_of(c, seq, from[u]), b[u] = page_of(c, seq, to[u]);
+#pragma unroll
+        for (int u = 0; u < U; ++u) x[u] = *(const u32x4_t*)(at + slot_at(c, max(a[u], 0), head, from[u]));
+        float w[U];
+        int p[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (part == 0) w[u] = w_in[row + from[u]];
+            if (part == 1) p[u] = p_in[row + from[u]];
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (i0 + u * PAIRS + which >= n) break;
+            if (a[u] >= 0 && b[u] >= 0) *(u32x4_t*)(at + slot_at(c, b[u], head, to[u])) = x[u];
+            if (part == 0) w_out[row + to[u]] = w[u];
+            if (part == 1) p_out[row + to[u]] = p[u];
         }
     }
 }
@@ -698,6 +718,10 @@ hipError_t launch_paged_evict(const Paged& c, const int* lengths, int budget, in
     else select(evict_select_long_kernel, EVICT_NT);
     const long room = (1L << 24) / ((long)c.n_seqs * c.heads);
     const int n_chunks = most > 0 ? (int)(cdiv(most, 32) < room ? cdiv(most, 32) : room < 1 ? 1 : room) : 1;
-    evict_move_kernel<<<c.n_seqs * c.heads * n_chunks, 256, 0, s>>>(c, budget, ws, ld, width <= 32 * 1024 ? 0 : most, w_in, p_in, ldw, w_out, p_out, lengths_out, n_chunks);
+    auto move = [&](auto kernel) {
+        kernel<<<c.n_seqs * c.heads * n_chunks, 256, 0, s>>>(c, budget, ws, ld, width <= 32768 ? 0 : most, w_in, p_in, ldw, w_out, p_out, lengths_out, n_chunks);
+    };
+    if (c.d == 128) move(evict_move_kernel<128>);
+    else move(evict_move_kernel<64>);
     return hipGetLastError();
 }
