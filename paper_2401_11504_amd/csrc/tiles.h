@@ -41,6 +41,9 @@ __device__ __forceinline__ void load_lds16(unsigned voff, const void* sbase, uns
 __device__ __forceinline__ void load_lds4(const void* p, unsigned lds_addr) {
     asm volatile("global_load_lds_dword %0, off" ::"v"(p), "{m0}"(lds_addr) : "memory");
 }
+__device__ __forceinline__ void load_lds4s(unsigned voff, const void* sbase, unsigned lds_addr) {
+    asm volatile("global_load_lds_dword %0, %1" ::"v"(voff), "s"(sbase), "{m0}"(lds_addr) : "memory");
+}
 // 16 bytes a lane to lds_addr + 16 lane, by such a load (DIRECT) or, where the address may be no multiple of 4, through registers (waited for at once)
 template <bool DIRECT>
 __device__ __forceinline__ void bring_lds16(unsigned voff, const void* sbase, unsigned lds_addr, int lane) {
@@ -72,6 +75,8 @@ struct TileFetch {
     int lane, fr;
     unsigned fc;
     __device__ __forceinline__ TileFetch(int lane) : lane(lane), fr(lane / CPR), fc((unsigned)((lane % CPR) ^ tile_swz<DH>(lane / CPR)) << 4) {}
+    // this lane's part of the address of fetch i where all its rows are there
+    __device__ __forceinline__ unsigned offset(unsigned ldb, int i) const { return (unsigned)(i * RPI + fr) * ldb + (fc ^ (unsigned)((i * (RPI / 4) & 3) << 4)); }
     __device__ __forceinline__ void operator()(const bf16_t* base, unsigned ldb, int i, int last, unsigned lds) const {
         const unsigned c = fc ^ (unsigned)((i * (RPI / 4) & 3) << 4);                  // swz of rows i RPI + fr
         bring_lds16<DIRECT>((unsigned)min(i * RPI + fr, last) * ldb + c, base, lds + i * 1024, lane);
