@@ -48,6 +48,35 @@ __device__ __forceinline__ u64 composite(float v, int i) { return (u64)key_of_lo
 __device__ __forceinline__ float logit_of(u64 e) { return logit_of_key((unsigned)(e >> 22)); }
 __device__ __forceinline__ int index_of(u64 e) { return 0x3fffff - (int)(e & 0x3fffff); }
 
+// a value of another lane of the wave by DPP (lanes without one: 0); 64 bits as two halves
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ int dpp(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ u64 dpp(u64 v) {
+    return (u64)(unsigned)dpp<CTRL, ROWS>((int)(v >> 32)) << 32 | (unsigned)dpp<CTRL, ROWS>((int)(unsigned)v);
+}
+// inclusive sums over the lanes of a wave: along rows of 16, then the rows' ends into the rows behind
+template <class N>
+__device__ __forceinline__ N wave_scan(N v) {
+    v += dpp<0x111>(v);                                    // row_shr:1
+    v += dpp<0x112>(v);
+    v += dpp<0x114>(v);
+    v += dpp<0x118>(v);
+    v += dpp<0x142, 0xa>(v);                               // row_bcast:15 into rows 1 and 3
+    v += dpp<0x143, 0xc>(v);                               // row_bcast:31 into rows 2 and 3
+    return v;
+}
+// the value of lane ^ j
+__device__ __forceinline__ u64 lane_xor(u64 v, int j) {
+    switch (j) {
+        case 1: return dpp<0xb1>(v);                       // quad_perm
+        case 2: return dpp<0x4e>(v);
+        case 4: return dpp<0x1b>(dpp<0x141>(v));           // mirrored in half rows, mirrored in fours
+        case 8: return dpp<0x128>(v);                      // row_ror:8
+        default: return __shfl_xor(v, j, 64);
+    }
+}
+
 template <int NT, int LIST>
 struct SampleLds {
     u64 sum[SAMPLE_BINS];
@@ -62,11 +91,7 @@ template <class S, class N>
 __device__ __forceinline__ N block_scan(S& s, N v, N* all) {
     constexpr int NW = sizeof(s.wave_sum) / sizeof(u64);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        const N o = __shfl_up(v, off, 64);
-        if (lane >= off) v += o;
-    }
+    v = wave_scan(v);
     __syncthreads();
     if (lane == 63) s.wave_sum[wave] = (u64)v;
     __syncthreads();
@@ -111,19 +136,28 @@ __device__ __forceinline__ u64 block_sort(S& s, u64 v, int n) {
     int size = 64;
     while (size < n) size <<= 1;
     const int t = threadIdx.x;
-    for (int k = 2; k <= size; k <<= 1) {
-        for (int j = k >> 1; j > 0; j >>= 1) {
-            u64 o;
-            if (j < 64) o = __shfl_xor(v, j, 64);
-            else {
-                __syncthreads();
-                s.list[t] = v;
-                __syncthreads();
-                o = s.list[t ^ j];
-            }
-            const bool larger = ((t & k) == 0) == ((t & j) == 0);      // this one keeps the larger
-            v = larger ? (v > o ? v : o) : (v < o ? v : o);
+    auto keep = [&](u64 o, int k, int j) {
+        const bool larger = ((t & k) == 0) == ((t & j) == 0);          // this one keeps the larger
+        v = larger == (v > o) ? v : o;
+    };
+    auto in_wave = [&](int k) {
+        if (k >= 64) keep(lane_xor(v, 32), k, 32);
+        if (k >= 32) keep(lane_xor(v, 16), k, 16);
+        if (k >= 16) keep(lane_xor(v, 8), k, 8);
+        if (k >= 8) keep(lane_xor(v, 4), k, 4);
+        if (k >= 4) keep(lane_xor(v, 2), k, 2);
+        keep(lane_xor(v, 1), k, 1);
+    };
+#pragma unroll
+    for (int k = 2; k <= 64; k <<= 1) in_wave(k);
+    for (int k = 128; k <= size; k <<= 1) {
+        for (int j = k >> 1; j >= 64; j >>= 1) {
+            __syncthreads();
+            s.list[t] = v;
+            __syncthreads();
+            keep(s.list[t ^ j], k, j);
         }
+        in_wave(k);
     }
     return v;
 }
