@@ -295,17 +295,40 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab) {
         return t < all ? t : all - 1;
     };
     u64 cut = 0;                                           // kept: composites from here on
+    // What is kept of each chunk of the row, to s.sum; a wave's share is n_chunks of them, so that a thread has few tokens to go through where the place is.
+    // Returns how many tokens this thread saw that are.
+    constexpr int UNIT = HELD ? 256 : 512, CHUNKS = HELD ? 1 : SAMPLE_BINS / NW;
+    const int per_wave = (vocab + NW - 1) / NW, chunk = ((per_wave + CHUNKS - 1) / CHUNKS + UNIT - 1) / UNIT * UNIT, n_chunks = (per_wave + chunk - 1) / chunk;
+    auto sum_chunks = [&](auto&& kept_of) __attribute__((always_inline)) -> int {
+        const int mine = wave * n_chunks * chunk;
+        int n = 0;
+        __syncthreads();
+        for (int j = 0; j < n_chunks; ++j) {
+            u64 sum = 0;
+            each(std::integral_constant<int, 64>{}, mine + j * chunk, min(mine + (j + 1) * chunk, padded), lane, [&](float v, int i) {
+                const u64 w = kept_of(v, i);
+                sum += w;
+                n += w != 0;
+            });
+            sum = wave_scan(sum);
+            if (lane == 63) s.sum[wave * n_chunks + j] = sum;
+        }
+        __syncthreads();
+        return n;
+    };
+    bool summed = false;
+    int n_kept = 0;
     if (k || p_on) {
         auto clear = [&]() __attribute__((always_inline)) {
             __syncthreads();
             for (int i = tid; i < SAMPLE_BINS; i += NT) s.sum[i] = 0, s.count[i] = 0;
             __syncthreads();
         };
-        auto weigh_bins = [&]() __attribute__((always_inline)) {
+        auto weigh_bins = [&](bool count) __attribute__((always_inline)) {
             all_of([&](float v, int i) {
                 const float b = place(v);
                 if (!(b < SAMPLE_REACH) || (cut && composite(v, i) < cut)) return;
-                atomicAdd(&s.count[(int)b], 1);
+                if (count) atomicAdd(&s.count[(int)b], 1);
                 atomicAdd(&s.sum[(int)b], weight(v));
             });
             __syncthreads();
@@ -335,6 +358,59 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab) {
             w = o ? ~o & ((1ull << 41) - 1) : 0;
             const u64 upto = block_scan(s, w, &all), t = place_in(all);
             if (upto - w <= t && t < upto) out((int)(~o >> 41), kept, (float)((double)w / (double)all));
+        };
+        // the last composite of the list, one token a thread, that is kept with `before` tokens and before_sum before it; what weighs up to it
+        auto cut_list = [&](int n, int before, u64 before_sum, bool count_mode, u64 limit, u64* sum_upto) __attribute__((always_inline)) -> u64 {
+            u64 e = tid < n ? s.list[tid] : 0, all;
+            __syncthreads();
+            e = block_sort(s, e, n);
+            const u64 w = tid < n ? weight(logit_of(e)) : 0, upto = block_scan(s, w, &all) + before_sum;
+            const bool keep = tid < n && (count_mode ? (u64)(before + tid) < limit : tid == 0 || upto - w < limit);
+            s.list[tid] = e;
+            const int kept = __syncthreads_count(keep);
+            if (tid == kept - 1) s.lowest = e, s.found_sum = upto;
+            __syncthreads();
+            *sum_upto = s.found_sum;
+            return s.lowest;
+        };
+        // f(composite) of the tokens of bin b that are not cut off already
+        auto of_bin = [&](float b, auto&& f) __attribute__((always_inline)) {
+            all_of([&](float v, int i) {
+                const float at = place(v);
+                if (at >= b && at < b + 1.f && (!cut || composite(v, i) >= cut)) f(composite(v, i));
+            });
+        };
+        // the same for n tokens of bin b, from the list where they fit it: digit by digit of the composite.  The bins are used for it.
+        auto cut_digits = [&](float b, int n, int before, u64 before_sum, bool count_mode, u64 limit, u64* sum_upto) __attribute__((always_inline)) -> u64 {
+            auto members = [&](auto&& f) __attribute__((always_inline)) {
+                if (n <= LIST) {
+                    for (int i = tid; i < n; i += NT) f(s.list[i]);
+                } else {
+                    of_bin(b, f);
+                }
+                __syncthreads();
+            };
+            if (tid == 0) s.lowest = ~0ull;
+            u64 prefix = 0;
+            int shift = 54;
+            for (int d = 0; d < 5; ++d) {
+                const int bits = d == 2 ? 10 : 11, above = shift;
+                shift -= bits;
+                clear();
+                members([&](u64 e) {
+                    if (d > 0 && e >> above != prefix >> above) return;
+                    const int bin = (SAMPLE_BINS - 1) - (int)(e >> shift & ((1 << bits) - 1));
+                    atomicAdd(&s.count[bin], 1);
+                    atomicAdd(&s.sum[bin], weight(logit_of(e)));
+                });
+                find_bin<NT, true>(s, count_mode, limit, before, before_sum);
+                prefix |= (u64)(SAMPLE_BINS - 1 - s.found) << shift;
+                before = s.found_before, before_sum = s.found_before_sum;
+                *sum_upto = before_sum + s.found_sum;
+                if (s.found_count == 1 || (count_mode && (u64)(before + s.found_count) == limit)) break;       // all of the bin
+            }
+            members([&](u64 e) { if (e >> shift == prefix >> shift) atomicMin(&s.lowest, e); });       // (tokens of other bins may lie above the prefix)
+            return s.lowest;
         };
         u64 total = 0;
         bool by_count = k > 0;
@@ -368,85 +444,97 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab) {
             if (!by_count && p_on) clear();
         }
         if (!by_count && p_on) {
-            weigh_bins();
+            weigh_bins(false);
             u64 mine = 0;
             for (int i = tid; i < SAMPLE_BINS; i += NT) mine += s.sum[i];
             block_scan(s, mine, &total);
             find_bin<NT, true>(s, false, limit_of(total), 0, 0);
-        }
-        if (by_count || p_on) {
+            const int found = s.found;
+            // each token of the bins up to this one weighs e^-((found + 1) / 64) at least, which says that few can be kept; else what lies before the bin is
+            // summed up and its own tokens are listed in one pass
+            const double upto = (double)(s.found_before_sum + s.found_sum) / (double)SAMPLE_ONE;
+            if (upto * (double)__expf((float)(found + 1) * (1.f / 64.f)) < 0.98 * NT) {
+                list_upto(found);
+                const int n = s.n_list;
+                if (n <= NT) {
+                    draw_listed(n, false, total);
+                    return;
+                }
+            } else {
+                const float b = (float)found;
+                const u64 before_sum = s.found_before_sum;
+                n_kept = sum_chunks([&](float v, int i) __attribute__((always_inline)) -> u64 {
+                    const float at = place(v);
+                    if (!(at < b + 1.f)) return 0;
+                    if (at >= b) {
+                        const int to = atomicAdd(&s.n_list, 1);
+                        if (to < LIST) s.list[to] = composite(v, i);
+                        return 0;
+                    }
+                    const u64 w = weight(v);
+                    return w >= least ? w : 0;
+                });
+                const int n = s.n_list;
+                if (n <= LIST) {
+                    u64 unused;
+                    if (n <= NT) cut = cut_list(n, 0, before_sum, false, limit_of(total), &unused);
+                    else {                                 // (the chunks' sums lie where the digits are counted)
+                        u64 sums[SAMPLE_BINS / NT];
+#pragma unroll
+                        for (int j = 0; j < SAMPLE_BINS / NT; ++j) sums[j] = s.sum[j * NT + tid];
+                        cut = cut_digits(b, n, 0, before_sum, false, limit_of(total), &unused);
+#pragma unroll
+                        for (int j = 0; j < SAMPLE_BINS / NT; ++j) s.sum[j * NT + tid] = sums[j];
+                        __syncthreads();
+                    }
+                    for (int i = tid; i < n; i += NT) {
+                        const u64 e = s.list[i], w = e >= cut ? weight(logit_of(e)) : 0;
+                        if (w >= least) {
+                            ++n_kept;
+                            atomicAdd(&s.sum[index_of(e) / chunk], w);
+                        }
+                    }
+                    __syncthreads();
+                    summed = true;
+                }
+            }
+            if (!summed) {                                 // (again with counts, and the list empty)
+                __syncthreads();
+                if (tid == 0) s.n_list = 0;
+                clear();
+                weigh_bins(true);
+                find_bin<NT, true>(s, false, limit_of(total), 0, 0);
+            }
+        } else if (by_count) {
             const int few = s.found_before + s.found_count;
             if (few <= NT) {
                 list_upto(s.found);
-                draw_listed(few, by_count, total);
+                draw_listed(few, true, total);
                 return;
             }
-            // the last composite that is kept, the cut lying in the bin that was found: digit by digit, among the tokens of the bin, from the list if they fit
+        }
+        if (!summed && (by_count || p_on)) {
+            // the last composite that is kept, the cut lying in the bin that was found
             auto find_cut = [&](bool count_mode, u64 limit, u64* sum_upto) __attribute__((always_inline)) -> u64 {
                 const float b = (float)s.found;
-                const int n = s.found_count;
-                int before = s.found_before;
-                u64 before_sum = s.found_before_sum;
-                const bool listed = n <= LIST;
+                const int n = s.found_count, before = s.found_before;
+                const u64 before_sum = s.found_before_sum;
                 __syncthreads();
-                if (tid == 0) s.n_list = 0, s.lowest = ~0ull;
+                if (tid == 0) s.n_list = 0;
                 __syncthreads();
-                auto of_bin = [&](auto&& f) __attribute__((always_inline)) {
-                    all_of([&](float v, int i) {
-                        const float at = place(v);
-                        if (at >= b && at < b + 1.f && (!cut || composite(v, i) >= cut)) f(composite(v, i));
-                    });
-                };
-                if (listed) of_bin([&](u64 e) { s.list[atomicAdd(&s.n_list, 1)] = e; });
-                auto members = [&](auto&& f) __attribute__((always_inline)) {
-                    if (listed) {
-                        for (int i = tid; i < n; i += NT) f(s.list[i]);
-                    } else {
-                        of_bin(f);
-                    }
-                    __syncthreads();
-                };
-                if (n <= NT) {
-                    __syncthreads();
-                    u64 e = tid < n ? s.list[tid] : 0, all;
-                    e = block_sort(s, e, n);
-                    const u64 w = tid < n ? weight(logit_of(e)) : 0, upto = block_scan(s, w, &all) + before_sum;
-                    const bool keep = tid < n && (count_mode ? (u64)(before + tid) < limit : tid == 0 || upto - w < limit);
-                    const int kept = __syncthreads_count(keep);
-                    if (tid == kept - 1) s.lowest = e, s.found_sum = upto;
-                    __syncthreads();
-                    *sum_upto = s.found_sum;
-                    return s.lowest;
-                }
-                u64 prefix = 0;
-                int shift = 54;
-                for (int d = 0; d < 5; ++d) {
-                    const int bits = d == 2 ? 10 : 11, above = shift;
-                    shift -= bits;
-                    clear();
-                    members([&](u64 e) {
-                        if (d > 0 && e >> above != prefix >> above) return;
-                        const int bin = (SAMPLE_BINS - 1) - (int)(e >> shift & ((1 << bits) - 1));
-                        atomicAdd(&s.count[bin], 1);
-                        atomicAdd(&s.sum[bin], weight(logit_of(e)));
-                    });
-                    find_bin<NT, true>(s, count_mode, limit, before, before_sum);
-                    prefix |= (u64)(SAMPLE_BINS - 1 - s.found) << shift;
-                    before = s.found_before, before_sum = s.found_before_sum;
-                    *sum_upto = before_sum + s.found_sum;
-                    if (s.found_count == 1 || (count_mode && (u64)(before + s.found_count) == limit)) break;       // all of the bin
-                }
-                members([&](u64 e) { if (e >> shift == prefix >> shift) atomicMin(&s.lowest, e); });       // (tokens of other bins may lie above the prefix)
-                return s.lowest;
+                if (n <= LIST) of_bin(b, [&](u64 e) { s.list[atomicAdd(&s.n_list, 1)] = e; });
+                __syncthreads();
+                if (n <= NT) return cut_list(n, before, before_sum, count_mode, limit, sum_upto);
+                return cut_digits(b, n, before, before_sum, count_mode, limit, sum_upto);
             };
             if (by_count) {
                 clear();
-                weigh_bins();
+                weigh_bins(true);
                 find_bin<NT, true>(s, true, (u64)k, 0, 0);
                 cut = find_cut(true, (u64)k, &total);
                 if (p_on) {                                // the cut by weight lies before the one by count
                     clear();
-                    weigh_bins();
+                    weigh_bins(true);
                     find_bin<NT, true>(s, false, limit_of(total), 0, 0);
                 }
             }
@@ -471,28 +559,10 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab) {
         const u64 w = weight(v);
         return w >= least ? w : 0;
     };
-    // chunks of a wave's share, so that a thread has few tokens to go through where the place is
-    constexpr int UNIT = HELD ? 256 : 512, CHUNKS = HELD ? 1 : SAMPLE_BINS / NW;
-    const int per_wave = (vocab + NW - 1) / NW, chunk = ((per_wave + CHUNKS - 1) / CHUNKS + UNIT - 1) / UNIT * UNIT, n_chunks = (per_wave + chunk - 1) / chunk;
-    const int mine = wave * n_chunks * chunk;
-    int n = 0;
-    __syncthreads();
-    for (int j = 0; j < n_chunks; ++j) {
-        u64 sum = 0;
-        each(std::integral_constant<int, 64>{}, mine + j * chunk, min(mine + (j + 1) * chunk, padded), lane, [&](float v, int i) {
-            const u64 w = kept_weight(v, i);
-            sum += w;
-            n += w != 0;
-        });
-        if (__builtin_amdgcn_ballot_w64(sum != 0)) {
-#pragma unroll
-            for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
-        }
-        if (lane == 0) s.sum[wave * n_chunks + j] = sum;
-    }
+    if (!summed) n_kept = sum_chunks(kept_weight);
     int kept;
     u64 all;
-    block_scan(s, n, &kept);
+    block_scan(s, n_kept, &kept);
     __syncthreads();
     // the chunk that holds the place
     constexpr int PER = SAMPLE_BINS / NT;
