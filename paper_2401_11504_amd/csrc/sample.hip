@@ -162,13 +162,131 @@ __device__ __forceinline__ u64 block_sort(S& s, u64 v, int n) {
     return v;
 }
 
+// What a row's pieces have found out before its one workgroup draws from it (few rows of many tokens, see launch_sample)
+constexpr int SAMPLE_PIECE = 8192, SAMPLE_CHUNK = 512;
+struct SampleFound {
+    u64* best;                            // [rows][pieces] a piece's largest as composite (0: none)
+    u64* sum;                             // [rows][SAMPLE_BINS] the bins' weights, or, without top_k and top_p, what is kept of each SAMPLE_CHUNK tokens
+    int* count;                           // [rows][SAMPLE_BINS + 1] the bins' tokens (with top_k; their weights without); how many tokens are kept
+    int pieces;
+};
+// how the tokens of a row are weighed
+struct SampleRow {
+    float top, to_bins;
+    double top64, per;                    // per: log2(e) / temperature
+    __device__ __forceinline__ SampleRow(float top, float temperature)
+        : top(top), to_bins(fminf(64.f / temperature, 3e38f)), top64((double)top), per(1.0 / (double)temperature * 1.44269504088896340736) {}
+    __device__ __forceinline__ u64 weight(float v) const { return weight_of(((double)v - top64) * per); }
+    __device__ __forceinline__ float place(float v) const { return (top - v) * to_bins; }      // monotone, as each step of it is; its whole part is the bin
+};
+__device__ __forceinline__ u64 least_weight(float min_p) {
+    return !(min_p > 0.f) ? 1ull : min_p >= 1.f ? SAMPLE_ONE : (u64)ceil((double)min_p * (double)SAMPLE_ONE);
+}
+__device__ __forceinline__ int wanted(float top_k, int vocab) { return top_k >= 1.f && top_k < (float)vocab ? (int)top_k : 0; }
+// the larger of all lanes' composites, in every lane
+__device__ __forceinline__ u64 wave_best(u64 v) {
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) {
+        const u64 o = __shfl_xor(v, off, 64);
+        v = v > o ? v : o;
+    }
+    return v;
+}
+__device__ __forceinline__ u64 row_best(const SampleFound& w, long r, int lane) {
+    u64 best = 0;
+    for (int i = lane; i < w.pieces; i += 64) best = best > w.best[r * w.pieces + i] ? best : w.best[r * w.pieces + i];
+    return wave_best(best);
+}
+// eight tokens of a piece a thread, one chunk a wave: 64 lanes x 4, twice
+template <class F>
+__device__ __forceinline__ void each_of_piece(const float* x, int vocab, F&& f) {
+    const int i0 = (int)blockIdx.x * SAMPLE_PIECE + (threadIdx.x >> 6) * SAMPLE_CHUNK + (threadIdx.x & 63) * 4;
+    float4 v[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int i = i0 + k * 256;
+        if (i + 4 <= vocab) v[k] = *(const float4*)(x + i);
+        else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) (&v[k].x)[e] = i + e < vocab ? x[i + e] : -INFINITY;
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f((&v[k].x)[e], i0 + k * 256 + e);
+}
+__global__ __launch_bounds__(1024) void sample_best_kernel(Sample c, int vocab, SampleFound w) {
+    __shared__ u64 part[16];
+    const long r = blockIdx.y;
+    u64 best = 0;
+    each_of_piece(c.logits + r * c.ldl, vocab, [&](float v, int i) {
+        const u64 e = v > -INFINITY ? composite(v, i) : 0;
+        best = best > e ? best : e;
+    });
+    best = wave_best(best);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = best;
+    for (int i = blockIdx.x * 1024 + threadIdx.x; i < SAMPLE_BINS; i += gridDim.x * 1024) w.sum[r * SAMPLE_BINS + i] = 0, w.count[r * (SAMPLE_BINS + 1) + i] = 0;
+    if (blockIdx.x == 0 && threadIdx.x == 0) w.count[r * (SAMPLE_BINS + 1) + SAMPLE_BINS] = 0;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < 16; ++i) best = best > part[i] ? best : part[i];
+        w.best[r * w.pieces + blockIdx.x] = best;
+    }
+}
+__global__ __launch_bounds__(1024) void sample_weigh_kernel(Sample c, int vocab, SampleFound w) {
+    __shared__ u64 sum[SAMPLE_BINS];
+    __shared__ int count[SAMPLE_BINS];
+    const long r = blockIdx.y;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const float* params = c.params ? c.params + r * c.ldp : c.now;
+    const float temperature = params[0], top_k = params[1], top_p = params[2], min_p = params[3];
+    float top = logit_of(row_best(w, r, lane));
+    if (!(temperature > 0.f) || !(top > -INFINITY)) return;
+    const bool infinite = top == INFINITY;
+    const SampleRow row(infinite ? 0.f : top, temperature);
+    auto each = [&](auto&& f) { each_of_piece(c.logits + r * c.ldl, vocab, [&](float v, int) { f(!infinite ? v : v == INFINITY ? 0.f : -INFINITY); }); };
+    const bool by_count = wanted(top_k, vocab) > 0;        // (the weights are not looked at then, or weighed again)
+    if (by_count || top_p < 1.f) {
+        for (int i = tid; i < SAMPLE_BINS; i += 1024) sum[i] = 0, count[i] = 0;
+        __syncthreads();
+        each([&](float v) {
+            const float b = row.place(v);
+            if (!(b < SAMPLE_REACH)) return;
+            if (by_count) atomicAdd(&count[(int)b], 1);
+            else atomicAdd(&sum[(int)b], row.weight(v));
+        });
+        __syncthreads();
+        for (int i = tid; i < SAMPLE_BINS; i += 1024) {
+            if (count[i]) atomicAdd(w.count + r * (SAMPLE_BINS + 1) + i, count[i]);
+            if (sum[i]) atomicAdd(w.sum + r * SAMPLE_BINS + i, sum[i]);
+        }
+    } else {
+        const u64 least = least_weight(min_p);
+        u64 all = 0;
+        int n = 0;
+        each([&](float v) {
+            const u64 x = row.weight(v);
+            if (x >= least) all += x, ++n;
+        });
+        all = wave_scan(all);
+        n = wave_scan(n);
+        if (lane == 63) {
+            const int at = (int)blockIdx.x * (SAMPLE_PIECE / SAMPLE_CHUNK) + (tid >> 6);
+            if (at < SAMPLE_BINS) w.sum[r * SAMPLE_BINS + at] = all;
+            if (n) atomicAdd(w.count + r * (SAMPLE_BINS + 1) + SAMPLE_BINS, n);
+        }
+    }
+}
+
 // One workgroup a row.  HELD: the row stays in LDS from its one reading on; else every pass over it reads it again.
 //   pass 1  the largest logit
 //   pass 2  with top_k or top_p: how many tokens (top_k), or how much weight (top_p), lies in each of 2048 ranges of (largest - x) / temperature, 64 to a unit
 //   pass 3  what lies in the ranges up to the one with the cut is listed; up to a token a thread, the list is sorted, cut and drawn from
 //   else    the cut is found digit by digit among the tokens of its range (from a list if they fit one), and a last pass draws
-template <int NT, int LIST, bool HELD>
-__global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab) {
+// FOUND: passes 1 and 2, and without top_k and top_p the last one's sums, have been made by the row's pieces.
+template <int NT, int LIST, bool HELD, bool FOUND>
+__global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, SampleFound found_in) {
     constexpr int NW = NT / 64;
     __shared__ SampleLds<NT, LIST> s;
     extern __shared__ __align__(16) float held[];
@@ -231,7 +349,10 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab) {
     const bool greedy = !(temperature > 0.f);
     float m = -INFINITY;
     int lowest = 0;
-    if (HELD) {
+    if (FOUND) {
+        const u64 best = row_best(found_in, r, lane);      // (the same in every wave)
+        if (best) m = logit_of(best), lowest = index_of(best);
+    } else if (HELD) {
         for (int i0 = 0; i0 < padded; i0 += 16 * NT) {
             float4 v[4];
 #pragma unroll
@@ -266,7 +387,7 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab) {
         return;
     }
     if (greedy) {                                          // the lowest index of the largest
-        if (HELD) all_of([&](float v, int i) { if (v == top) atomicMax(&s.lowest, composite(0.f, i)); });
+        if (HELD && !FOUND) all_of([&](float v, int i) { if (v == top) atomicMax(&s.lowest, composite(0.f, i)); });
         else if (own_top == top) atomicMax(&s.lowest, composite(0.f, lowest));
         __syncthreads();
         if (tid == 0) out(index_of(s.lowest), 1, 1.f);
@@ -280,15 +401,12 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab) {
             __syncthreads();
         }
     }
-    const double per = 1.0 / (double)temperature * 1.44269504088896340736, top64 = (double)top;
-    const float to_bins = fminf(64.f / temperature, 3e38f);
-    auto weight = [&](float v) __attribute__((always_inline)) -> u64 { return weight_of(((double)v - top64) * per); };
-    auto place = [&](float v) -> float { return (top - v) * to_bins; };      // monotone, as each step of it is; its whole part is the bin
-
-    const int k = top_k >= 1.f && top_k < (float)vocab ? (int)top_k : 0;
+    const SampleRow row(top, temperature);
+    auto weight = [&](float v) __attribute__((always_inline)) -> u64 { return row.weight(v); };
+    auto place = [&](float v) -> float { return row.place(v); };
+    const int k = wanted(top_k, vocab);
     const bool p_on = top_p < 1.f;
-    u64 least = 1;
-    if (min_p > 0.f) least = min_p >= 1.f ? SAMPLE_ONE : (u64)ceil((double)min_p * (double)SAMPLE_ONE);
+    const u64 least = least_weight(min_p);
     auto limit_of = [&](u64 sum) -> u64 { return top_p > 0.f ? (u64)ceil((double)top_p * (double)sum) : 1ull; };
     auto place_in = [&](u64 all) -> u64 {
         const u64 t = (u64)floor((double)fminf(fmaxf(u, 0.f), 1.f) * (double)all);
@@ -412,11 +530,15 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab) {
             members([&](u64 e) { if (e >> shift == prefix >> shift) atomicMin(&s.lowest, e); });       // (tokens of other bins may lie above the prefix)
             return s.lowest;
         };
+        if (FOUND) {
+            for (int i = tid; i < SAMPLE_BINS; i += NT) s.sum[i] = found_in.sum[r * SAMPLE_BINS + i], s.count[i] = found_in.count[r * (SAMPLE_BINS + 1) + i];
+            __syncthreads();
+        }
         u64 total = 0;
         bool by_count = k > 0;
         // The top_k-th largest of the threads' own largest is no larger than the top_k-th of all: with few wanted, what lies from its bin on is listed without
         // counting all tokens, and most often fits the list.
-        if (by_count && k <= NT / 4) {
+        if (!FOUND && by_count && k <= NT / 4) {
             const float b = place(infinite ? (own_top == INFINITY ? 0.f : -INFINITY) : own_top);
             if (b < SAMPLE_REACH) atomicAdd(&s.count[(int)b], 1);
             __syncthreads();
@@ -434,17 +556,19 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab) {
             if (tid == 0) s.n_list = 0;
         }
         if (by_count) {
-            all_of([&](float v, int) {
-                const float b = place(v);
-                if (b < SAMPLE_REACH) atomicAdd(&s.count[(int)b], 1);
-            });
-            __syncthreads();
+            if (!FOUND) {
+                all_of([&](float v, int) {
+                    const float b = place(v);
+                    if (b < SAMPLE_REACH) atomicAdd(&s.count[(int)b], 1);
+                });
+                __syncthreads();
+            }
             find_bin<NT, false>(s, true, (u64)k, 0, 0);
             by_count = s.found >= 0;
             if (!by_count && p_on) clear();
         }
         if (!by_count && p_on) {
-            weigh_bins(false);
+            if (!FOUND || k) weigh_bins(false);
             u64 mine = 0;
             for (int i = tid; i < SAMPLE_BINS; i += NT) mine += s.sum[i];
             block_scan(s, mine, &total);
@@ -559,7 +683,13 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab) {
         const u64 w = weight(v);
         return w >= least ? w : 0;
     };
-    if (!summed) n_kept = sum_chunks(kept_weight);
+    if (FOUND && !k && !p_on) {
+        for (int i = tid; i < SAMPLE_BINS; i += NT) s.sum[i] = found_in.sum[r * SAMPLE_BINS + i];
+        if (tid == 0) n_kept = found_in.count[r * (SAMPLE_BINS + 1) + SAMPLE_BINS];
+        __syncthreads();
+    } else if (!summed) {
+        n_kept = sum_chunks(kept_weight);
+    }
     int kept;
     u64 all;
     block_scan(s, n_kept, &kept);
@@ -603,14 +733,31 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab) {
 constexpr int SAMPLE_HELD = 32512;         // logits that fit LDS beside the bins
 hipError_t launch_sample(const Sample& c, int rows, int vocab, float* ws, size_t ws_elems, hipStream_t s) {
     if (rows <= 0) return hipSuccess;
-    (void)ws, (void)ws_elems;
+    SampleFound w{};
     if (vocab <= SAMPLE_HELD && rows <= 256) {
         const int lds = ((vocab + 3) & ~3) * 4;
-        const hipError_t e = hipFuncSetAttribute((const void*)sample_kernel<1024, 1024, true>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        const hipError_t e = hipFuncSetAttribute((const void*)sample_kernel<1024, 1024, true, false>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
         if (e != hipSuccess) return e;
-        sample_kernel<1024, 1024, true><<<rows, 1024, lds, s>>>(c, vocab);
-    } else {
-        sample_kernel<512, 2048, false><<<rows, 512, 0, s>>>(c, vocab);
+        sample_kernel<1024, 1024, true, false><<<rows, 1024, lds, s>>>(c, vocab, w);
+        return hipGetLastError();
     }
+    // Few rows of many tokens: pieces of a row on CUs of their own, then a workgroup a row.  us for one row of 40000 / 65000 / 128000 in pieces and in one
+    // workgroup: top-k 50 21 and 14 / 23 and 16 / 26 and 22, top-p 0.9 30 and 33 / 35 and 46 / 46 and 79, min-p 16 and 12 / 16 and 16 / 16 and 24, no limit 16 and
+    // 24 / 16 and 35 / 17 and 63 (two launches more are 6 us of it); 16 rows of 128000 31 and 22, 88 and 116, 18 and 25, 19 and 64.
+    const size_t at = (uintptr_t)ws & 7 ? 1 : 0;           // (64-bit places in scratch that begins at any multiple of 4)
+    w.pieces = cdiv(vocab, SAMPLE_PIECE);
+    const size_t need = at + (size_t)rows * (2 * w.pieces + 3 * SAMPLE_BINS + 1);
+    if (ws && vocab > 65536 && rows <= 16 && vocab <= SAMPLE_BINS * SAMPLE_CHUNK && need <= ws_elems) {
+        w.best = (u64*)(ws + at);
+        w.sum = w.best + (size_t)rows * w.pieces;
+        w.count = (int*)(w.sum + (size_t)rows * SAMPLE_BINS);
+        const dim3 grid(w.pieces, rows);
+        sample_best_kernel<<<grid, 1024, 0, s>>>(c, vocab, w);
+        sample_weigh_kernel<<<grid, 1024, 0, s>>>(c, vocab, w);
+        sample_kernel<1024, 2048, false, true><<<rows, 1024, 0, s>>>(c, vocab, w);
+        return hipGetLastError();
+    }
+    if (rows <= 256) sample_kernel<1024, 2048, false, false><<<rows, 1024, 0, s>>>(c, vocab, w);
+    else sample_kernel<512, 2048, false, false><<<rows, 512, 0, s>>>(c, vocab, w);
     return hipGetLastError();
 }

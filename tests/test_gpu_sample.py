@@ -51,6 +51,17 @@ def test_settings(api, V):
     check(api, x, SETTINGS, u)
 
 
+@pytest.mark.parametrize("V", [32512, 32513, 65536, 65537, 100003])
+def test_few_rows_of_many_tokens(api, V):
+    """rows that one CU does not hold: pieces of them on others"""
+    x, u, _ = make(V, len(SETTINGS), V)
+    for a in range(0, len(SETTINGS), 8):
+        check(api, x[a:a + 8], SETTINGS[a:a + 8], u[a:a + 8])
+    one = draw(api, x[:8], SETTINGS[:8], u[:8], torch.empty(1 << 18, device="cuda"))
+    odd = draw(api, x[:8], SETTINGS[:8], u[:8], torch.empty((1 << 18) + 1, device="cuda")[1:])       # scratch at 4 bytes
+    assert all(torch.equal(a, b) for a, b in zip(one, odd))
+
+
 @pytest.mark.parametrize("rows,V", [(3, 128001), (40, 3001), (300, 40)])
 def test_many_rows(api, rows, V):
     x, u, g = make(rows, rows, V)
@@ -59,7 +70,7 @@ def test_many_rows(api, rows, V):
 
 
 @pytest.mark.parametrize("params", [[1.0, 700, 1.0, 0.0], [1.0, 0, 0.5, 0.0], [1.0, 0, 0.3333, 0.0], [1.0, 1500, 0.5, 0.0], [0.5, 1500, 0.75, 0.5], [1.0, 9000, 0.7, 0.0], [1.0, 0, 1.0, 0.5]])
-@pytest.mark.parametrize("V", [2000, 20000])
+@pytest.mark.parametrize("V", [2000, 20000, 70000])
 def test_equal_logits(api, params, V):
     """cuts among equal logits go by the index; sums that fall on the limits exactly"""
     x = torch.zeros(4, V)
@@ -82,8 +93,8 @@ def test_ends_of_the_number(api):
         assert torch.equal(draw(api, x, p, torch.full((6,), math.nan))[0], low)
 
 
-def test_no_infinite_and_undefined_logits(api):
-    V = 5000
+@pytest.mark.parametrize("V", [5000, 70000])
+def test_no_infinite_and_undefined_logits(api, V):
     x, u, g = make(2, 9, V)
     x[0] = math.nan
     x[1] = -math.inf
@@ -91,7 +102,7 @@ def test_no_infinite_and_undefined_logits(api):
     x[3, ::2] = -math.inf
     x[4, [7, 4000]] = math.inf                                # those alone
     x[5] = -math.inf
-    x[5, 4999] = -3.0                                         # one token
+    x[5, V - 1] = -3.0                                        # one token
     x[6] = math.nan
     x[6, 0] = -1e30
     x[7] = 1e38 * torch.sign(x[7])
