@@ -554,7 +554,7 @@ tl_status tl_k_sample(const float* logits, int32_t ldl, int32_t rows, int32_t vo
  *   table : int32 [n_seqs][n_table]; slot j of sequence s lies on page table[s][j / page_size] at place j % page_size.  An entry outside [0, n_pages)
  *           is no page: what would lie there is not written, and passed over when it is read.
  * A sequence's slots are in use from 0 up to its length, which is the caller's to keep (lengths: device int32 [n_seqs]; below 0 counts as 0, beyond the table as
- * all of it).  Keys hold their rotation, so that the order of the slots means nothing to attention.  n_seqs up to 65536, n_seqs * n_kv_heads up to 2^24, n_table * page_size and n_pages up to 2^30.
+ * all of it).  Keys hold their rotation, so that the order of the slots means nothing to attention.  n_seqs up to 65535, n_seqs * n_kv_heads up to 2^24, n_table * page_size and n_pages up to 2^30.
  * Where the table, lengths, first_row or positions change on the device between two calls, the next call sees it (captured graphs as well).
  */
 typedef struct {

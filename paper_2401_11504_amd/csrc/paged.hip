@@ -86,11 +86,13 @@ __global__ __launch_bounds__(PAGED_NW * 64, 2) void attn_paged_kernel(Paged c, c
     typedef typename Words<NV>::type vword_t;
     __shared__ __align__(16) float part[NW][16 * LDP];     // a column's output, maximum and sum, wave by wave
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m16 = lane & 15, g = lane >> 4;
-    const int tiles = (group + 15) >> 4, heads = c.heads * group;
-    int idx = blockIdx.x;
-    const int ht = idx % (c.heads * tiles), head = ht / tiles, c0 = ht % tiles * 16, n_cols = min(16, group - c0);
-    idx /= c.heads * tiles;
-    const int split = idx % n_ranges, seq = idx / n_ranges;
+    const int heads = c.heads * group, split = blockIdx.y, seq = blockIdx.z;
+    int head = blockIdx.x, c0 = 0;
+    if (group > 16) {                                      // (uniform) several tiles of columns to a key head
+        const int tiles = (group + 15) >> 4;
+        head = blockIdx.x / tiles, c0 = blockIdx.x % tiles * 16;
+    }
+    const int n_cols = min(16, group - c0);
     const int len = min(max(lengths[seq], 0), max_len), k0 = split * range, kend = min(k0 + range, len);
     if (k0 >= len && split > 0) return;
     const long qh0 = (long)seq * heads + head * group + c0;
@@ -331,12 +333,13 @@ PagedPlan attention_paged_plan(int max_len, int n_seqs, int heads, int kv_heads,
     const size_t scores = weights ? (size_t)rows * (size_t)(((long)max_len + 31) & ~31L) : 0;
     const int most = (int)((max_len + unit - 1L) / unit);
     PagedPlan p;
-    // Ranges of 512 keys where sequences differ in length, and no fewer workgroups than CUs; a range alone needs no second launch.  us, by ranges:
-    // 131072 keys of 8 key heads 16 / 24 / 32 / 48 / 64: 136 / 102 / 89 / 107 / 90; 3800 of 32 heads 4 / 8 / 16: 27 / 21 / 21; 64 texts of up to
-    // 4096, 8 key heads 1 / 2 / 4 / 6 / 8 / 16 / 32: 130 / 149 / 140 / 124 / 127 / 131 / 148; 33 of up to 2000 1 / 2 / 4 / 8: 74 / 64 / 57 / 52; 64 of up to 500
-    // 1 / 2 / 4: 23 / 28 / 30; one of 200 1 / 2: 14.5 / 17.3 (the launches bound the last two).
+    // Few key heads in all: as many workgroups as CUs; more: four times that, or, as sequences differ in length and the last round of workgroups is
+    // seldom full, ranges of 256 (short texts) or 640 keys.  A range alone needs no second launch.  us, by ranges:
+    // 131072 keys of 8 key heads 16 / 24 / 32 / 64: 136 / 102 / 89 / 90; 3800 of 32 heads 4 / 8 / 16: 27 / 21 / 21; 8 texts of up to 4000, 8 key heads 4 / 7 / 8 / 16:
+    // 27 / 29 / 26 / 25; 64 of up to 4096 1 / 2 / 4 / 7 / 8 / 16 / 32: 130 / 149 / 140 / 120 / 127 / 131 / 146; 16 of up to 16000 8 / 16 / 24 / 32 / 64: 139 / 118 /
+    // 113 / 118 / 123; 33 of up to 2000, with weights 1 / 2 / 4 / 8 / 16: 74 / 64 / 58 / 52 / 53; 64 of up to 500 1 / 2 / 4: 23 / 28 / 31.
     int n = 1;
-    if (max_len > 512) n = (int)std::max(256 / groups, n_seqs > 1 ? ((long)max_len + 511) / 512 : 1L);
+    if (max_len > 512) n = (int)(groups < 64 ? 256 / groups : std::max(1024 / groups, max_len <= 2048 ? ((long)max_len + 255) / 256 : ((long)max_len + 639) / 640));
     n = n > most ? most : n;
     n = n > PAGED_MAX_RANGES ? PAGED_MAX_RANGES : n;
     for (;; --n) {
@@ -363,7 +366,7 @@ hipError_t launch_attention_paged(const Paged& c, const int* lengths, int max_le
         w.ml = (float2*)(ws + p.ml_at);
         w.o = ws + p.o_at;
     }
-    const int grid = c.n_seqs * c.heads * tiles * p.n_ranges;
+    const dim3 grid(c.heads * tiles, p.n_ranges, c.n_seqs);
     auto attend = [&](auto kernel) { kernel<<<grid, PAGED_NW * 64, 0, s>>>(c, lengths, max_len, q, ldq, group, scale, o, ldo, w, p.range, p.n_ranges); };
     if (c.d == 128) w_out ? attend(attn_paged_kernel<128, true>) : attend(attn_paged_kernel<128, false>);
     else w_out ? attend(attn_paged_kernel<64, true>) : attend(attn_paged_kernel<64, false>);

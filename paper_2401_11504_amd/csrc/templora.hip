@@ -1964,7 +1964,7 @@ static tl_status paged_of(const tl_paged_mem* m, const char* name, Paged* out) {
     if (((uintptr_t)m->k | (uintptr_t)m->v) & 15) return fail(TL_ERR_ARG, "%s: pages start at multiples of 16 bytes", name);
     const int32_t page = m->page_size;
     if (m->n_kv_heads < 1 || m->n_kv_heads > 4096 || (m->d_head != 64 && m->d_head != 128) || page < 16 || page > 65536 || (page & (page - 1)) || m->n_pages < 1 ||
-        m->n_pages > kMost || m->n_seqs < 0 || m->n_seqs > 65536 || (int64_t)m->n_seqs * m->n_kv_heads > 1 << 24 || m->n_table < 1 || (int64_t)m->n_table * page > kMost)
+        m->n_pages > kMost || m->n_seqs < 0 || m->n_seqs > 65535 || (int64_t)m->n_seqs * m->n_kv_heads > 1 << 24 || m->n_table < 1 || (int64_t)m->n_table * page > kMost)
         return fail(TL_ERR_ARG, "%s: %d heads of %d, %d pages of %d, %d sequences of up to %d", name, m->n_kv_heads, m->d_head, m->n_pages, page, m->n_seqs, m->n_table);
     int shift = 4;
     while (1 << shift < page) ++shift;
@@ -1984,7 +1984,7 @@ extern "C" tl_status tl_k_paged_append(const tl_paged_mem* cache, const int32_t*
 }
 // sizes of an attention over pages
 static bool attention_paged_ok(int64_t max_len, int64_t n_seqs, int64_t n_heads, int64_t n_kv_heads) {
-    return max_len >= 1 && max_len <= kMost && n_seqs >= 0 && n_seqs <= 65536 && n_heads >= 1 && n_heads <= 65536 && n_heads % n_kv_heads == 0 &&
+    return max_len >= 1 && max_len <= kMost && n_seqs >= 0 && n_seqs <= 65535 && n_heads >= 1 && n_heads <= 65536 && n_heads % n_kv_heads == 0 &&
            n_seqs * n_heads <= 1 << 24;
 }
 extern "C" tl_status tl_k_attention_paged(const tl_paged_mem* cache, const int32_t* lengths, int32_t max_len, const uint16_t* q, int32_t ldq, int32_t n_heads,
