@@ -55,6 +55,8 @@ template <int CTRL, int ROWS = 0xf>
 __device__ __forceinline__ u64 dpp(u64 v) {
     return (u64)(unsigned)dpp<CTRL, ROWS>((int)(v >> 32)) << 32 | (unsigned)dpp<CTRL, ROWS>((int)(unsigned)v);
 }
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ float dpp(float v) { return __int_as_float(dpp<CTRL, ROWS>(__float_as_int(v))); }
 // inclusive sums over the lanes of a wave: along rows of 16, then the rows' ends into the rows behind
 template <class N>
 __device__ __forceinline__ N wave_scan(N v) {
@@ -85,6 +87,7 @@ struct SampleLds {
     u64 wave_sum[NT / 64];
     u64 found_sum, found_before_sum, lowest;
     int found, found_count, found_before, n_list;
+    float about;
 };
 // inclusive sums over the threads of the workgroup; the total to *all
 template <class S, class N>
@@ -92,13 +95,14 @@ __device__ __forceinline__ N block_scan(S& s, N v, N* all) {
     constexpr int NW = sizeof(s.wave_sum) / sizeof(u64);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     v = wave_scan(v);
+    N* ends = (N*)s.wave_sum;
     __syncthreads();
-    if (lane == 63) s.wave_sum[wave] = (u64)v;
+    if (lane == 63) ends[wave] = v;
     __syncthreads();
     N total = 0;
 #pragma unroll 4
     for (int w = 0; w < NW; ++w) {
-        const N o = (N)s.wave_sum[w];
+        const N o = ends[w];
         if (w < wave) v += o;
         total += o;
     }
@@ -129,6 +133,28 @@ __device__ __forceinline__ void find_bin(S& s, bool by_count, u64 limit, int bef
         cs += c[i], ws += w[i];
     }
     __syncthreads();
+}
+// The same where about so much weighs: in the place of the counts lie the tokens' weights as parts of the largest that the bin has room for, whole
+// numbers in units of 2^-bits.  (32-bit sums of whole numbers are several times faster here than of 64 bits, or of floating point.)  Returns what weighs up to
+// the bin's end, in units of the largest weight.
+template <int NT, class S>
+__device__ __forceinline__ float find_about(S& s, float p, int bits) {
+    constexpr int N = SAMPLE_BINS / NT;
+    const int b = N * threadIdx.x;
+    float w[N], ws = 0.f, all;
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i] = (float)(unsigned)s.count[b + i] * __builtin_amdgcn_exp2f((float)(b + i) * (-1.44269504088896340736f / 64.f) - (float)bits), ws += w[i];
+    if (threadIdx.x == 0) s.found = SAMPLE_BINS - 1, s.about = 0.f;       // (nowhere: roundings, and the caller finds out)
+    const float mine = ws;
+    ws = block_scan(s, ws, &all) - mine;
+    const float limit = p * all;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if (w[i] > 0.f && (ws < limit || b + i == 0) && limit <= ws + w[i]) atomicMin(&s.found, b + i), s.about = ws + w[i];
+        ws += w[i];
+    }
+    __syncthreads();
+    return s.about;
 }
 // one value a thread, the largest in thread 0; n of them are not 0
 template <class S>
@@ -463,12 +489,14 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, Samp
             __syncthreads();
         };
         // the list, one token a thread, holds all that can be kept: sorted, cut, sorted by index and drawn from
-        auto draw_listed = [&](int n, bool by_count, u64 total) __attribute__((always_inline)) {
+        auto draw_listed = [&](int n, bool by_count, u64 total) __attribute__((always_inline)) -> bool {
             u64 e = tid < n ? s.list[tid] : 0;
+            __syncthreads();
             e = block_sort(s, e, n);
             u64 w = tid < n && !(by_count && tid >= k) ? weight(logit_of(e)) : 0, all;
             const u64 before = block_scan(s, w, &all) - w;
             if (by_count) total = all;
+            else if (all < limit_of(total)) return false;        // (uniform) the cut lies behind what is listed
             const bool keep = w >= least && (!p_on || tid == 0 || before < limit_of(total));
             const int kept = __syncthreads_count(keep);
             u64 o = keep ? ~((u64)index_of(e) << 41 | w) : 0;    // (weights have 41 bits, indices 22)
@@ -476,6 +504,7 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, Samp
             w = o ? ~o & ((1ull << 41) - 1) : 0;
             const u64 upto = block_scan(s, w, &all), t = place_in(all);
             if (upto - w <= t && t < upto) out((int)(~o >> 41), kept, (float)((double)w / (double)all));
+            return true;
         };
         // the last composite of the list, one token a thread, that is kept with `before` tokens and before_sum before it; what weighs up to it
         auto cut_list = [&](int n, int before, u64 before_sum, bool count_mode, u64 limit, u64* sum_upto) __attribute__((always_inline)) -> u64 {
@@ -568,65 +597,108 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, Samp
             if (!by_count && p_on) clear();
         }
         if (!by_count && p_on) {
-            if (!FOUND || k) weigh_bins(false);
-            u64 mine = 0;
-            for (int i = tid; i < SAMPLE_BINS; i += NT) mine += s.sum[i];
-            block_scan(s, mine, &total);
-            find_bin<NT, true>(s, false, limit_of(total), 0, 0);
+            // Where the cut lies, by masses to a few parts in 2^bits (or, from the row's pieces, by weights): then one pass weighs all tokens, and each exactly once; it finds
+            // out whether that was right.
+            const bool known = FOUND && !k;
+            float upto;
+            if (known) {
+                u64 mine = 0;
+                for (int i = tid; i < SAMPLE_BINS; i += NT) mine += s.sum[i];
+                block_scan(s, mine, &total);
+                find_bin<NT, true>(s, false, limit_of(total), 0, 0);
+                upto = (float)((double)(s.found_before_sum + s.found_sum) / (double)SAMPLE_ONE);
+            } else {
+                const int bits = __clz(vocab) - 1;         // (as many units as tokens fit 31 bits)
+                const float unit = (float)(1 << bits);
+                all_of([&](float v, int) {
+                    const float b = place(v);
+                    if (!(b < SAMPLE_REACH)) return;
+                    const float in = __builtin_amdgcn_fractf(b) * (1.f / 64.f);      // e^-in, in < 1/64, by its first three terms
+                    atomicAdd(&s.count[(int)b], (int)(unit * fmaf(in, fmaf(in, 0.5f, -1.f), 1.f)));
+                });
+                __syncthreads();
+                upto = find_about<NT>(s, top_p, bits);
+            }
             const int found = s.found;
-            // each token of the bins up to this one weighs e^-((found + 1) / 64) at least, which says that few can be kept; else what lies before the bin is
-            // summed up and its own tokens are listed in one pass
-            const double upto = (double)(s.found_before_sum + s.found_sum) / (double)SAMPLE_ONE;
-            if (upto * (double)__expf((float)(found + 1) * (1.f / 64.f)) < 0.98 * NT) {
-                list_upto(found);
-                const int n = s.n_list;
-                if (n <= NT) {
-                    draw_listed(n, false, total);
-                    return;
+            u64 before_sum = known ? s.found_before_sum : 0, weighed = 0;
+            // each token of the bins up to this one weighs about e^-((found + 1) / 64) at least, which says that few can be kept; else what lies before the bin
+            // is summed up and its own tokens are listed
+            if (upto * __expf((float)(found + 1) * (1.f / 64.f)) < 0.9f * NT) {
+                if (known) list_upto(found);
+                else {
+                    const float end = (float)(found + 1);
+                    all_of([&](float v, int i) {
+                        const float at = place(v);
+                        if (!(at < SAMPLE_REACH)) return;
+                        weighed += weight(v);
+                        if (at < end) {
+                            const int to = atomicAdd(&s.n_list, 1);
+                            if (to < LIST) s.list[to] = composite(v, i);
+                        }
+                    });
+                    block_scan(s, weighed, &total);
+                    __syncthreads();
                 }
+                const int n = s.n_list;
+                if (n <= NT && draw_listed(n, false, total)) return;
             } else {
                 const float b = (float)found;
-                const u64 before_sum = s.found_before_sum;
+                u64 ahead = 0;
                 n_kept = sum_chunks([&](float v, int i) __attribute__((always_inline)) -> u64 {
                     const float at = place(v);
-                    if (!(at < b + 1.f)) return 0;
-                    if (at >= b) {
+                    if (!(at < (known ? b + 1.f : SAMPLE_REACH))) return 0;
+                    if (at >= b && at < b + 1.f) {
                         const int to = atomicAdd(&s.n_list, 1);
                         if (to < LIST) s.list[to] = composite(v, i);
-                        return 0;
                     }
+                    if (known && at >= b) return 0;
                     const u64 w = weight(v);
+                    weighed += w;
+                    if (at >= b) return 0;
+                    ahead += w;
                     return w >= least ? w : 0;
                 });
                 const int n = s.n_list;
+                if (!known) {
+                    block_scan(s, weighed, &total);
+                    block_scan(s, ahead, &before_sum);
+                }
+                const u64 limit = limit_of(total);
                 if (n <= LIST) {
-                    u64 unused;
-                    if (n <= NT) cut = cut_list(n, 0, before_sum, false, limit_of(total), &unused);
-                    else {                                 // (the chunks' sums lie where the digits are counted)
-                        u64 sums[SAMPLE_BINS / NT];
+                    u64 of_bin_sum = 0, mine = 0, unused;
+                    for (int i = tid; i < n; i += NT) mine += weight(logit_of(s.list[i]));
+                    block_scan(s, mine, &of_bin_sum);
+                    if (before_sum < limit && limit <= before_sum + of_bin_sum) {
+                        if (n <= NT) cut = cut_list(n, 0, before_sum, false, limit, &unused);
+                        else {                             // (the chunks' sums lie where the digits are counted)
+                            u64 sums[SAMPLE_BINS / NT];
 #pragma unroll
-                        for (int j = 0; j < SAMPLE_BINS / NT; ++j) sums[j] = s.sum[j * NT + tid];
-                        cut = cut_digits(b, n, 0, before_sum, false, limit_of(total), &unused);
+                            for (int j = 0; j < SAMPLE_BINS / NT; ++j) sums[j] = s.sum[j * NT + tid];
+                            cut = cut_digits(b, n, 0, before_sum, false, limit, &unused);
 #pragma unroll
-                        for (int j = 0; j < SAMPLE_BINS / NT; ++j) s.sum[j * NT + tid] = sums[j];
-                        __syncthreads();
-                    }
-                    for (int i = tid; i < n; i += NT) {
-                        const u64 e = s.list[i], w = e >= cut ? weight(logit_of(e)) : 0;
-                        if (w >= least) {
-                            ++n_kept;
-                            atomicAdd(&s.sum[index_of(e) / chunk], w);
+                            for (int j = 0; j < SAMPLE_BINS / NT; ++j) s.sum[j * NT + tid] = sums[j];
+                            __syncthreads();
                         }
+                        for (int i = tid; i < n; i += NT) {
+                            const u64 e = s.list[i], w = e >= cut ? weight(logit_of(e)) : 0;
+                            if (w >= least) {
+                                ++n_kept;
+                                atomicAdd(&s.sum[index_of(e) / chunk], w);
+                            }
+                        }
+                        __syncthreads();
+                        summed = true;
                     }
-                    __syncthreads();
-                    summed = true;
                 }
             }
-            if (!summed) {                                 // (again with counts, and the list empty)
+            if (!summed) {                                 // by weights and with counts, the list empty
                 __syncthreads();
                 if (tid == 0) s.n_list = 0;
                 clear();
                 weigh_bins(true);
+                u64 mine = 0;
+                for (int i = tid; i < SAMPLE_BINS; i += NT) mine += s.sum[i];
+                block_scan(s, mine, &total);
                 find_bin<NT, true>(s, false, limit_of(total), 0, 0);
             }
         } else if (by_count) {

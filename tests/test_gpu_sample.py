@@ -81,6 +81,27 @@ def test_equal_logits(api, params, V):
     check(api, x, torch.tensor(params), torch.tensor([0.0, 0.5, 0.9999999, 0.25]))
 
 
+@pytest.mark.parametrize("V", [900, 9000, 40000, 70000])
+def test_limits_next_to_a_border_of_masses(api, V):
+    """levels of equal logits, and limits of weight a rounding or two beside the sums of levels: what a sum in 32 bits takes for one side lies on the other"""
+    levels = torch.tensor([0.0, -0.5, -2.0, -3.3])
+    x = levels[torch.randint(0, 4, (V,), generator=torch.Generator().manual_seed(V))]
+    w = torch.round(torch.exp(x.double()) * 2 ** 40)
+    total = float(w.sum())
+    ps = []
+    for level in levels[:3]:
+        at = torch.tensor(float(w[x >= level].sum()) / total, dtype=torch.float32)
+        for _ in range(3):
+            at = torch.nextafter(at, torch.tensor(0.0))
+        for _ in range(7):
+            ps.append(float(at))
+            at = torch.nextafter(at, torch.tensor(1.0))
+    params = torch.tensor([[1.0, 0, p, 0.0] for p in ps])
+    u = torch.linspace(0, 0.999, len(ps))
+    for a in range(0, len(ps), 11):
+        check(api, x[None].expand(len(ps[a:a + 11]), V).contiguous(), params[a:a + 11], u[a:a + 11])
+
+
 def test_ends_of_the_number(api):
     x, _, _ = make(1, 6, 3000)
     u = torch.tensor([0.0, 1 - 2.0 ** -24, 2.0 ** -24, 0.0, 0.5, 1 - 2.0 ** -24])
