@@ -592,7 +592,7 @@ tl_status tl_k_attention_weights(const uint16_t* q, int32_t ldq, const uint16_t*
                                  void* hip_stream);
 /* Cuts sequences longer than `budget` slots back to it, each key head by itself: kept are the first `budget` slots of the order
  *     recent tokens (position > the head's newest position - n_recent) before others, then larger weights (NaN counts as the least), then lower slots;
- *     slots on no page come after all others.
+ *     a slot on no page holds nothing and can take nothing: below the budget it comes first (it stays), behind it after all others.
  * Kept slots below the budget stay where they are; the i-th slot there that is not kept receives the i-th kept one from behind (key, value, weight, position).
  *   weights fp32, positions int32 [n_seqs][n_kv_heads][ldw] (slots from ldw on are not looked at: lengths count as ldw at most); weights_out, positions_out: as
  *   large, or the same; slots below min(length, budget) are written.  lengths_out (int32 [n_seqs], or lengths): min(length, budget).  Pages wholly behind it are free.

@@ -389,6 +389,8 @@ __device__ __forceinline__ unsigned order_key(float w) {
     const unsigned u = __float_as_uint(w + 0.f);           // (-0 counts as 0)
     return w != w ? 0u : u & 0x80000000u ? ~u : u | 0x80000000u;
 }
+// A slot on no page holds nothing and could take nothing: below the budget it stays, behind it goes before all others.
+__device__ __forceinline__ unsigned no_page_key(int slot, int budget) { return slot < budget ? 0xffffffffu : 0u; }
 // the bin, from the last down, in which the count first reaches `need`: *bin, and what of `need` is left for it (hist: BINS counts)
 template <int NT, int BINS>
 __device__ __forceinline__ void find_from_top(const int* hist, int* sums, int* found, int need, int* bin, int* left) {
@@ -475,7 +477,10 @@ __global__ __launch_bounds__(NT, 4) void evict_select_kernel(Paged c, const int*
 #pragma unroll
     for (int k = 0; k < K; ++k)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) key[k][e] = id[k] < 0 || id[k] >= c.n_pages ? 0u : (long)p[k][e] > border ? 0xffffffffu : order_key(w[k][e]);
+        for (int e = 0; e < 4; ++e) {
+            const bool there = id[k] >= 0 && id[k] < c.n_pages;
+            key[k][e] = !there ? no_page_key(4 * (k * NT + tid) + e, budget) : (long)p[k][e] > border ? 0xffffffffu : order_key(w[k][e]);
+        }
     __builtin_amdgcn_sched_barrier(0);
     unsigned prefix = 0;
     int need = budget;                                     // of the slots whose key begins with the prefix, so many stay
@@ -612,7 +617,7 @@ __global__ __launch_bounds__(EVICT_NT) void evict_select_long_kernel(Paged c, co
     for (int w = 0; w < NWV; ++w) newest = max(newest, sums[0][w]);
     const long border = (long)newest - n_recent;
     auto key_of = [&](int i) -> unsigned {
-        if (page_of(c, seq, i) < 0) return 0u;
+        if (page_of(c, seq, i) < 0) return no_page_key(i, budget);
         return (long)p_in[row + i] > border ? 0xffffffffu : order_key(w_in[row + i]);
     };
     unsigned prefix = 0;

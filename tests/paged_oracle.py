@@ -79,7 +79,7 @@ def evict(k_pool, v_pool, table, lengths, budget, recent, weights, positions):
 
             def rank(j):
                 if page_of(table, n_pages, s, j, page) < 0:
-                    return (2, 0.0, j)
+                    return (0 if j < budget else 2, 0.0, j)
                 if int(positions[s, h, j]) > newest - recent:
                     return (0, 0.0, j)
                 w = float(weights[s, h, j])
@@ -91,9 +91,9 @@ def evict(k_pool, v_pool, table, lengths, budget, recent, weights, positions):
             for a, b in zip(src, dst):
                 weights_out[s, h, b], positions_out[s, h, b] = weights[s, h, a], positions[s, h, a]
                 pa, pb = page_of(table, n_pages, s, a, page), page_of(table, n_pages, s, b, page)
-                if pa >= 0 and pb >= 0:
-                    for x in (k_pool, v_pool):
-                        x[pb, h, b % page] = x[pa, h, a % page]
+                assert pa >= 0 and pb >= 0                # nothing moves from or to where there is no page
+                for x in (k_pool, v_pool):
+                    x[pb, h, b % page] = x[pa, h, a % page]
     return torch.tensor(after, dtype=torch.int32), weights_out, positions_out
 
 

@@ -307,6 +307,11 @@ def test_evict_pages_that_are_not_there_and_short_rows(api):
     k, v, table, w, p = evict_case(g, [400, 390, 250], 2, 16, 64)
     table[0, 3], table[0, 20], table[1, 5:20], table[2, 10] = -1, 10 ** 6, -1, -1
     check_evict(api, k.clone(), v.clone(), table, ints([400, 390, 250]), 200, 50, w, p, False)
+    # hardly more slots on pages than stay, and fewer
+    table[0, 1:14] = -1
+    check_evict(api, k.clone(), v.clone(), table, ints([400, 390, 250]), 200, 50, w, p, False)
+    table[0, 14:20] = -1
+    check_evict(api, k.clone(), v.clone(), table, ints([400, 390, 250]), 200, 50, w, p, True)
     # weights for fewer slots than the table has room for: lengths count as that
     check_evict(api, k, v, table, ints([400, 390, 250]), 200, 50, w[:, :, :300].contiguous(), p[:, :, :300].contiguous(), True)
 
@@ -344,3 +349,15 @@ def test_evict_of_many_slots(api, n, budget):
                 at = table[0].long()
                 got = x.cpu()[at, h].reshape(-1, d)[:n]
                 assert torch.equal(got, y[at, h].reshape(-1, d)[slots])
+
+
+def test_evict_of_many_slots_with_pages_that_are_not_there(api):
+    g = gen(12)
+    kv, page, d, n, budget = 1, 16, 64, 33000, 20000
+    n_table = -(-n // page)
+    k, v = (bf16(g, n_table, kv, page, d) for _ in range(2))
+    table = torch.randperm(n_table, generator=g)[None].int()
+    table[0, torch.randperm(n_table, generator=g)[:300]] = -1
+    w, p = torch.rand(1, kv, n, generator=g), torch.randperm(n, generator=g)[None, None].int()
+    for m in (n, 30000):                                     # read again, and held in registers
+        check_evict(api, k.clone(), v.clone(), table, ints([m]), budget, 500, w[:, :, :m].contiguous(), p[:, :, :m].contiguous(), False)
