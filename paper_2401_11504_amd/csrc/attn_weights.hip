@@ -8,18 +8,17 @@
 #include "kernels.h"
 #include "tiles.h"
 
-// KW waves side by side own 64 keys each, their fragments in registers for all heads and queries; the 8 / KW groups of such waves take the tiles of
+// KW waves side by side own 64 keys each, their fragments in registers for all heads and queries; the WAVES / KW groups of such waves take the tiles of
 // queries (32, or 64 where waves share them and each tile costs a barrier) in turn, through LDS, up to two tiles ahead.  A workgroup has key block b and,
 // PAIRED, the one as far from the end, so that all have the same number of tiles.
-constexpr int AW_WAVES = 8;
 constexpr int aw_rows(int kw) { return kw == 1 ? 32 : 64; }
 constexpr int aw_buffers(int dh, int kw) { return dh == 128 && kw < 4 ? 2 : 3; }      // as many tiles as fit
-template <int DH, int KW, bool DIRECT>
-__global__ __launch_bounds__(AW_WAVES * 64, 2) void attn_weights_kernel(const bf16_t* __restrict__ q, long ldq, const bf16_t* __restrict__ k, long ldk, int T,
+template <int DH, int KW, int WAVES, bool DIRECT>
+__global__ __launch_bounds__(WAVES * 64, 2) void attn_weights_kernel(const bf16_t* __restrict__ q, long ldq, const bf16_t* __restrict__ k, long ldk, int T,
                                                                         int kv_heads, int group, int first_row, const float* __restrict__ lse,
                                                                         float scale_log2e, const float* w_in, long ldi, float* w_out, long ldo, int n_blocks,
                                                                         int paired) {
-    constexpr int QG = AW_WAVES / KW, KB = 64 * KW, NKS = DH / 16, ROWS = aw_rows(KW), SUB = ROWS / 32, NB = aw_buffers(DH, KW);
+    constexpr int QG = WAVES / KW, KB = 64 * KW, NKS = DH / 16, ROWS = aw_rows(KW), SUB = ROWS / 32, NB = aw_buffers(DH, KW);
     constexpr int TQ = ROWS * DH * 2, TB = TQ + 256, NI = TQ / 1024 / KW;      // bytes of a tile's queries, and with their lse; fetches a wave
     static_assert(NI >= 1, "every wave of a group fetches a part of a tile");
     extern __shared__ __align__(16) unsigned char smem_raw[];            // [QG][NB] tiles, then a sum for each key and group
@@ -196,7 +195,7 @@ __global__ __launch_bounds__(AW_WAVES * 64, 2) void attn_weights_kernel(const bf
         __syncthreads();                                                  // (the block before has been read)
         red[qg * KB + kw * 64 + 32 * (l32 >> 4) + 8 * ((l32 & 15) >> 2) + 4 * g + (l32 & 3)] = got[0];
         __syncthreads();
-        for (int i = threadIdx.x; i < KB; i += AW_WAVES * 64) {
+        for (int i = threadIdx.x; i < KB; i += WAVES * 64) {
             const int u = block * KB + i;
             if (u >= T) break;
             float sum = 0.f;
@@ -212,22 +211,29 @@ hipError_t launch_attention_weights(const bf16_t* q, long ldq, const bf16_t* k, 
     const int group = heads / kv_heads;
     const float scale = 1.44269504088896340736f / sqrtf((float)d);
     const bool direct = loads_to_lds(q) && (ldq & 1) == 0;
-    // keys side by side share the queries' way to LDS; fewer where the GPU would not be filled
-    const int kw = (long)kv_heads * (T / 512) >= 256 ? 4 : (long)kv_heads * (T / 256) >= 256 ? 2 : 1;
-    const int n_blocks = cdiv(T, 64 * kw), paired = (long)kv_heads * n_blocks > 256;
+    // Keys side by side share the queries' way to LDS; fewer where the GPU would not be filled.  Four waves, two workgroups to a CU, where the walk over the queries is
+    // short: one workgroup's beginning and end pass under the other's walk.  us with 1, 2, 4 waves side by side of 8, and 1, 2 of 4 (heads over key heads):
+    // 1024 tokens, 32/32: 19.1, 16.7, 22.9, 13.3, 16.3; 2048, 32/32: 45.7, 33.6, 37.2, 32.1, 29.9; 2048, 32/8: 37.1, 63.1, -, 45.5, -; 4096, 32/32: 129, 100, 83.2, 98.9, 86.4;
+    // 4096, 32/8: 89, 123, 215, 101, 149; 8192, 32/8: 322, 292, 429, 314, 348; 777 of 4/4 with heads of 64: 9.2, 12.9, 17.6, 10.5, 13.6
+    const long blocks = (long)kv_heads * ((T + 63) / 64);
+    const int kw = blocks >= 2048 ? 4 : blocks >= 1024 ? 2 : 1;
+    const int waves = kw < 4 && blocks > 256 && (long)T * group <= 4096 ? 4 : 8;
+    const int n_blocks = cdiv(T, 64 * kw), paired = (long)kv_heads * n_blocks > 256 * 8 / waves;
     const int grid = kv_heads * (paired ? (n_blocks + 1) / 2 : n_blocks);
-    const int groups = AW_WAVES / kw, lds = groups * (aw_buffers(d, kw) * (aw_rows(kw) * d * 2 + 256) + 64 * kw * 4);
+    const int groups = waves / kw, lds = groups * (aw_buffers(d, kw) * (aw_rows(kw) * d * 2 + 256) + 64 * kw * 4);
     hipError_t e = hipSuccess;
     auto run = [&](auto kernel) {
         e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-        if (e == hipSuccess) kernel<<<grid, AW_WAVES * 64, lds, s>>>(q, ldq, k, ldk, T, kv_heads, group, first_row, lse, scale, w_in, ldi, w_out, ldo, n_blocks, paired);
+        if (e == hipSuccess)
+            kernel<<<grid, waves * 64, lds, s>>>(q, ldq, k, ldk, T, kv_heads, group, first_row, lse, scale, w_in, ldi, w_out, ldo, n_blocks, paired);
     };
     auto of_width = [&](auto dh, auto di) {
         constexpr int DH = decltype(dh)::value;
         constexpr bool DI = decltype(di)::value;
-        if (kw == 4) run(attn_weights_kernel<DH, 4, DI>);
-        else if (kw == 2) run(attn_weights_kernel<DH, 2, DI>);
-        else run(attn_weights_kernel<DH, 1, DI>);
+        if (waves == 4) kw == 2 ? run(attn_weights_kernel<DH, 2, 4, DI>) : run(attn_weights_kernel<DH, 1, 4, DI>);
+        else if (kw == 4) run(attn_weights_kernel<DH, 4, 8, DI>);
+        else if (kw == 2) run(attn_weights_kernel<DH, 2, 8, DI>);
+        else run(attn_weights_kernel<DH, 1, 8, DI>);
     };
     auto of = [&](auto dh) { direct ? of_width(dh, std::true_type{}) : of_width(dh, std::false_type{}); };
     if (d == 128) of(std::integral_constant<int, 128>{});

@@ -44,9 +44,10 @@ def test_column_sums(api, T, heads, kv, d):
     assert ((both.cpu().double() - full).abs() <= tol + 2.0 ** -24 * full).all()
 
 
-@pytest.mark.parametrize("T,heads,kv,d", [(2300, 32, 32, 64), (1100, 64, 64, 64), (1500, 64, 64, 128), (3000, 64, 64, 128), (2500, 64, 64, 64)])
+@pytest.mark.parametrize("T,heads,kv,d", [(2300, 32, 32, 64), (1100, 64, 64, 64), (1500, 64, 64, 128), (3000, 64, 64, 128), (2500, 64, 64, 64), (900, 32, 32, 128),
+                                            (2050, 32, 32, 128), (1999, 64, 32, 64), (3001, 64, 32, 128), (4300, 64, 32, 64), (700, 64, 64, 64)])
 def test_column_sums_of_many_heads(api, T, heads, kv, d):
-    """keys side by side in two and four waves, blocks in pairs; the columns of a head are what they are without the others"""
+    """keys side by side in one, two and four waves, workgroups of four and of eight, blocks alone and in pairs"""
     g = torch.Generator(device="cuda").manual_seed(T)
     q, k = (torch.randn(T, n * d, generator=g, device="cuda").bfloat16() for n in (heads, kv))
     lse = torch.empty(heads, T, device="cuda")
