@@ -133,6 +133,34 @@ def test_no_infinite_and_undefined_logits(api, V):
         check(api, x, torch.tensor(params), u)
 
 
+@pytest.mark.parametrize("V", [40000, 70000])
+def test_largest_far_above_the_first_logits(api, V):
+    """what the first 2^14 logits say of the largest is wrong by more than any range, or says nothing"""
+    x, u, g = make(4, 12, V)
+    far = (1 << 14) + 5
+    for row, jump in enumerate((7.9, 8.1, 31.0, 33.0, 200.0)):
+        x[row, :far] = x[row, :far].clamp(max=0.0)
+        x[row, far:] -= 30.0
+        x[row, far + row] = jump
+        x[row, far + 50:far + 90] = jump - torch.rand(40, generator=g)
+    x[5, :far] = -math.inf
+    x[6, :far] = math.nan
+    x[7, V - 3] = x[7, far] = math.inf
+    x[8, :far] = -3e38
+    x[9, far:] = 3e38
+    x[10, :-1] = -math.inf
+    x[11, :far] = 100.0                                       # all that counts lies in front
+    for params in ([1.0, 0, 0.9, 0.0], [1.0, 0, 0.5, 0.0], [0.3, 0, 0.97, 0.0], [30.0, 0, 0.8, 0.01], [1e-30, 0, 0.9, 0.0], [1e30, 0, 0.9, 0.0], [math.inf, 0, 0.25, 0.0]):
+        check(api, x, torch.tensor(params), u)
+
+
+def test_many_rows_with_the_largest_far_behind(api):
+    x, u, g = make(5, 260, 33000, 1.0)
+    x[::3, 8192 + 700:] += 40.0
+    x[1::3, 32000] = 11.0
+    check(api, x, torch.tensor([1.0, 0, 0.9, 0.0]), u)
+
+
 def test_strides_and_missing_outputs(api):
     x, u, _ = make(3, 5, 1003)
     want = draw(api, x, SETTINGS[9], u)
