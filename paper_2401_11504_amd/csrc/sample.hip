@@ -198,12 +198,13 @@ struct SampleFound {
 };
 // how the tokens of a row are weighed
 struct SampleRow {
-    float top, to_bins;
+    float half, to_bins;                  // half the largest; bins to half a unit of a logit (halves: a difference of two logits may overflow)
     double top64, per;                    // per: log2(e) / temperature
     __device__ __forceinline__ SampleRow(float top, float temperature)
-        : top(top), to_bins(fminf(64.f / temperature, 3e38f)), top64((double)top), per(1.0 / (double)temperature * 1.44269504088896340736) {}
+        : half(0.5f * top), to_bins(fminf(128.f / temperature, 3e38f)), top64((double)top), per(1.0 / (double)temperature * 1.44269504088896340736) {}
     __device__ __forceinline__ u64 weight(float v) const { return weight_of(((double)v - top64) * per); }
-    __device__ __forceinline__ float place(float v) const { return (top - v) * to_bins; }      // monotone, as each step of it is; its whole part is the bin
+    __device__ __forceinline__ float place_below(float from, float v) const { return fmaf(-0.5f, v, from) * to_bins; }
+    __device__ __forceinline__ float place(float v) const { return place_below(half, v); }      // monotone, as each step of it is; its whole part is the bin
 };
 __device__ __forceinline__ u64 least_weight(float min_p) {
     return !(min_p > 0.f) ? 1ull : min_p >= 1.f ? SAMPLE_ONE : (u64)ceil((double)min_p * (double)SAMPLE_ONE);
@@ -314,7 +315,7 @@ __global__ __launch_bounds__(1024) void sample_weigh_kernel(Sample c, int vocab,
 //   else    the cut is found digit by digit among the tokens of its range (from a list if they fit one), and a last pass draws
 // FOUND: passes 1 and 2, and without top_k and top_p the last one's sums, have been made by the row's pieces.
 // What bounds it: a weight is a series in fp64, 53 us for all tokens of 512 rows of 128000; reading those once is 48 us (5.5 TB/s, the greedy call), and what does not
-// fit a CU is read two or three times.  512 rows of 128000: without a limit 161 us, min-p 89, top-k 50 85, top-k 400 124, top-p 0.9 187, greedy 48.  One row of
+// fit a CU is read two or three times.  512 rows of 128000: without a limit 161 us, min-p 89, top-k 50 85, top-k 400 124, top-p 0.9 190, greedy 48.  One row of
 // 32000, in LDS: 21, 11, 13, 22, 27 and 9 (a call that does nothing: 6); what bounds it is the chain of barriers, scans and sorts on one CU.
 template <int NT, int LIST, bool HELD, bool FOUND>
 __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, SampleFound found_in) {
@@ -426,13 +427,13 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, Samp
         __syncthreads();
 #pragma unroll
         for (int w = 0; w < NW; ++w) first = fmaxf(first, __uint_as_float((unsigned)s.wave_sum[w]));
-        anchor = first + 8.f * temperature;
-        anchored = fabsf(anchor) < INFINITY;
-        const float per_bin = fminf(64.f / temperature, 3e38f);
+        anchor = 0.5f * first + 4.f * temperature;        // (half of it)
+        anchored = fabsf(anchor) < 0x1p126f;              // (nor does a difference from it overflow)
+        const SampleRow from(0.f, temperature);
         if (anchored) {
             all_of([&](float v, int) {
                 m = fmaxf(m, v);
-                const float at = fmaxf((anchor - v) * per_bin, 0.f);
+                const float at = fmaxf(from.place_below(anchor, v), 0.f);
                 if (at < (float)SAMPLE_BINS && v == v) add_about(at);
             });
         } else {
@@ -667,7 +668,7 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, Samp
             const int found = s.found;
             const bool by_anchor = anchored && !infinite;
             const float reach = by_anchor ? INFINITY : SAMPLE_REACH;
-            auto spot = [&](float v) __attribute__((always_inline)) -> float { return by_anchor ? fmaxf((anchor - v) * row.to_bins, 0.f) : place(v); };
+            auto spot = [&](float v) __attribute__((always_inline)) -> float { return by_anchor ? fmaxf(row.place_below(anchor, v), 0.f) : place(v); };
             u64 before_sum = known ? s.found_before_sum : 0, weighed = 0;
             // each token of the bins up to this one weighs about e^-((found + 1) / 64) at least, which says that few can be kept; else what lies before the bin
             // is summed up and its own tokens are listed

@@ -154,6 +154,29 @@ def test_largest_far_above_the_first_logits(api, V):
         check(api, x, torch.tensor(params), u)
 
 
+@pytest.mark.parametrize("V", [3000, 40000, 70000])
+def test_differences_beyond_the_type(api, V):
+    """logits further apart than fp32 goes, and temperatures that bring them together again"""
+    x, u, g = make(6, 10, V)
+    x = 3e38 * torch.sign(x)
+    x[1] = 3.4e38 * (2 * torch.rand(V, generator=g) - 1)
+    x[2, ::7] = 0.0
+    x[3] = -3.4e38
+    x[3, [5, V - 2]] = 3.4e38
+    for params in ([1e38, 0, 0.9, 0.0], [3e37, 0, 0.5, 0.0], [3e38, 30, 1.0, 0.0], [2e37, 3000, 0.99, 0.0], [1e38, 0, 1.0, 0.05], [3e38, 0, 0.6, 0.1], [1e-38, 0, 0.7, 0.0]):
+        check(api, x, torch.tensor(params), u)
+
+
+@pytest.mark.parametrize("V", [3000, 40000, 70000])
+def test_some_undefined_logits(api, V):
+    x, u, g = make(7, 8, V)
+    x[torch.randint(0, 8, (300,), generator=g), torch.randint(0, V, (300,), generator=g)] = math.nan
+    x[0] *= 4.0
+    x[1] *= 0.01
+    for params in ([1.0, 0, 0.9, 0.0], [0.2, 0, 0.6, 0.0], [1.0, 0, 0.999, 0.0], [1.0, 50, 1.0, 0.0], [1.0, 3000, 1.0, 0.0], [1.0, 2500, 0.8, 0.01]):
+        check(api, x, torch.tensor(params), u)
+
+
 def test_many_rows_with_the_largest_far_behind(api):
     x, u, g = make(5, 260, 33000, 1.0)
     x[::3, 8192 + 700:] += 40.0
