@@ -534,7 +534,7 @@ tl_status tl_k_choose(const float* logits, int32_t ldl, int32_t rows, int32_t vo
                       float presence, float frequency, const float* bias, int32_t ldb, const uint32_t* allowed, int32_t lda, float* out,
                       int32_t ldo, int32_t* choice, float* workspace, size_t workspace_elems, void* hip_stream);
 /*
- * A token drawn from each row of logits (fp32 [rows, vocab], vocab up to 2^22) by a given number u (fp32 [rows], from [0, 1); below counts as 0).
+ * A token drawn from each row of logits (fp32 [rows, vocab], each up to 2^22) by a given number u (fp32 [rows], from [0, 1); below counts as 0).
  *   params : fp32 [rows, 4], row stride ldp (0: one row for all): temperature, top_k, top_p, min_p
  *   w_i = round(2^40 exp((x_i - largest) / temperature)): whole numbers, so that sums are exact in any order; NaN and -infinity weigh 0, and where the
  *   largest is infinity only its equals weigh.  The order: larger logits first, the lowest index among equals.  Kept are
@@ -554,7 +554,7 @@ tl_status tl_k_sample(const float* logits, int32_t ldl, int32_t rows, int32_t vo
  *   table : int32 [n_seqs][n_table]; slot j of sequence s lies on page table[s][j / page_size] at place j % page_size.  An entry outside [0, n_pages)
  *           is no page: what would lie there is not written, and passed over when it is read.
  * A sequence's slots are in use from 0 up to its length, which is the caller's to keep (lengths: device int32 [n_seqs]; below 0 counts as 0, beyond the table as
- * all of it).  Keys hold their rotation, so that the order of the slots means nothing to attention.  n_seqs up to 65535, n_seqs * n_kv_heads up to 2^24, n_table * page_size and n_pages up to 2^30.
+ * all of it).  Keys hold their rotation, so that the order of the slots means nothing to attention.  n_seqs up to 65535, n_seqs * n_kv_heads up to 2^21, n_table * page_size and n_pages up to 2^30.
  * Where the table, lengths, first_row or positions change on the device between two calls, the next call sees it (captured graphs as well).
  */
 typedef struct {
@@ -563,7 +563,7 @@ typedef struct {
     int32_t n_pages, page_size, n_kv_heads, d_head, n_seqs, n_table;
 } tl_paged_mem;
 /* Keys and values of new tokens, rows of [n_kv_heads * d_head] bf16 (row strides ldk, ldv in elements, first elements anywhere).  first_row: NULL, row s is sequence s's
- * one new token (n_rows <= n_seqs); or device int32 [n_seqs + 1], not falling: rows first_row[s] .. first_row[s + 1] - 1 are sequence s's, the others nobody's.
+ * one new token (n_rows <= n_seqs, and up to 2^23); or device int32 [n_seqs + 1], not falling: rows first_row[s] .. first_row[s + 1] - 1 are sequence s's, the others nobody's.
  * The i-th of them goes to slot lengths[s] + i (lengths before the call; slots behind the table's end are not written).
  * weights (fp32), positions (int32): [n_seqs][n_kv_heads][ldw], each may be NULL: of the new slots (those below ldw) they become 0 and pos[row] (pos: device int32
  * [n_rows]; NULL: the slot).  A page that two sequences share is written by both. */
@@ -571,10 +571,10 @@ tl_status tl_k_paged_append(const tl_paged_mem* cache, const int32_t* lengths, c
                             const int32_t* first_row, int32_t n_rows, const int32_t* pos, float* weights, int32_t* positions, int32_t ldw, void* hip_stream);
 /* Attention of one query a sequence over its slots 0 .. lengths[s] - 1 (the new token's among them): o = softmax(q K^T / sqrt(d_head)) V, q and o bf16
  * [n_seqs, n_heads * d_head]; n_heads a multiple of n_kv_heads, query head j reads key head j / (n_heads / n_kv_heads).  A sequence without a slot on a page gets 0.
- * max_len: no length is larger (what lies behind is passed over); TL_ERR_WINDOW beyond the table.  n_seqs * n_heads <= 2^24.  Sums over the keys are fp32.
+ * max_len: no length is larger (what lies behind is passed over); TL_ERR_WINDOW beyond the table.  n_seqs * n_heads <= 2^22.  Sums over the keys are fp32.
  * weights_out (fp32 [n_seqs][n_kv_heads][ldw], ldw >= max_len; may be NULL): what each slot got of attention is added up,
  *     weights_out = weights_in + the sum over the query heads of the key head of the softmax's weight      (weights_in: as large, NULL for 0, or weights_out)
- * for slots below the length; the others stay as they are.
+ * for slots below the length; the others stay as they are.  n_seqs * n_kv_heads * ceil(max_len / 1024) <= 2^23 with it.
  * workspace: device fp32 scratch of workspace_elems floats, or NULL: with it the keys are cut into ranges, so that few sequences fill the GPU.  With weights it
  * is needed (TL_ERR_SHAPE otherwise).  Contents are undefined before and after; calls that overlap in time need one each.  tl_k_attention_paged_plan: the ranges that
  * these sizes get with it and the floats that are used (more than workspace_elems: too little for the weights); host only. */

@@ -1951,7 +1951,7 @@ extern "C" tl_status tl_k_choose(const float* logits, int32_t ldl, int32_t rows,
 }
 extern "C" tl_status tl_k_sample(const float* logits, int32_t ldl, int32_t rows, int32_t vocab, const float* params, int32_t ldp, const float* u,
                                  int32_t* choice, int32_t* kept, float* prob, float* workspace, size_t workspace_elems, void* hip_stream) {
-    KARGS_OK(((logits && params && u && choice) || rows == 0) && rows >= 0 && vocab >= 1 && vocab <= kMostSampled && (rows <= 1 || ldl >= vocab) &&
+    KARGS_OK(((logits && params && u && choice) || rows == 0) && rows >= 0 && rows <= kMostSampled && vocab >= 1 && vocab <= kMostSampled && (rows <= 1 || ldl >= vocab) &&
                  (rows <= 1 || ldp == 0 || ldp >= 4), "tl_k_sample");
     Sample c{};
     c.logits = logits, c.ldl = ldl, c.params = params, c.ldp = ldp, c.u = u, c.choice = choice, c.kept = kept, c.prob = prob;
@@ -1964,7 +1964,7 @@ static tl_status paged_of(const tl_paged_mem* m, const char* name, Paged* out) {
     if (((uintptr_t)m->k | (uintptr_t)m->v) & 15) return fail(TL_ERR_ARG, "%s: pages start at multiples of 16 bytes", name);
     const int32_t page = m->page_size;
     if (m->n_kv_heads < 1 || m->n_kv_heads > 4096 || (m->d_head != 64 && m->d_head != 128) || page < 16 || page > 65536 || (page & (page - 1)) || m->n_pages < 1 ||
-        m->n_pages > kMost || m->n_seqs < 0 || m->n_seqs > 65535 || (int64_t)m->n_seqs * m->n_kv_heads > 1 << 24 || m->n_table < 1 || (int64_t)m->n_table * page > kMost)
+        m->n_pages > kMost || m->n_seqs < 0 || m->n_seqs > 65535 || (int64_t)m->n_seqs * m->n_kv_heads > 1 << 21 || m->n_table < 1 || (int64_t)m->n_table * page > kMost)
         return fail(TL_ERR_ARG, "%s: %d heads of %d, %d pages of %d, %d sequences of up to %d", name, m->n_kv_heads, m->d_head, m->n_pages, page, m->n_seqs, m->n_table);
     int shift = 4;
     while (1 << shift < page) ++shift;
@@ -1977,7 +1977,7 @@ extern "C" tl_status tl_k_paged_append(const tl_paged_mem* cache, const int32_t*
     Paged c;
     TLCHK(paged_of(cache, "tl_k_paged_append", &c));
     const int64_t width = (int64_t)c.heads * c.d;
-    KARGS_OK(n_rows >= 0 && n_rows <= kMost && ((lengths && k && v) || n_rows == 0) && (n_rows <= 1 || (ldk >= width && ldv >= width)) &&
+    KARGS_OK(n_rows >= 0 && n_rows <= 1 << 23 && ((lengths && k && v) || n_rows == 0) && (n_rows <= 1 || (ldk >= width && ldv >= width)) &&
                  (first_row ? c.n_seqs > 0 || n_rows == 0 : n_rows <= c.n_seqs) && ((!weights && !positions) || ldw >= 1), "tl_k_paged_append");
     HIPCHK(launch_paged_append(c, lengths, k, ldk, v, ldv, first_row, n_rows, pos, weights, positions, ldw, (hipStream_t)hip_stream));
     return TL_OK;
@@ -1985,7 +1985,7 @@ extern "C" tl_status tl_k_paged_append(const tl_paged_mem* cache, const int32_t*
 // sizes of an attention over pages
 static bool attention_paged_ok(int64_t max_len, int64_t n_seqs, int64_t n_heads, int64_t n_kv_heads) {
     return max_len >= 1 && max_len <= kMost && n_seqs >= 0 && n_seqs <= 65535 && n_heads >= 1 && n_heads <= 65536 && n_heads % n_kv_heads == 0 &&
-           n_seqs * n_heads <= 1 << 24;
+           n_seqs * n_heads <= 1 << 22;
 }
 extern "C" tl_status tl_k_attention_paged(const tl_paged_mem* cache, const int32_t* lengths, int32_t max_len, const uint16_t* q, int32_t ldq, int32_t n_heads,
                                           uint16_t* o, int32_t ldo, const float* weights_in, float* weights_out, int32_t ldw, float* workspace,
@@ -1994,7 +1994,7 @@ extern "C" tl_status tl_k_attention_paged(const tl_paged_mem* cache, const int32
     TLCHK(paged_of(cache, "tl_k_attention_paged", &c));
     KARGS_OK(((lengths && q && o) || c.n_seqs == 0) && attention_paged_ok(max_len, c.n_seqs, n_heads, c.heads) &&
                  (c.n_seqs <= 1 || ((int64_t)ldq >= (int64_t)n_heads * c.d && (int64_t)ldo >= (int64_t)n_heads * c.d)) && (weights_out || !weights_in) &&
-                 (!weights_out || ldw >= max_len), "tl_k_attention_paged");
+                 (!weights_out || (ldw >= max_len && (int64_t)c.n_seqs * c.heads * ((max_len + 1023) / 1024) <= 1 << 23)), "tl_k_attention_paged");
     if (max_len > (int64_t)c.n_table << c.shift) return fail(TL_ERR_WINDOW, "tl_k_attention_paged: %d keys, room for %d pages of %d", max_len, c.n_table, 1 << c.shift);
     if (c.n_seqs == 0) return TL_OK;
     const PagedPlan p = attention_paged_plan(max_len, c.n_seqs, n_heads, c.heads, c.d, weights_out != nullptr, workspace ? workspace_elems : 0);

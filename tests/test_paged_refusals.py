@@ -40,7 +40,7 @@ def evict(api, m, **change):
 @pytest.mark.parametrize("change", [
     dict(k=0), dict(v=0), dict(table=0), dict(k=4104), dict(v=8196), dict(n_pages=0), dict(n_pages=-1), dict(n_pages=2 ** 30 + 1), dict(page_size=0), dict(page_size=8),
     dict(page_size=24), dict(page_size=131072), dict(page_size=-16), dict(n_kv_heads=0), dict(n_kv_heads=5000), dict(d_head=96), dict(d_head=0), dict(n_seqs=-1),
-    dict(n_seqs=65536), dict(n_seqs=65535, n_kv_heads=512), dict(n_table=0), dict(n_table=2 ** 27)])
+    dict(n_seqs=65536), dict(n_seqs=65535, n_kv_heads=512), dict(n_seqs=65535, n_kv_heads=33), dict(n_table=0), dict(n_table=2 ** 27)])
 def test_bad_caches(api, change):
     m = mem(api, **change)
     assert append(api, m) == ARG and attend(api, m) == ARG and evict(api, m) == ARG
@@ -59,7 +59,7 @@ def test_nothing_to_do_is_no_error(api):
 
 
 @pytest.mark.parametrize("change", [
-    dict(lengths=None), dict(k=None), dict(v=None), dict(ldk=127), dict(ldv=100), dict(n_rows=-1), dict(n_rows=4), dict(n_rows=2 ** 30 + 1, first_row=P),
+    dict(lengths=None), dict(k=None), dict(v=None), dict(ldk=127), dict(ldv=100), dict(n_rows=-1), dict(n_rows=4), dict(n_rows=2 ** 30 + 1, first_row=P), dict(n_rows=2 ** 23 + 1, first_row=P),
     dict(weights=P), dict(positions=P, ldw=0), dict(weights=P, ldw=-3)])
 def test_append(api, change):
     assert append(api, mem(api), **change) == ARG
@@ -71,6 +71,13 @@ def test_append(api, change):
     (dict(w_out=P, ldw=80), SHAPE), (dict(w_out=P, ldw=80, workspace=P, elems=3 * 4 * 96 + 23), SHAPE), (dict(w_out=P, ldw=80, elems=1 << 20), SHAPE)])
 def test_attention(api, change, status):
     assert attend(api, mem(api), **change) == status
+
+
+def test_more_weights_than_one_launch_adds_up(api):
+    m = mem(api, n_seqs=1024, n_table=2 ** 26)
+    n = 2 ** 12 * 1024
+    assert attend(api, m, max_len=n + 1, w_out=P, ldw=2 ** 30) == ARG
+    assert attend(api, m, max_len=n, w_out=P, ldw=2 ** 30) == SHAPE
 
 
 @pytest.mark.parametrize("change,status", [
@@ -93,7 +100,7 @@ def test_attention_weights(api, change):
 
 
 @pytest.mark.parametrize("change", [
-    dict(logits=None), dict(params=None), dict(u=None), dict(choice=None), dict(rows=-1), dict(vocab=0), dict(vocab=2 ** 22 + 1), dict(ldl=39), dict(ldp=3), dict(ldp=-4)])
+    dict(logits=None), dict(params=None), dict(u=None), dict(choice=None), dict(rows=-1), dict(rows=2 ** 22 + 1), dict(vocab=0), dict(vocab=2 ** 22 + 1), dict(ldl=39), dict(ldp=3), dict(ldp=-4)])
 def test_sample(api, change):
     a = dict(logits=P, ldl=40, rows=2, vocab=40, params=P, ldp=4, u=P, choice=P, kept=None, prob=None)
     a.update(change)
@@ -101,7 +108,7 @@ def test_sample(api, change):
 
 
 @pytest.mark.parametrize("args", [(0, 1, 4, 4, 64), (2 ** 30 + 1, 1, 4, 4, 64), (5, 0, 4, 4, 64), (5, 1, 3, 2, 64), (5, 1, 4, 0, 64), (5, 1, 4, 4, 80), (5, 65536, 4, 4, 64),
-                                  (5, 65535, 512, 4, 64)])
+                                  (5, 65535, 512, 4, 64), (5, 65535, 68, 4, 64)])
 def test_bad_plans(api, args):
     with pytest.raises(api.TlError):
         api.tl_k_attention_paged_plan(*args)
