@@ -12,6 +12,12 @@ constexpr u64 SAMPLE_ONE = 1ull << 40;
 constexpr int SAMPLE_BINS = 2048;
 constexpr float SAMPLE_REACH = 1846.f;     // 64 units of the bins to one of (largest - x) / temperature: what lies further than 28.84 weighs less than half a unit
 
+// p f + c with a constant of all lanes (the compiler takes the form that adds to its third operand, and copies the constant there before each)
+__device__ __forceinline__ double fma_by(double p, double f, double c) {
+    double r;
+    asm("v_fma_f64 %0, %1, %2, %3" : "=v"(r) : "v"(p), "v"(f), "s"(c));
+    return r;
+}
 // 2^y in units of 2^-40, y <= 0 (NaN: 0), rounded to the nearest: 2^n e^(f ln 2) with y = n + f, |f| <= 1/2, the exponential by its series up to the 13th
 // power (the first term left out is below 2^-57).  n goes into the exponent; adding 2^52 rounds to a whole number and leaves it in the mantissa's low bits.
 __device__ __forceinline__ u64 weight_of(double y) {
@@ -21,18 +27,18 @@ __device__ __forceinline__ u64 weight_of(double y) {
     constexpr double l2 = L * L, l3 = l2 * L, l4 = l3 * L, l5 = l4 * L, l6 = l5 * L, l7 = l6 * L, l8 = l7 * L, l9 = l8 * L, l10 = l9 * L, l11 = l10 * L, l12 = l11 * L,
                      l13 = l12 * L;
     double p = l13 / 6227020800.0;
-    p = fma(p, f, l12 / 479001600.0);
-    p = fma(p, f, l11 / 39916800.0);
-    p = fma(p, f, l10 / 3628800.0);
-    p = fma(p, f, l9 / 362880.0);
-    p = fma(p, f, l8 / 40320.0);
-    p = fma(p, f, l7 / 5040.0);
-    p = fma(p, f, l6 / 720.0);
-    p = fma(p, f, l5 / 120.0);
-    p = fma(p, f, l4 / 24.0);
-    p = fma(p, f, l3 / 6.0);
-    p = fma(p, f, l2 / 2.0);
-    p = fma(p, f, L);
+    p = fma_by(p, f, l12 / 479001600.0);
+    p = fma_by(p, f, l11 / 39916800.0);
+    p = fma_by(p, f, l10 / 3628800.0);
+    p = fma_by(p, f, l9 / 362880.0);
+    p = fma_by(p, f, l8 / 40320.0);
+    p = fma_by(p, f, l7 / 5040.0);
+    p = fma_by(p, f, l6 / 720.0);
+    p = fma_by(p, f, l5 / 120.0);
+    p = fma_by(p, f, l4 / 24.0);
+    p = fma_by(p, f, l3 / 6.0);
+    p = fma_by(p, f, l2 / 2.0);
+    p = fma_by(p, f, L);
     p = fma(p, f, 1.0);
     p = __hiloint2double(__double2hiint(p) + (((int)n + 40) << 20), __double2loint(p)) + 4503599627370496.0;
     return (u64)__double_as_longlong(p) & 0xfffffffffffffull;
