@@ -18,27 +18,22 @@ __device__ __forceinline__ double fma_by(double p, double f, double c) {
     asm("v_fma_f64 %0, %1, %2, %3" : "=v"(r) : "v"(p), "v"(f), "s"(c));
     return r;
 }
-// 2^y in units of 2^-40, y <= 0 (NaN: 0), rounded to the nearest: 2^n e^(f ln 2) with y = n + f, |f| <= 1/2, the exponential by its series up to the 13th
-// power (the first term left out is below 2^-57).  n goes into the exponent; adding 2^52 rounds to a whole number and leaves it in the mantissa's low bits.
+// 2^y in units of 2^-40, y <= 0 (NaN: 0), rounded to the nearest: 2^n 2^f with y = n + f, |f| <= 1/2, 2^f by the polynomial of the 10th degree that equals it at the
+// 11 Chebyshev points of [-1/2, 1/2] (solved for in 50 digits; with its coefficients in fp64 it is off by 2^-51.5 of 2^f at most, as several of an fp64 sum's
+// roundings are).  n goes into the exponent; adding 2^52 rounds to a whole number and leaves it in the mantissa's low bits.
 __device__ __forceinline__ u64 weight_of(double y) {
-    constexpr double L = 0.693147180559945309417;
     y = fmax(y, -60.0);
     const double n = rint(y), f = y - n;
-    constexpr double l2 = L * L, l3 = l2 * L, l4 = l3 * L, l5 = l4 * L, l6 = l5 * L, l7 = l6 * L, l8 = l7 * L, l9 = l8 * L, l10 = l9 * L, l11 = l10 * L, l12 = l11 * L,
-                     l13 = l12 * L;
-    double p = l13 / 6227020800.0;
-    p = fma_by(p, f, l12 / 479001600.0);
-    p = fma_by(p, f, l11 / 39916800.0);
-    p = fma_by(p, f, l10 / 3628800.0);
-    p = fma_by(p, f, l9 / 362880.0);
-    p = fma_by(p, f, l8 / 40320.0);
-    p = fma_by(p, f, l7 / 5040.0);
-    p = fma_by(p, f, l6 / 720.0);
-    p = fma_by(p, f, l5 / 120.0);
-    p = fma_by(p, f, l4 / 24.0);
-    p = fma_by(p, f, l3 / 6.0);
-    p = fma_by(p, f, l2 / 2.0);
-    p = fma_by(p, f, L);
+    double p = 7.072585949269223e-09;
+    p = fma_by(p, f, 1.0208690299958306e-07);
+    p = fma_by(p, f, 1.321544258792169e-06);
+    p = fma_by(p, f, 1.5252657260200837e-05);
+    p = fma_by(p, f, 0.0001540353044173605);
+    p = fma_by(p, f, 0.0013333558230164974);
+    p = fma_by(p, f, 0.009618129107606888);
+    p = fma_by(p, f, 0.05550410866444772);
+    p = fma_by(p, f, 0.24022650695910097);
+    p = fma_by(p, f, 0.69314718055995);
     p = fma(p, f, 1.0);
     p = __hiloint2double(__double2hiint(p) + (((int)n + 40) << 20), __double2loint(p)) + 4503599627370496.0;
     return (u64)__double_as_longlong(p) & 0xfffffffffffffull;
@@ -320,7 +315,7 @@ __global__ __launch_bounds__(1024) void sample_weigh_kernel(Sample c, int vocab,
 //           weighs all tokens, each exactly and once; if more are kept than the list holds, it sums up what lies before the range and lists the range alone
 //   else    the cut is found digit by digit among the tokens of its range (from a list if they fit one), and a last pass draws
 // FOUND: passes 1 and 2, and without top_k and top_p the last one's sums, have been made by the row's pieces.
-// What bounds it: a weight is a series in fp64, 53 us for all tokens of 512 rows of 128000; reading those once is 48 us (5.5 TB/s, the greedy call), and what does not
+// What bounds it: a weight is a polynomial in fp64, 53 us for all tokens of 512 rows of 128000; reading those once is 48 us (5.5 TB/s, the greedy call), and what does not
 // fit a CU is read two or three times.  512 rows of 128000: without a limit 161 us, min-p 89, top-k 50 85, top-k 400 124, top-p 0.9 190, greedy 48.  One row of
 // 32000, in LDS: 21, 11, 13, 22, 27 and 9 (a call that does nothing: 6); what bounds it is the chain of barriers, scans and sorts on one CU.
 template <int NT, int LIST, bool HELD, bool FOUND>
