@@ -801,7 +801,7 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, Samp
         if (low <= top) bar = fmaxf(bar, low);
     }
     auto kept_weight = [&](float v, int i) __attribute__((always_inline)) -> u64 {
-        if (!(v >= bar) || (v == cut_at && i > cut_index)) return 0;
+        if (!(v >= bar) || (cut && v == cut_at && i > cut_index)) return 0;
         const u64 w = weight(v);
         return w >= least ? w : 0;
     };
@@ -810,7 +810,8 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, Samp
         if (tid == 0) n_kept = found_in.count[r * (SAMPLE_BINS + 1) + SAMPLE_BINS];
         __syncthreads();
     } else if (!summed) {
-        n_kept = sum_chunks(kept_weight);
+        if (!cut && least == 1) n_kept = sum_chunks([&](float v, int) __attribute__((always_inline)) -> u64 { return weight(v); });      // (19 of 133 us for 512 rows of 128000)
+        else n_kept = sum_chunks(kept_weight);
     }
     int kept;
     u64 all;
