@@ -383,9 +383,10 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, Samp
     const int k = wanted(top_k, vocab);
     const int bits = __clz(vocab) - 1;                     // (as many units of 2^-bits as tokens fit 31 bits)
     // a token's weight into the count of its bin, as find_about reads it: the part of e^(-place / 64) behind the bin's own, e^-in with in < 1/64, by three terms
+    const float unit = (float)(1 << bits);
     auto add_about = [&](float at) __attribute__((always_inline)) {
-        const float in = __builtin_amdgcn_fractf(at) * (1.f / 64.f);
-        atomicAdd(&s.count[(int)at], (int)((float)(1 << bits) * fmaf(in, fmaf(in, 0.5f, -1.f), 1.f)));
+        const float in = __builtin_amdgcn_fractf(at);
+        atomicAdd(&s.count[(int)at], (int)fmaf(in, fmaf(in, unit * (0.5f / 4096.f), unit * (-1.f / 64.f)), unit));
     };
     // With top_p alone a row that has to be read again is looked through for its largest and for where the cut lies at once: the bins then begin 8 temperatures
     // above the largest of its first logits.  (512 rows of 128000, top_p 0.9: 213 us with a pass for each.)
@@ -434,8 +435,8 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, Samp
         if (anchored) {
             all_of([&](float v, int) {
                 m = fmaxf(m, v);
-                const float at = fmaxf(from.place_below(anchor, v), 0.f);
-                if (at < (float)SAMPLE_BINS && v == v) add_about(at);
+                const float at = from.place_below(anchor, v);
+                if (at < (float)SAMPLE_BINS) add_about(fmaxf(at, 0.f));
             });
         } else {
             all_of([&](float v, int) { m = fmaxf(m, v); });
@@ -668,8 +669,9 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, Samp
             }
             const int found = s.found;
             const bool by_anchor = anchored && !infinite;
-            const float reach = by_anchor ? INFINITY : SAMPLE_REACH;
-            auto spot = [&](float v) __attribute__((always_inline)) -> float { return by_anchor ? fmaxf(row.place_below(anchor, v), 0.f) : place(v); };
+            // (what lies as far below the largest weighs nothing from the anchor on either)
+            const float half = by_anchor ? anchor : row.half, reach = by_anchor ? fmaxf(row.place_below(anchor, top), 0.f) + SAMPLE_REACH : SAMPLE_REACH;
+            auto spot = [&](float v) __attribute__((always_inline)) -> float { return row.place_below(half, v); };
             u64 before_sum = known ? s.found_before_sum : 0, weighed = 0;
             // each token of the bins up to this one weighs about e^-((found + 1) / 64) at least, which says that few can be kept; else what lies before the bin
             // is summed up and its own tokens are listed
@@ -692,24 +694,29 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, Samp
                 const int n = s.n_list;
                 if (n <= NT && draw_listed(n, false, total)) return;
             } else {
-                const float b = (float)found;
+                const float b = found ? (float)found : -INFINITY;        // (the first bin: from anywhere on; its end is 1)
+                const float b_end = (float)(found + 1);
                 u64 ahead = 0;
                 n_kept = sum_chunks([&](float v, int i) __attribute__((always_inline)) -> u64 {
                     const float at = spot(v);
-                    if (!(at < (known ? b + 1.f : reach))) return 0;
-                    if (at >= b && at < b + 1.f) {
+                    if (!(at < (known ? b_end : reach))) return 0;
+                    const bool before = at < b;
+                    if (!before && at < b_end) {
                         const int to = atomicAdd(&s.n_list, 1);
                         if (to < LIST) s.list[to] = composite(v, i);
                     }
-                    if (known && at >= b) return 0;
+                    if (known && !before) return 0;
                     const u64 w = weight(v);
                     weighed += w;
-                    if (at >= b) return 0;
+                    if (!before) return 0;
+                    if (least == 1) return w;
                     ahead += w;
                     return w >= least ? w : 0;
                 });
                 const int n = s.n_list;
                 if (!known) {
+                    if (least == 1)
+                        for (int i = tid; i < NW * n_chunks; i += NT) ahead += s.sum[i];
                     block_scan(s, weighed, &total);
                     block_scan(s, ahead, &before_sum);
                 }
@@ -724,7 +731,7 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, Samp
                             u64 sums[SAMPLE_BINS / NT];
 #pragma unroll
                             for (int j = 0; j < SAMPLE_BINS / NT; ++j) sums[j] = s.sum[j * NT + tid];
-                            cut = cut_digits(b, n, 0, before_sum, false, limit, &unused);
+                            cut = cut_digits((float)found, n, 0, before_sum, false, limit, &unused);
 #pragma unroll
                             for (int j = 0; j < SAMPLE_BINS / NT; ++j) s.sum[j * NT + tid] = sums[j];
                             __syncthreads();
