@@ -19,7 +19,8 @@ __device__ __forceinline__ long slot_at(const Paged& c, int id, int head, int sl
 }
 
 // ---------------------------------------------------------------- append
-// One workgroup a row of new tokens: 16 bytes of k and of v a thread at a time.
+// One workgroup a row of new tokens: 16 bytes of k and of v a thread at a time.  Bytes bound it from some hundred rows on (2048 rows of 32 heads of 128: 67 MB in and out, 14 us,
+// 4.8 TB/s, as a large copy), below that one chain of loads and stores: 1.8 us for a row, 4.6 for 64.
 __global__ __launch_bounds__(256) void paged_append_kernel(Paged c, const int* __restrict__ lengths, const bf16_t* __restrict__ k, long ldk,
                                                            const bf16_t* __restrict__ v, long ldv, const int* __restrict__ first_row,
                                                            const int* __restrict__ pos, float* __restrict__ weights, int* __restrict__ positions, long ldw) {
@@ -72,8 +73,8 @@ hipError_t launch_paged_append(const Paged& c, const int* lengths, const bf16_t*
 // they lie there, nothing goes through LDS, and nothing is exchanged between lanes but the maximum, and that only where it grows by 2^8.
 // Weights are split into two bf16 parts, cut off and rounded, so that they are off by 2^-15 of themselves (the matrix unit has nothing else to do
 // here); the second is above 0, so that an infinite value gives an infinity and not 0 times it.
-// What bounds it: HBM for long texts (131072 keys of 8 key heads 81 us, 6.6 TB/s; 64 texts of up to 4096, 671 MB, 112 us, 6 TB/s), below that the chain at a
-// workgroup's start: length, page, keys (3800 keys of 32 heads 13 us, 62 MB).
+// What bounds it: HBM for long texts (131072 keys of 8 key heads 81 us, 6.6 TB/s; 64 texts of up to 4096, 683 MB, 117 us, 5.8 TB/s), below that the chain at a
+// workgroup's start: length, page, keys (3800 keys of 32 heads 13 us for 63 MB).
 __device__ __forceinline__ f32x4_t mfma16(bf16x8_t a, bf16x8_t b, f32x4_t c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 template <int W> struct Words;
 template <> struct Words<4> { typedef u32x4_t type; };
@@ -260,8 +261,8 @@ __device__ __forceinline__ float join_ranges(const float2* ml, int live, int lan
     *sum = wave_sum(*a != 0.f ? *a * mine.y : 0.f);
     return top;
 }
-// Behind the ranges: the first n_join workgroups join the outputs, 256 / D query heads each, NR ranges' columns asked for at a time, the others add what
-// 1024 slots of a key head got:
+// Behind the ranges: the first n_join workgroups join the outputs, 256 / D query heads each, NR ranges' columns asked for at a time (as a chain of loads 32 ranges take
+// 4.6 us, 8 take 4.0), the others add what 1024 slots of a key head got (33 texts of up to 2000, 40 heads over 8: 7 us for both):
 //   weights_out[slot] = weights_in[slot] + the sum over the group's query heads of 2^(x - log2 of the sum of weights)
 template <int D, int NR>
 __global__ __launch_bounds__(256) void paged_join_kernel(Paged c, const int* __restrict__ lengths, int max_len, int group, bf16_t* __restrict__ o, long ldo,

@@ -315,9 +315,10 @@ __global__ __launch_bounds__(1024) void sample_weigh_kernel(Sample c, int vocab,
 //           weighs all tokens, each exactly and once; if more are kept than the list holds, it sums up what lies before the range and lists the range alone
 //   else    the cut is found digit by digit among the tokens of its range (from a list if they fit one), and a last pass draws
 // FOUND: passes 1 and 2, and without top_k and top_p the last one's sums, have been made by the row's pieces.
-// What bounds it: a weight is a polynomial in fp64, 53 us for all tokens of 512 rows of 128000; reading those once is 48 us (5.5 TB/s, the greedy call), and what does not
-// fit a CU is read two or three times.  512 rows of 128000: without a limit 161 us, min-p 89, top-k 50 85, top-k 400 124, top-p 0.9 190, greedy 48.  One row of
-// 32000, in LDS: 21, 11, 13, 22, 27 and 9 (a call that does nothing: 6); what bounds it is the chain of barriers, scans and sorts on one CU.
+// What bounds it: a weight is 21 instructions of the vector unit, most in fp64 (35 us for all tokens of 512 rows of 128000), and with what goes on around it 25 to 50;
+// reading those once is 47 us (5.6 TB/s, the greedy call), and what does not fit a CU is read two or three times.  512 rows of 128000: without a limit 114 us, min-p 88,
+// top-k 50 85, top-k 400 124, top-p 0.9 158, greedy 47.  One row of 32000, in LDS: 15, 11, 13, 22, 24 and 8 (a call that does nothing: 6); what bounds it is the chain of
+// barriers, scans and sorts on one CU.
 template <int NT, int LIST, bool HELD, bool FOUND>
 __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, SampleFound found_in) {
     constexpr int NW = NT / 64;
@@ -389,7 +390,7 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, Samp
         atomicAdd(&s.count[(int)at], (int)fmaf(in, fmaf(in, unit * (0.5f / 4096.f), unit * (-1.f / 64.f)), unit));
     };
     // With top_p alone a row that has to be read again is looked through for its largest and for where the cut lies at once: the bins then begin 8 temperatures
-    // above the largest of its first logits.  (512 rows of 128000, top_p 0.9: 213 us with a pass for each.)
+    // above the largest of its first logits.  (512 rows of 128000, top_p 0.9: 213 us with a pass for each, 186 so; other steps since: 158.)
     bool anchored = false;
     float anchor = 0.f;
     float m = -INFINITY;
@@ -871,9 +872,9 @@ hipError_t launch_sample(const Sample& c, int rows, int vocab, float* ws, size_t
         sample_kernel<1024, 1024, true, false><<<rows, 1024, lds, s>>>(c, vocab, w);
         return hipGetLastError();
     }
-    // Few rows of many tokens: pieces of a row on CUs of their own, then a workgroup a row.  us for one row of 40000 / 65000 / 128000 in pieces and in one
-    // workgroup: top-k 50 21 and 14 / 23 and 16 / 26 and 22, top-p 0.9 30 and 33 / 35 and 46 / 46 and 79, min-p 16 and 12 / 16 and 16 / 16 and 24, no limit 16 and
-    // 24 / 16 and 35 / 17 and 63 (two launches more are 6 us of it); 16 rows of 128000 31 and 22, 88 and 116, 18 and 25, 19 and 64.
+    // Few rows of many tokens: pieces of a row on CUs of their own, then a workgroup a row.  us in pieces and in one workgroup, one row of 66000 / of 128000 / 16 rows of
+    // 66000 / of 128000: no limit 17 and 25 / 18 and 40 / 17 and 26 / 19 and 40, min-p 17 and 17 / 16 and 25 / 17 and 17 / 18 and 25, top-p 0.9 36 and 38 / 45 and 60 /
+    // 58 and 51 / 83 and 77, top-k 50 23 and 17 / 27 and 22 / 25 and 17 / 32 and 23 (two launches more are 6 us of it; the settings are not known here).
     const size_t at = (uintptr_t)ws & 7 ? 1 : 0;           // (64-bit places in scratch that begins at any multiple of 4)
     w.pieces = cdiv(vocab, SAMPLE_PIECE);
     const size_t need = at + (size_t)rows * (2 * w.pieces + 3 * SAMPLE_BINS + 1);
