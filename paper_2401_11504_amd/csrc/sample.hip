@@ -317,7 +317,7 @@ __global__ __launch_bounds__(1024) void sample_weigh_kernel(Sample c, int vocab,
 // FOUND: passes 1 and 2, and without top_k and top_p the last one's sums, have been made by the row's pieces.
 // What bounds it: a weight is 21 instructions of the vector unit, most in fp64 (35 us for all tokens of 512 rows of 128000), and with what goes on around it 25 to 50;
 // reading those once is 47 us (5.6 TB/s, the greedy call), and what does not fit a CU is read two or three times.  512 rows of 128000: without a limit 114 us, min-p 88,
-// top-k 50 85, top-k 400 124, top-p 0.9 158, greedy 47.  One row of 32000, in LDS: 15, 11, 13, 22, 24 and 8 (a call that does nothing: 6); what bounds it is the chain of
+// top-k 50 85, top-k 400 93 (124 with a pass of its own to count), top-p 0.9 158, greedy 47.  One row of 32000, in LDS: 15, 11, 13, 22, 24 and 8 (a call that does nothing: 6); what bounds it is the chain of
 // barriers, scans and sorts on one CU.
 template <int NT, int LIST, bool HELD, bool FOUND>
 __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, SampleFound found_in) {
@@ -389,8 +389,8 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, Samp
         const float in = __builtin_amdgcn_fractf(at);
         atomicAdd(&s.count[(int)at], (int)fmaf(in, fmaf(in, unit * (0.5f / 4096.f), unit * (-1.f / 64.f)), unit));
     };
-    // With top_p alone a row that has to be read again is looked through for its largest and for where the cut lies at once: the bins then begin 8 temperatures
-    // above the largest of its first logits.  (512 rows of 128000, top_p 0.9: 213 us with a pass for each, 186 so; other steps since: 158.)
+    // With top_p alone, or as many wanted as a sort holds, a row that has to be read again is looked through for its largest and for where the cut lies at once: the bins
+    // then begin 8 temperatures above the largest of its first logits.  (512 rows of 128000, top_p 0.9: 213 us with a pass for each, 186 so; other steps since: 158.)
     bool anchored = false;
     float anchor = 0.f;
     float m = -INFINITY;
@@ -414,7 +414,7 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, Samp
                 m = fmaxf(m, fmaxf(fmaxf(v[k].x, v[k].y), fmaxf(v[k].z, v[k].w)));
             }
         }
-    } else if (p_on && !k && !greedy) {
+    } else if (!greedy && (k ? k > NT / 4 && k <= NT - NT / 8 : p_on)) {
         float first = -INFINITY;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -437,7 +437,9 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, Samp
             all_of([&](float v, int) {
                 m = fmaxf(m, v);
                 const float at = from.place_below(anchor, v);
-                if (at < (float)SAMPLE_BINS) add_about(fmaxf(at, 0.f));
+                if (!(at < (float)SAMPLE_BINS)) return;
+                if (k) atomicAdd(&s.count[(int)fmaxf(at, 0.f)], 1);
+                else add_about(fmaxf(at, 0.f));
             });
         } else {
             all_of([&](float v, int) { m = fmaxf(m, v); });
@@ -633,6 +635,22 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, Samp
             }
             clear();
             if (tid == 0) s.n_list = 0;
+        }
+        if (by_count && anchored) {                        // as many as are wanted, and few more, where the bins from the anchor on say
+            const bool told = !infinite;
+            if (told) find_bin<NT, false>(s, true, (u64)k, 0, 0);
+            const int few = s.found_before + s.found_count;
+            if (told && s.found >= 0 && few <= NT) {
+                const float end = (float)(s.found + 1);
+                all_of([&](float v, int i) {
+                    if (row.place_below(anchor, v) < end) s.list[atomicAdd(&s.n_list, 1)] = composite(v, i);
+                });
+                __syncthreads();
+                draw_listed(few, true, 0);
+                return;
+            }
+            anchored = false;
+            clear();
         }
         if (by_count) {
             if (!FOUND) {

@@ -154,6 +154,24 @@ def test_largest_far_above_the_first_logits(api, V):
         check(api, x, torch.tensor(params), u)
 
 
+@pytest.mark.parametrize("rows,k", [(9, 257), (9, 600), (9, 896), (9, 897), (257, 129), (257, 400), (257, 448), (257, 449)])
+def test_as_many_wanted_as_a_sort_holds(api, rows, k):
+    """rows that are read again, the wanted tokens spread, among equals, behind the first logits, fewer than there are, none defined, infinite"""
+    V, far = (33001, 20000) if rows < 257 else (9501, 8500)
+    x, u, g = make(k, rows, V, 1.0)
+    x[1, far:] += 12.0
+    x[2, far:far + 300] += 60.0
+    x[3] = torch.round(x[3])
+    x[4, 100:] = -math.inf
+    x[5] = -90.0
+    x[5, ::500] = 0.0
+    x[6, ::3] = math.nan
+    x[7, far:far + 500] = math.inf
+    x[8] *= 40.0
+    for params in ([1.0, k, 1.0, 0.0], [0.3, k, 0.7, 0.0], [1.0, k, 0.95, 0.01]):
+        check(api, x, torch.tensor(params), u)
+
+
 @pytest.mark.parametrize("V", [3000, 40000, 70000])
 def test_differences_beyond_the_type(api, V):
     """logits further apart than fp32 goes, and temperatures that bring them together again"""
