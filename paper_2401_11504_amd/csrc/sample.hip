@@ -210,6 +210,8 @@ struct SampleRow {
 __device__ __forceinline__ u64 least_weight(float min_p) {
     return !(min_p > 0.f) ? 1ull : min_p >= 1.f ? SAMPLE_ONE : (u64)ceil((double)min_p * (double)SAMPLE_ONE);
 }
+// How far below the largest, in temperatures, a weight that rounds to `least` lies at most, and a little more for the roundings of what is compared with it
+__device__ __forceinline__ float reach_of_least(u64 least) { return 0.001f - __logf(((float)least - 0.5f) * 0x1p-40f); }
 __device__ __forceinline__ int wanted(float top_k, int vocab) { return top_k >= 1.f && top_k < (float)vocab ? (int)top_k : 0; }
 // the larger of all lanes' composites, in every lane
 __device__ __forceinline__ u64 wave_best(u64 v) {
@@ -823,7 +825,7 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, Samp
     const int cut_index = cut ? index_of(cut) : 0;
     float bar = cut_at;
     if (least > 1) {
-        const float low = top - 1.0001f * temperature * (0.001f - __logf(fminf(min_p, 1.f))) - 1e-6f * fabsf(top);
+        const float low = top - 1.0001f * temperature * reach_of_least(least) - 1e-6f * fabsf(top);
         if (low <= top) bar = fmaxf(bar, low);
     }
     auto kept_weight = [&](float v, int i) __attribute__((always_inline)) -> u64 {

@@ -154,6 +154,18 @@ def test_largest_far_above_the_first_logits(api, V):
         check(api, x, torch.tensor(params), u)
 
 
+@pytest.mark.parametrize("V", [3000, 40000, 70000])
+def test_least_weights_of_a_few_units(api, V):
+    """min_p of a unit or two of 2^-40: weights round up to it"""
+    g = torch.Generator().manual_seed(V)
+    x = -26.0 - 3.0 * torch.rand(6, V, generator=g)
+    x[torch.arange(6), torch.randint(0, V, (6,), generator=g)] = 0.0
+    u = 1 - torch.rand(6, generator=g) * 2.0 ** -20
+    for units in (0.3, 1.0, 1.2, 1.5, 1.9, 2.0, 2.4, 5.7):
+        check(api, x, torch.tensor([1.0, 0, 1.0, units * 2.0 ** -40]), u)
+    check(api, 0.5 * x, torch.tensor([0.5, 0, 1.0, 1.9 * 2.0 ** -40]), u)
+
+
 @pytest.mark.parametrize("rows,k", [(9, 257), (9, 600), (9, 896), (9, 897), (257, 129), (257, 400), (257, 448), (257, 449)])
 def test_as_many_wanted_as_a_sort_holds(api, rows, k):
     """rows that are read again, the wanted tokens spread, among equals, behind the first logits, fewer than there are, none defined, infinite"""
