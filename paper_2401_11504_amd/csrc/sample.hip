@@ -383,6 +383,7 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, Samp
     auto all_of = [&](auto&& f) __attribute__((always_inline)) { each(std::integral_constant<int, NT>{}, 0, padded, tid, f); };
 
     const bool greedy = !(temperature > 0.f), p_on = top_p < 1.f;
+    const u64 least = least_weight(min_p);
     const int k = wanted(top_k, vocab);
     const int bits = __clz(vocab) - 1;                     // (as many units of 2^-bits as tokens fit 31 bits)
     // a token's weight into the count of its bin, as find_about reads it: the part of e^(-place / 64) behind the bin's own, e^-in with in < 1/64, by three terms
@@ -395,6 +396,9 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, Samp
     // then begin 8 temperatures above the largest of its first logits.  (512 rows of 128000, top_p 0.9: 213 us with a pass for each, 186 so; other steps since: 158.)
     bool anchored = false;
     float anchor = 0.f;
+    // With few wanted, or min_p alone, what the first logits rule out is ruled out by all: the others, as far as they find room, are listed while the largest is looked for.
+    // (512 rows of 128000, top-k 50 85 us with a reading for each, min-p 88.)
+    bool listed = false;
     float m = -INFINITY;
     int lowest = 0;
     if (FOUND) {
@@ -416,7 +420,7 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, Samp
                 m = fmaxf(m, fmaxf(fmaxf(v[k].x, v[k].y), fmaxf(v[k].z, v[k].w)));
             }
         }
-    } else if (!greedy && (k ? k > NT / 4 && k <= NT - NT / 8 : p_on)) {
+    } else if (!greedy && (k ? k <= NT - NT / 8 : p_on || min_p > 0.f)) {
         float first = -INFINITY;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -426,8 +430,10 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, Samp
                 first = fmaxf(first, fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)));
             }
         }
+        const float own_first = first;
         first = wave_max(first);
         if (lane == 0) s.wave_sum[wave] = __float_as_uint(first);
+        if (tid == 0) s.n_list = 0;
         for (int i = tid; i < SAMPLE_BINS; i += NT) s.count[i] = 0;
         __syncthreads();
 #pragma unroll
@@ -435,7 +441,30 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, Samp
         anchor = 0.5f * first + 4.f * temperature;        // (half of it)
         anchored = fabsf(anchor) < 0x1p126f;              // (nor does a difference from it overflow)
         const SampleRow from(0.f, temperature);
-        if (anchored) {
+        float end = 0.f;
+        if (anchored && (k ? k <= NT / 4 : !p_on)) {
+            anchored = false;
+            anchor = 0.5f * first;
+            if (k) {                                       // the k-th of the threads' own largest is no larger than the k-th of all
+                const float b = from.place_below(anchor, own_first);
+                if (b < (float)SAMPLE_BINS) atomicAdd(&s.count[(int)b], 1);
+                __syncthreads();
+                find_bin<NT, false>(s, true, (u64)k, 0, 0);
+                end = (float)(s.found + 1);
+            } else {                                       // (with a margin for the roundings)
+                end = 64.f * 1.0001f * reach_of_least(least) + 1.f;
+            }
+            listed = end > 0.f;
+        }
+        if (listed) {
+            all_of([&](float v, int i) {
+                m = fmaxf(m, v);
+                if (from.place_below(anchor, v) < end) {
+                    const int at = atomicAdd(&s.n_list, 1);
+                    if (at < LIST) s.list[at] = composite(v, i);
+                }
+            });
+        } else if (anchored) {
             all_of([&](float v, int) {
                 m = fmaxf(m, v);
                 const float at = from.place_below(anchor, v);
@@ -455,7 +484,8 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, Samp
     const float own_top = m;
     m = wave_max(m);
     if (lane == 0) s.wave_sum[wave] = __float_as_uint(m);
-    if (tid == 0) s.n_list = 0, s.lowest = 0;
+    if (tid == 0) s.lowest = 0;
+    if (tid == 0 && !listed) s.n_list = 0;
     for (int i = tid; i < SAMPLE_BINS; i += NT) {
         s.sum[i] = 0;
         if (!anchored) s.count[i] = 0;
@@ -486,12 +516,65 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, Samp
     const SampleRow row(top, temperature);
     auto weight = [&](float v) __attribute__((always_inline)) -> u64 { return row.weight(v); };
     auto place = [&](float v) -> float { return row.place(v); };
-    const u64 least = least_weight(min_p);
     auto limit_of = [&](u64 sum) -> u64 { return top_p > 0.f ? (u64)ceil((double)top_p * (double)sum) : 1ull; };
     auto place_in = [&](u64 all) -> u64 {
         const u64 t = (u64)floor((double)fminf(fmaxf(u, 0.f), 1.f) * (double)all);
         return t < all ? t : all - 1;
     };
+    // the list, one token a thread, holds all that can be kept: sorted, cut, sorted by index and drawn from
+    auto draw_listed = [&](int n, bool by_count, u64 total) __attribute__((always_inline)) -> bool {
+        u64 e = tid < n ? s.list[tid] : 0;
+        __syncthreads();
+        e = block_sort(s, e, n);
+        u64 w = tid < n && !(by_count && tid >= k) ? weight(logit_of(e)) : 0, all;
+        const u64 before = block_scan(s, w, &all) - w;
+        if (by_count) total = all;
+        else if (all < limit_of(total)) return false;        // (uniform) the cut lies behind what is listed
+        const bool keep = w >= least && (!p_on || tid == 0 || before < limit_of(total));
+        const int kept = __syncthreads_count(keep);
+        u64 o = keep ? ~((u64)index_of(e) << 41 | w) : 0;    // (weights have 41 bits, indices 22)
+        o = block_sort(s, o, by_count ? min(n, k) : n);
+        w = o ? ~o & ((1ull << 41) - 1) : 0;
+        const u64 upto = block_scan(s, w, &all), t = place_in(all);
+        if (upto - w <= t && t < upto) out((int)(~o >> 41), kept, (float)((double)w / (double)all));
+        return true;
+    };
+    if (listed) {
+        int n = s.n_list;
+        if (!infinite && n > NT && n <= LIST) {            // by the row's own largest now
+            u64 e[LIST / NT];
+            float end = SAMPLE_REACH;
+#pragma unroll
+            for (int j = 0; j < LIST / NT; ++j) {
+                e[j] = j * NT + tid < n ? s.list[j * NT + tid] : 0;
+                const float b = place(logit_of(e[j]));
+                if (k && e[j] && b < SAMPLE_REACH) atomicAdd(&s.count[(int)b], 1);
+            }
+            __syncthreads();
+            if (tid == 0) s.n_list = 0;
+            if (k) {
+                find_bin<NT, false>(s, true, (u64)k, 0, 0);
+                if (s.found >= 0) end = (float)(s.found + 1);
+            }
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < LIST / NT; ++j)
+                if (e[j] && (k ? place(logit_of(e[j])) < end : weight(logit_of(e[j])) >= least)) {
+                    const int at = atomicAdd(&s.n_list, 1);
+                    if (at < NT) s.list[at] = e[j];
+                }
+            __syncthreads();
+            n = s.n_list;
+        }
+        if (!infinite && n <= NT) {
+            draw_listed(n, k > 0, 0);
+            return;
+        }
+        __syncthreads();
+        if (tid == 0) s.n_list = 0;
+        for (int i = tid; i < SAMPLE_BINS; i += NT) s.count[i] = 0;
+        __syncthreads();
+    }
     u64 cut = 0;                                           // kept: composites from here on
     // What is kept of each chunk of the row, to s.sum; a wave's share is n_chunks of them, so that a thread has few tokens to go through where the place is.
     // Returns how many tokens this thread saw that are.
@@ -541,24 +624,6 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, Samp
                 }
             });
             __syncthreads();
-        };
-        // the list, one token a thread, holds all that can be kept: sorted, cut, sorted by index and drawn from
-        auto draw_listed = [&](int n, bool by_count, u64 total) __attribute__((always_inline)) -> bool {
-            u64 e = tid < n ? s.list[tid] : 0;
-            __syncthreads();
-            e = block_sort(s, e, n);
-            u64 w = tid < n && !(by_count && tid >= k) ? weight(logit_of(e)) : 0, all;
-            const u64 before = block_scan(s, w, &all) - w;
-            if (by_count) total = all;
-            else if (all < limit_of(total)) return false;        // (uniform) the cut lies behind what is listed
-            const bool keep = w >= least && (!p_on || tid == 0 || before < limit_of(total));
-            const int kept = __syncthreads_count(keep);
-            u64 o = keep ? ~((u64)index_of(e) << 41 | w) : 0;    // (weights have 41 bits, indices 22)
-            o = block_sort(s, o, by_count ? min(n, k) : n);
-            w = o ? ~o & ((1ull << 41) - 1) : 0;
-            const u64 upto = block_scan(s, w, &all), t = place_in(all);
-            if (upto - w <= t && t < upto) out((int)(~o >> 41), kept, (float)((double)w / (double)all));
-            return true;
         };
         // the last composite of the list, one token a thread, that is kept with `before` tokens and before_sum before it; what weighs up to it
         auto cut_list = [&](int n, int before, u64 before_sum, bool count_mode, u64 limit, u64* sum_upto) __attribute__((always_inline)) -> u64 {

@@ -166,6 +166,28 @@ def test_least_weights_of_a_few_units(api, V):
     check(api, 0.5 * x, torch.tensor([0.5, 0, 1.0, 1.9 * 2.0 ** -40]), u)
 
 
+@pytest.mark.parametrize("rows,V", [(12, 33001), (12, 150001), (257, 9501)])
+def test_few_wanted_where_the_first_logits_rule_out_others(api, rows, V):
+    """what is listed beside the first look: more than a sort holds, more than the list holds, all of it, nothing that counts, undefined and infinite logits"""
+    far = (1 << 14) + 5 if rows < 257 else 8200
+    x, u, g = make(rows + V, rows, V, 2.0)
+    x[1, far:] += 30.0                                        # the first say nothing
+    x[2, far:far + 700] += 30.0
+    x[3] = 0.0                                                # equals
+    x[4] = torch.round(x[4])
+    x[5, :far] = -math.inf
+    x[6, :far] = math.nan
+    x[7, far + 3] = x[7, far + 900] = math.inf
+    x[8, 40:] = -math.inf
+    x[9] = torch.linspace(-50, 0, V)                          # each larger than all before
+    x[10] = torch.linspace(0, -50, V)
+    x[11] *= 1e30
+    for params in ([1.0, 1, 1.0, 0.0], [1.0, 50, 1.0, 0.0], [0.7, 128, 0.9, 0.01], [1.0, 0, 1.0, 0.02], [0.4, 0, 1.0, 1e-6], [1.0, 0, 1.0, 1.0], [1e30, 60, 1.0, 0.0]):
+        check(api, x[:12], torch.tensor(params), u[:12])
+    check(api, x, torch.tensor([1.0, 30, 0.95, 0.0]), u)
+    check(api, x, torch.tensor([1.0, 0, 1.0, 0.05]), u)
+
+
 @pytest.mark.parametrize("rows,k", [(9, 257), (9, 600), (9, 896), (9, 897), (257, 129), (257, 400), (257, 448), (257, 449)])
 def test_as_many_wanted_as_a_sort_holds(api, rows, k):
     """rows that are read again, the wanted tokens spread, among equals, behind the first logits, fewer than there are, none defined, infinite"""
