@@ -136,25 +136,32 @@ __device__ __forceinline__ void find_bin(S& s, bool by_count, u64 limit, int bef
     __syncthreads();
 }
 // The same where about so much weighs: in the place of the counts lie the tokens' weights as parts of the largest that the bin has room for, whole
-// numbers in units of 2^-bits.  (32-bit sums of whole numbers are several times faster here than of 64 bits, or of floating point.)  Returns what weighs up to
-// the bin's end, in units of the largest weight.
+// numbers in units of 2^-bits.  (32-bit sums of whole numbers are several times faster here than of 64 bits, or of floating point.)  Where the place lies next to a
+// border, s.found and *last are the bins on both sides: a row whose cut lies beside the bin found is read twice more (before, one of some thousands: a call of 256 rows 145
+// instead of 89 us).  Returns what weighs up to the last one's end, in units of the largest weight.
 template <int NT, class S>
-__device__ __forceinline__ float find_about(S& s, float p, int bits) {
+__device__ __forceinline__ float find_about(S& s, float p, int bits, int* last) {
     constexpr int N = SAMPLE_BINS / NT;
     const int b = N * threadIdx.x;
     float w[N], ws = 0.f, all;
 #pragma unroll
     for (int i = 0; i < N; ++i) w[i] = (float)(unsigned)s.count[b + i] * __builtin_amdgcn_exp2f((float)(b + i) * (-1.44269504088896340736f / 64.f) - (float)bits), ws += w[i];
-    if (threadIdx.x == 0) s.found = SAMPLE_BINS - 1, s.about = 0.f;       // (nowhere: roundings, and the caller finds out)
+    if (threadIdx.x == 0) s.found = SAMPLE_BINS - 1, s.found_count = 0, s.about = 0.f;       // (nowhere: roundings, and the caller finds out)
     const float mine = ws;
     ws = block_scan(s, ws, &all) - mine;
-    const float limit = p * all;
+    const float slack = all * __builtin_amdgcn_exp2f((float)(-bits - 4)), low = p * all - slack, high = p * all + slack;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        if (w[i] > 0.f && (ws < limit || b + i == 0) && limit <= ws + w[i]) atomicMin(&s.found, b + i), s.about = ws + w[i];
-        ws += w[i];
+        const float end = ws + w[i];
+        if (w[i] > 0.f && (ws < high || b + i == 0) && low <= end) {
+            atomicMin(&s.found, b + i);
+            atomicMax(&s.found_count, b + i);
+            atomicMax((int*)&s.about, __float_as_int(end));        // (both above 0)
+        }
+        ws = end;
     }
     __syncthreads();
+    *last = max(s.found, s.found_count);
     return s.about;
 }
 // one value a thread, the largest in thread 0; n of them are not 0
@@ -316,10 +323,11 @@ __global__ __launch_bounds__(1024) void sample_weigh_kernel(Sample c, int vocab,
 //   pass 3  what lies in the ranges up to the one with the cut is listed; up to a token a thread, the list is sorted, cut and drawn from.  With top_p this pass
 //           weighs all tokens, each exactly and once; if more are kept than the list holds, it sums up what lies before the range and lists the range alone
 //   else    the cut is found digit by digit among the tokens of its range (from a list if they fit one), and a last pass draws
+// Where a row has to be read again, passes 1 and 2 are one, from what the first logits say of the largest (anchored), or all three are (listed).
 // FOUND: passes 1 and 2, and without top_k and top_p the last one's sums, have been made by the row's pieces.
 // What bounds it: a weight is 21 instructions of the vector unit, most in fp64 (35 us for all tokens of 512 rows of 128000), and with what goes on around it 25 to 50;
-// reading those once is 47 us (5.6 TB/s, the greedy call), and what does not fit a CU is read two or three times.  512 rows of 128000: without a limit 114 us, min-p 88,
-// top-k 50 85, top-k 400 93 (124 with a pass of its own to count), top-p 0.9 158, greedy 47.  One row of 32000, in LDS: 15, 11, 13, 22, 24 and 8 (a call that does nothing: 6); what bounds it is the chain of
+// reading those once is 47 us (5.6 TB/s, the greedy call), and what does not fit a CU is read two or three times.  512 rows of 128000: without a limit 114 us, min-p 59,
+// top-k 50 59, top-k 400 93 (124 with a pass of its own to count), top-p 0.9 158, greedy 47.  One row of 32000, in LDS: 15, 11, 13, 22, 24 and 8 (a call that does nothing: 6); what bounds it is the chain of
 // barriers, scans and sorts on one CU.
 template <int NT, int LIST, bool HELD, bool FOUND>
 __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, SampleFound found_in) {
@@ -736,12 +744,14 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, Samp
             // out whether that was right.
             const bool known = FOUND && !k;
             float upto;
+            int last;
             if (known) {
                 u64 mine = 0;
                 for (int i = tid; i < SAMPLE_BINS; i += NT) mine += s.sum[i];
                 block_scan(s, mine, &total);
                 find_bin<NT, true>(s, false, limit_of(total), 0, 0);
                 upto = (float)((double)(s.found_before_sum + s.found_sum) / (double)SAMPLE_ONE);
+                last = s.found;
             } else {
                 if (!anchored || infinite) {
                     if (anchored) clear();
@@ -751,7 +761,7 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, Samp
                     });
                     __syncthreads();
                 }
-                upto = find_about<NT>(s, top_p, bits);
+                upto = find_about<NT>(s, top_p, bits, &last);
             }
             const int found = s.found;
             const bool by_anchor = anchored && !infinite;
@@ -761,10 +771,10 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, Samp
             u64 before_sum = known ? s.found_before_sum : 0, weighed = 0;
             // each token of the bins up to this one weighs about e^-((found + 1) / 64) at least, which says that few can be kept; else what lies before the bin
             // is summed up and its own tokens are listed
-            if (upto * __expf((float)(found + 1) * (1.f / 64.f)) < 0.9f * NT) {
+            if (upto * __expf((float)(last + 1) * (1.f / 64.f)) < 0.9f * NT) {
                 if (known) list_upto(found);
                 else {
-                    const float end = (float)(found + 1);
+                    const float end = (float)(last + 1);
                     all_of([&](float v, int i) {
                         const float at = spot(v);
                         if (!(at < reach)) return;
@@ -781,7 +791,7 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, Samp
                 if (n <= NT && draw_listed(n, false, total)) return;
             } else {
                 const float b = found ? (float)found : -INFINITY;        // (the first bin: from anywhere on; its end is 1)
-                const float b_end = (float)(found + 1);
+                const float b_end = (float)(last + 1);
                 u64 ahead = 0;
                 n_kept = sum_chunks([&](float v, int i) __attribute__((always_inline)) -> u64 {
                     const float at = spot(v);
