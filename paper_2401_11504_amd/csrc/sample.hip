@@ -967,9 +967,10 @@ hipError_t launch_sample(const Sample& c, int rows, int vocab, float* ws, size_t
         sample_kernel<1024, 1024, true, false><<<rows, 1024, lds, s>>>(c, vocab, w);
         return hipGetLastError();
     }
-    // Few rows of many tokens: pieces of a row on CUs of their own, then a workgroup a row.  us in pieces and in one workgroup, one row of 66000 / of 128000 / 16 rows of
-    // 66000 / of 128000: no limit 17 and 25 / 18 and 40 / 17 and 26 / 19 and 40, min-p 17 and 17 / 16 and 25 / 17 and 17 / 18 and 25, top-p 0.9 36 and 38 / 45 and 60 /
-    // 58 and 51 / 83 and 77, top-k 50 23 and 17 / 27 and 22 / 25 and 17 / 32 and 23 (two launches more are 6 us of it; the settings are not known here).
+    // Few rows of many tokens: pieces of a row on CUs of their own, then a workgroup a row.  us in pieces and in one workgroup, one row of 66000 / 128000 / 262144 / 1000000, 16 of
+    // 66000 / 128000 / 262144: no limit 17 and 26 / 18 and 40 / 21 and 73 / 37 and 283, 18 and 26 / 19 and 41 / 27 and 81; min-p 17 and 15 / 17 and 18 / 17 and 26 / 18 and 91, 18 and 16 / 18
+    // and 22 / 23 and 36; top-p 0.9 36 and 40 / 46 and 62 / 68 and 111 / 193 and 396, 58 and 53 / 83 and 79 / 139 and 144; top-k 50 24 and 18 / 27 and 24 / 34 and 35 / 100 and 167, 24
+    // and 19 / 31 and 25 / 45 and 43 (two launches more are 6 us of it; the settings are not known here).
     const size_t at = (uintptr_t)ws & 7 ? 1 : 0;           // (64-bit places in scratch that begins at any multiple of 4)
     w.pieces = cdiv(vocab, SAMPLE_PIECE);
     const size_t need = at + (size_t)rows * (2 * w.pieces + 3 * SAMPLE_BINS + 1);
