@@ -356,7 +356,7 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, Samp
     };
     // f(x[i], i), the lanes side by side, from the first on to the end, both multiples of 4; U times four a lane at a time, the next on their way
     auto each = [&](auto lanes, int first, int end, int at, auto&& f) __attribute__((always_inline)) {
-        constexpr int LANES = decltype(lanes)::value, U = HELD ? 1 : 2;
+        constexpr int LANES = decltype(lanes)::value, U = HELD ? 1 : FOUND ? 2 : 4;
         float4 v[U], next[U];
         auto fetch = [&](int i0) __attribute__((always_inline)) {
 #pragma unroll
@@ -586,7 +586,7 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, Samp
     u64 cut = 0;                                           // kept: composites from here on
     // What is kept of each chunk of the row, to s.sum; a wave's share is n_chunks of them, so that a thread has few tokens to go through where the place is.
     // Returns how many tokens this thread saw that are.
-    constexpr int UNIT = HELD ? 256 : 512, CHUNKS = HELD ? 1 : SAMPLE_BINS / NW;
+    constexpr int UNIT = HELD ? 256 : FOUND ? SAMPLE_CHUNK : 1024, CHUNKS = HELD ? 1 : SAMPLE_BINS / NW;
     const int per_wave = (vocab + NW - 1) / NW, chunk = ((per_wave + CHUNKS - 1) / CHUNKS + UNIT - 1) / UNIT * UNIT, n_chunks = (per_wave + chunk - 1) / chunk;
     auto sum_chunks = [&](auto&& kept_of) __attribute__((always_inline)) -> int {
         const int mine = wave * n_chunks * chunk;
