@@ -326,8 +326,8 @@ __global__ __launch_bounds__(1024) void sample_weigh_kernel(Sample c, int vocab,
 // Where a row has to be read again, passes 1 and 2 are one, from what the first logits say of the largest (anchored), or all three are (listed).
 // FOUND: passes 1 and 2, and without top_k and top_p the last one's sums, have been made by the row's pieces.
 // What bounds it: a weight is 21 instructions of the vector unit, most in fp64 (35 us for all tokens of 512 rows of 128000), and with what goes on around it 25 to 50;
-// reading those once is 47 us (5.6 TB/s, the greedy call), and what does not fit a CU is read two or three times.  512 rows of 128000: without a limit 114 us, min-p 59,
-// top-k 50 59, top-k 400 93 (124 with a pass of its own to count), top-p 0.9 158, greedy 47.  One row of 32000, in LDS: 15, 11, 13, 22, 24 and 8 (a call that does nothing: 6); what bounds it is the chain of
+// reading those once is 47 us (5.6 TB/s, the greedy call), and what does not fit a CU is read two or three times.  512 rows of 128000: without a limit 110 us, min-p 59,
+// top-k 50 59, top-k 400 93 (124 with a pass of its own to count), top-p 0.9 156, greedy 47.  One row of 32000, in LDS: 15, 11, 13, 22, 24 and 8 (a call that does nothing: 6); what bounds it is the chain of
 // barriers, scans and sorts on one CU.
 template <int NT, int LIST, bool HELD, bool FOUND>
 __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, SampleFound found_in) {
@@ -401,7 +401,7 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, Samp
         atomicAdd(&s.count[(int)at], (int)fmaf(in, fmaf(in, unit * (0.5f / 4096.f), unit * (-1.f / 64.f)), unit));
     };
     // With top_p alone, or as many wanted as a sort holds, a row that has to be read again is looked through for its largest and for where the cut lies at once: the bins
-    // then begin 8 temperatures above the largest of its first logits.  (512 rows of 128000, top_p 0.9: 213 us with a pass for each, 186 so; other steps since: 158.)
+    // then begin 8 temperatures above the largest of its first logits.  (512 rows of 128000, top_p 0.9: 213 us with a pass for each, 186 so; other steps since: 156.)
     bool anchored = false;
     float anchor = 0.f;
     // With few wanted, or min_p alone, what the first logits rule out is ruled out by all: the others, as far as they find room, are listed while the largest is looked for.
@@ -462,7 +462,9 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, Samp
             } else {                                       // (with a margin for the roundings)
                 end = 64.f * 1.0001f * reach_of_least(least) + 1.f;
             }
-            listed = end > 0.f;
+            // (not where so many threads' tokens pass that all will not find room: 104 us instead of 111 with min_p 1e-3)
+            const int pass = __syncthreads_count(from.place_below(anchor, own_first) < end);
+            listed = pass > 0 && (long)pass * vocab <= (long)LIST * 16 * NT;
         }
         if (listed) {
             all_of([&](float v, int i) {
