@@ -964,7 +964,8 @@ hipError_t launch_sample(const Sample& c, int rows, int vocab, float* ws, size_t
     SampleFound w{};
     if (vocab <= SAMPLE_HELD && rows <= 256) {
         const int lds = ((vocab + 3) & ~3) * 4;
-        const hipError_t e = hipFuncSetAttribute((const void*)sample_kernel<1024, 1024, true, false>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        const hipError_t e = hipFuncSetAttribute((const void*)sample_kernel<1024, 1024, true, false>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                                 SAMPLE_HELD * 4);        // (the same from every thread of the host)
         if (e != hipSuccess) return e;
         sample_kernel<1024, 1024, true, false><<<rows, 1024, lds, s>>>(c, vocab, w);
         return hipGetLastError();

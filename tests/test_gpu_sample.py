@@ -300,3 +300,27 @@ def test_captured(api):
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(choice, want[0]) and torch.equal(kept, want[1]) and torch.equal(prob, want[2])
+
+
+def test_two_threads_of_the_host(api):
+    """rows of different lengths drawn at once, each thread on a stream of its own"""
+    from concurrent.futures import ThreadPoolExecutor
+
+    def work(V):
+        x, u, _ = make(V, 8, V)
+        x, u, p = x.cuda(), u.cuda(), SETTINGS[:8].cuda()
+        choice = torch.empty(8, dtype=torch.int32, device="cuda")
+        torch.cuda.synchronize()
+        stream, out = torch.cuda.Stream(), []
+        with torch.cuda.stream(stream):
+            for _ in range(40):
+                choice.fill_(-9)
+                api.tl_k_sample(x, p, u, choice)
+                out.append(choice.tolist())
+        return out
+
+    sizes = (32000, 64, 20001)
+    want = {V: draw(api, make(V, 8, V)[0], SETTINGS[:8], make(V, 8, V)[1])[0].tolist() for V in sizes}
+    with ThreadPoolExecutor(3) as pool:
+        for V, got in zip(sizes, pool.map(work, sizes)):
+            assert all(g == want[V] for g in got)
