@@ -386,7 +386,9 @@ hipError_t launch_attention_paged(const Paged& c, const int* lengths, int max_le
 
 // ---------------------------------------------------------------- eviction
 // One workgroup a sequence and key head: which slots stay.  The order: recent tokens, larger weights, lower slots; the budget-th of it is
-// found digit by digit (11, 11 and 10 bits) by counts of a key that has the same order.  Kept slots below the budget stay where they are; the
+// found digit by digit (11, 11 and 10 bits) by counts of a key of 32 bits that has the same order: that of the weight, and the largest for what is recent, which
+// all stays.  Where the counts of the first digit say that more come first than stay, the keys become those of the order among these (crowded_key), and the count
+// begins again.  Kept slots below the budget stay where they are; the
 // i-th slot that becomes free there receives the i-th kept one from behind.  The pairs go to ws: [count or ~length][from .., to ..].
 __device__ __forceinline__ unsigned order_key(float w) {
     const unsigned u = __float_as_uint(w + 0.f);           // (-0 counts as 0)
@@ -394,6 +396,10 @@ __device__ __forceinline__ unsigned order_key(float w) {
 }
 // A slot on no page holds nothing and could take nothing: below the budget it stays, behind it goes before all others.
 __device__ __forceinline__ unsigned no_page_key(int slot, int budget) { return slot < budget ? 0xffffffffu : 0u; }
+// Only what comes first can stay: the recent ones by their weights, all of them before the others.
+__device__ __forceinline__ unsigned crowded_key(bool recent, float w) { return recent ? max(order_key(w), 1u) : 0u; }
+// (No weight's key reaches this bin of the first digit.)
+constexpr int EVICT_FIRST_BIN = 2047;
 // the bin, from the last down, in which the count first reaches `need`: *bin, and what of `need` is left for it (hist: BINS counts)
 template <int NT, int BINS>
 __device__ __forceinline__ void find_from_top(const int* hist, int* sums, int* found, int need, int* bin, int* left) {
@@ -487,6 +493,7 @@ __global__ __launch_bounds__(NT, 4) void evict_select_kernel(Paged c, const int*
     __builtin_amdgcn_sched_barrier(0);
     unsigned prefix = 0;
     int need = budget;                                     // of the slots whose key begins with the prefix, so many stay
+    bool crowded = false;                                  // more come first than stay
     auto digit = [&](auto shift_of, auto above_of) {
         constexpr int SHIFT = decltype(shift_of)::value, ABOVE = decltype(above_of)::value, BINS = 1 << (ABOVE - SHIFT);
 #pragma unroll
@@ -498,6 +505,10 @@ __global__ __launch_bounds__(NT, 4) void evict_select_kernel(Paged c, const int*
         int bin;
         find_from_top<NT, BINS>(hist, sums, found, need, &bin, &need);
         prefix |= (unsigned)bin << SHIFT;
+        if (SHIFT == 21 && bin == EVICT_FIRST_BIN) {       // (uniform)
+            crowded = hist[EVICT_FIRST_BIN] > need;
+            __syncthreads();
+        }
         if (SHIFT) {
             for (int i = tid; i < 2048; i += NT) hist[i] = 0;
             __syncthreads();
@@ -505,6 +516,18 @@ __global__ __launch_bounds__(NT, 4) void evict_select_kernel(Paged c, const int*
     };
     using std::integral_constant;
     digit(integral_constant<int, 21>{}, integral_constant<int, 32>{});
+    if (crowded) {                                         // (uniform; what the keys were made of is read again, so that no registers hold it)
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int i = 4 * (k * NT + tid) + e;
+                const bool first = i < len && key[k][e] == 0xffffffffu;
+                if (!first || page_of(c, seq, i) >= 0) key[k][e] = crowded_key(first, first ? wr[i] : 0.f);
+            }
+        prefix = 0, need = budget;
+        digit(integral_constant<int, 21>{}, integral_constant<int, 32>{});
+    }
     digit(integral_constant<int, 10>{}, integral_constant<int, 21>{});
     digit(integral_constant<int, 0>{}, integral_constant<int, 10>{});
     const int n_equal = hist[prefix & 1023];
@@ -619,9 +642,11 @@ __global__ __launch_bounds__(EVICT_NT) void evict_select_long_kernel(Paged c, co
     __syncthreads();
     for (int w = 0; w < NWV; ++w) newest = max(newest, sums[0][w]);
     const long border = (long)newest - n_recent;
+    unsigned recent_bits = 0xffffffffu, other_bits = 0xffffffffu;        // (both 0: crowded_key)
     auto key_of = [&](int i) -> unsigned {
         if (page_of(c, seq, i) < 0) return no_page_key(i, budget);
-        return (long)p_in[row + i] > border ? 0xffffffffu : order_key(w_in[row + i]);
+        const unsigned key = order_key(w_in[row + i]);
+        return (long)p_in[row + i] > border ? max(key | recent_bits, 1u) : key & other_bits;
     };
     unsigned prefix = 0;
     int need = budget;                                     // of the slots whose key begins with the prefix, so many stay
@@ -639,6 +664,10 @@ __global__ __launch_bounds__(EVICT_NT) void evict_select_long_kernel(Paged c, co
         int bin;
         if (d == 2) find_from_top<NT, 1024>(hist, sums[0], found, need, &bin, &need);
         else find_from_top<NT, 2048>(hist, sums[0], found, need, &bin, &need);
+        if (d == 0 && bin == EVICT_FIRST_BIN && hist[EVICT_FIRST_BIN] > need) {        // (uniform; once: then no more slots than stay are left in this bin)
+            recent_bits = other_bits = 0, need = budget, d = -1;
+            continue;
+        }
         prefix |= (unsigned)bin << shift;
     }
     // in the order of the slots: equal keys, slots that become free below the budget, kept ones behind it

@@ -79,11 +79,10 @@ def evict(k_pool, v_pool, table, lengths, budget, recent, weights, positions):
 
             def rank(j):
                 if page_of(table, n_pages, s, j, page) < 0:
-                    return (0 if j < budget else 2, 0.0, j)
-                if int(positions[s, h, j]) > newest - recent:
-                    return (0, 0.0, j)
+                    return (0 if j < budget else 3, 0, 0.0, j)
                 w = float(weights[s, h, j])
-                return (2, 0.0, j) if w != w else (1, -w, j)
+                of_recent = 1 if int(positions[s, h, j]) > newest - recent else 2
+                return (of_recent, 1, 0.0, j) if w != w else (of_recent, 0, -w, j)
             kept = sorted(range(n), key=rank)[:budget]
             src = sorted(j for j in kept if j >= budget)
             dst = sorted(set(range(min(n, budget))) - set(kept))
