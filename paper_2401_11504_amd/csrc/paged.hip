@@ -756,10 +756,10 @@ hipError_t launch_paged_evict(const Paged& c, const int* lengths, int budget, in
     else if (width <= 16384) select(evict_select_kernel<1024, 4>, 1024);
     else if (width <= 32768) select(evict_select_kernel<1024, 8>, 1024);
     else select(evict_select_long_kernel, EVICT_NT);
-    const long room = (1L << 24) / ((long)c.n_seqs * c.heads);
-    const int n_chunks = most > 0 ? (int)(cdiv(most, 32) < room ? cdiv(most, 32) : room < 1 ? 1 : room) : 1;
+    const long room = (1L << 23) / rows;                   // (fewer than 2^32 threads in a launch; at most 2^21 rows, so 4 and more)
+    const int n_chunks = most > 0 ? (int)(cdiv(most, 32) < room ? cdiv(most, 32) : room) : 1;
     auto move = [&](auto kernel) {
-        kernel<<<c.n_seqs * c.heads * n_chunks, 256, 0, s>>>(c, budget, ws, ld, width <= 32768 ? 0 : most, w_in, p_in, ldw, w_out, p_out, lengths_out, n_chunks);
+        kernel<<<rows * n_chunks, 256, 0, s>>>(c, budget, ws, ld, width <= 32768 ? 0 : most, w_in, p_in, ldw, w_out, p_out, lengths_out, n_chunks);
     };
     if (c.d == 128) move(evict_move_kernel<128>);
     else move(evict_move_kernel<64>);
