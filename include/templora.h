@@ -538,7 +538,7 @@ tl_status tl_k_choose(const float* logits, int32_t ldl, int32_t rows, int32_t vo
  *   params : fp32 [rows, 4], row stride ldp (0: one row for all): temperature, top_k, top_p, min_p
  *   w_i = round(2^40 exp((x_i - largest) / temperature)): whole numbers, so that sums are exact in any order; NaN and -infinity weigh 0, and where the
  *   largest is infinity only its equals weigh.  The order: larger logits first, the lowest index among equals.  Kept are
- *     the first top_k of the order (below 1, or vocab and more: all; fractions are cut off),
+ *     the first top_k of the order (below 1, vocab and more, or NaN: all; fractions are cut off),
  *     of these, with W the sum of their weights, those before which less than ceil(top_p W) weighs (1 and more, or NaN: all; the first always),
  *     of these, those that weigh at least ceil(min_p 2^40), min_p taken as 1 at most (0 and below, or NaN: all), and at least 1.
  *   choice (int32 [rows]): with S the kept weight, the first token in the order of indices up to which more than min(floor(u S), S - 1) is kept;
@@ -571,7 +571,8 @@ tl_status tl_k_paged_append(const tl_paged_mem* cache, const int32_t* lengths, c
                             const int32_t* first_row, int32_t n_rows, const int32_t* pos, float* weights, int32_t* positions, int32_t ldw, void* hip_stream);
 /* Attention of one query a sequence over its slots 0 .. lengths[s] - 1 (the new token's among them): o = softmax(q K^T / sqrt(d_head)) V, q and o bf16
  * [n_seqs, n_heads * d_head]; n_heads a multiple of n_kv_heads, query head j reads key head j / (n_heads / n_kv_heads).  A sequence without a slot on a page gets 0.
- * max_len: no length is larger (what lies behind is passed over); TL_ERR_WINDOW beyond the table.  n_seqs * n_heads <= 2^22.  Sums over the keys are fp32.
+ * max_len: no length is larger (what lies behind is passed over); TL_ERR_WINDOW beyond the table.  n_seqs * n_heads <= 2^22.  Sums over the keys are fp32; the softmax's weights
+ * go into the product with V in two bf16 parts, off by 2^-15 of themselves at most (what weights_out adds up is fp32).
  * weights_out (fp32 [n_seqs][n_kv_heads][ldw], ldw >= max_len; may be NULL): what each slot got of attention is added up,
  *     weights_out = weights_in + the sum over the query heads of the key head of the softmax's weight      (weights_in: as large, NULL for 0, or weights_out)
  * for slots below the length; the others stay as they are.  n_seqs * n_kv_heads * ceil(max_len / 1024) <= 2^23 with it.
@@ -591,14 +592,15 @@ tl_status tl_k_attention_weights(const uint16_t* q, int32_t ldq, const uint16_t*
                                  int32_t d_head, int32_t first_row, const float* lse, const float* weights_in, int32_t ldi, float* weights_out, int32_t ldo,
                                  void* hip_stream);
 /* Cuts sequences longer than `budget` slots back to it, each key head by itself: kept are the first `budget` slots of the order
- *     recent tokens (position > the head's newest position - n_recent) before others, then larger weights (NaN counts as the least), then lower slots;
+ *     recent tokens (position > the head's newest position - n_recent, the newest of all its slots, on pages or not) before others, then, among either, larger weights
+ *     (NaN counts as the least), then lower slots: where more are recent than `budget`, the recent ones that got most stay;
  *     a slot on no page holds nothing and can take nothing: below the budget it comes first (it stays), behind it after all others.
  * Kept slots below the budget stay where they are; the i-th slot there that is not kept receives the i-th kept one from behind (key, value, weight, position).
  *   weights fp32, positions int32 [n_seqs][n_kv_heads][ldw] (slots from ldw on are not looked at: lengths count as ldw at most); weights_out, positions_out: as
  *   large, or the same; slots below min(length, budget) are written.  lengths_out (int32 [n_seqs], or lengths): min(length, budget).  Pages wholly behind it are free.
  * workspace: device fp32 scratch of n_seqs * n_kv_heads * (2 * min(budget, longest - budget) + 1) floats or more, longest = min(n_table * page_size, ldw), the
- * minimum taken as 0 at least (TL_ERR_SHAPE otherwise); calls that overlap in time need one each.  A page that a table holds twice, or that sequences that
- * are cut back share, ends up with what either wrote. */
+ * minimum taken as 0 at least (TL_ERR_SHAPE otherwise); calls that overlap in time need one each.  A page below the budget that a table holds twice, or that another
+ * sequence's table holds too (cut back or not), is written for each sequence that is cut back, in any order. */
 tl_status tl_k_paged_evict(const tl_paged_mem* cache, const int32_t* lengths, int32_t budget, int32_t n_recent, const float* weights, const int32_t* positions,
                            int32_t ldw, float* weights_out, int32_t* positions_out, int32_t* lengths_out, float* workspace, size_t workspace_elems,
                            void* hip_stream);

@@ -340,7 +340,8 @@ PagedPlan attention_paged_plan(int max_len, int n_seqs, int heads, int kv_heads,
     // seldom full, ranges of 256 (short texts) or 640 keys.  A range alone needs no second launch.  us, by ranges:
     // 131072 keys of 8 key heads 16 / 24 / 32 / 64: 136 / 102 / 89 / 90; 3800 of 32 heads 4 / 8 / 16: 27 / 21 / 21; 8 texts of up to 4000, 8 key heads 4 / 7 / 8 / 16:
     // 27 / 29 / 26 / 25; 64 of up to 4096 1 / 2 / 4 / 7 / 8 / 16 / 32: 130 / 149 / 140 / 120 / 127 / 131 / 146; 16 of up to 16000 8 / 16 / 24 / 32 / 64: 139 / 118 /
-    // 113 / 118 / 123; 33 of up to 2000, with weights 1 / 2 / 4 / 8 / 16: 74 / 64 / 58 / 52 / 53; 64 of up to 500 1 / 2 / 4: 23 / 28 / 31.
+    // 113 / 118 / 123; 33 of up to 2000, with weights 1 / 2 / 4 / 8 / 16: 74 / 64 / 58 / 52 / 53; 64 of up to 500 1 / 2 / 4: 23 / 28 / 31.  Ranges of
+    // 256 and of 640 keys around the border, 8 key heads: 64 of up to 1500 50 and 51, 2040 68 and 73, 2400 76 and 88, 3000 96 and 89, 4096 128 and 117; 33 with weights, 2000 48 and 55, 2400 54 and 65, 3600 75 and 79.
     int n = 1;
     if (max_len > 512) n = (int)(groups < 64 ? 256 / groups : std::max(1024 / groups, max_len <= 2048 ? ((long)max_len + 255) / 256 : ((long)max_len + 639) / 640));
     n = n > most ? most : n;
@@ -614,7 +615,8 @@ __global__ __launch_bounds__(NT, 4) void evict_select_kernel(Paged c, const int*
             }
         }
 }
-// The same for any number of slots, which are read again by every pass; the slots that move there lie `most` behind those that become free.
+// The same for any number of slots, which are read again by every pass; the slots that move there lie `most` behind those that become free.  The call for 8 heads: 40000
+// slots 149 us, 131072 452; what bounds it is one CU a head, five readings and four barriers to 1024 slots in the last.
 constexpr int EVICT_NT = 1024;
 __global__ __launch_bounds__(EVICT_NT) void evict_select_long_kernel(Paged c, const int* __restrict__ lengths, int budget, int n_recent, const float* w_in,
                                                                 const int* p_in, long ldw, float* w_out, int* p_out, int* __restrict__ ws, long ws_ld) {
@@ -701,7 +703,7 @@ __global__ __launch_bounds__(EVICT_NT) void evict_select_long_kernel(Paged c, co
     if (tid == 0) list[0] = n_move;
 }
 // The rows of the pairs, d / 8 lanes each for k and for v, 32 pairs a workgroup at a time, their weights and positions, and the new lengths.  apart: how far behind
-// the first free slot of a list the first one that moves lies (0: as many as there are).  Bytes bound it: 131072 pairs of 512 bytes 32 us, 4.2 TB/s in and out.
+// the first free slot of a list the first one that moves lies (0: as many as there are).  Bytes bound it: 118000 pairs of 512 bytes 31.5 us, 3.85 TB/s in and out.
 template <int D>
 __global__ __launch_bounds__(256) void evict_move_kernel(Paged c, int budget, const int* __restrict__ ws, long ws_ld, long apart, const float* w_in, const int* p_in,
                                                          long ldw, float* w_out, int* p_out, int* __restrict__ lengths_out, int n_chunks) {
@@ -748,7 +750,7 @@ hipError_t launch_paged_evict(const Paged& c, const int* lengths, int budget, in
     const long most = width - budget < budget ? (width - budget > 0 ? width - budget : 0) : budget, ld = 1 + 2 * most;
     const int rows = c.n_seqs * c.heads;
     // Many threads a row, few slots a thread: latency bounds these kernels.  us, 64 sequences of 8 heads and 2112 slots with 256 threads of up to 32 / 16 slots,
-    // 512 of 8, 1024 of 4: 25.5 / 20.5 / 18.3 / 17.2 for the call
+    // 512 of 8, 1024 of 4: 25.5 / 20.5 / 18.3 / 17.2 for the call.  By the room for slots, as lengths are not known here: the same with room for 2112 / 32768 / 65536: 22 / 89 / 68.
     auto select = [&](auto kernel, int threads) { kernel<<<rows, threads, 0, s>>>(c, lengths, budget, n_recent, w_in, p_in, ldw, w_out, p_out, ws, ld); };
     if (width <= 1024) select(evict_select_kernel<256, 1>, 256);
     else if (width <= 4096) select(evict_select_kernel<1024, 1>, 1024);

@@ -327,7 +327,7 @@ __global__ __launch_bounds__(1024) void sample_weigh_kernel(Sample c, int vocab,
 // FOUND: passes 1 and 2, and without top_k and top_p the last one's sums, have been made by the row's pieces.
 // What bounds it: a weight is 21 instructions of the vector unit, most in fp64 (35 us for all tokens of 512 rows of 128000), and with what goes on around it 25 to 50;
 // reading those once is 47 us (5.6 TB/s, the greedy call), and what does not fit a CU is read two or three times.  512 rows of 128000: without a limit 110 us, min-p 59,
-// top-k 50 59, top-k 400 93 (124 with a pass of its own to count), top-p 0.9 156, greedy 47.  One row of 32000, in LDS: 15, 11, 13, 22, 24 and 8 (a call that does nothing: 6); what bounds it is the chain of
+// top-k 50 59, top-k 400 93 (124 with a pass of its own to count), top-k 1000 217, top-p 0.9 148 to 156, greedy 47.  One row of 32000, in LDS: 15, 11, 13, 22, 24 and 8 (a call that does nothing: 6); what bounds it is the chain of
 // barriers, scans and sorts on one CU.
 template <int NT, int LIST, bool HELD, bool FOUND>
 __global__ __launch_bounds__(NT, 4) void sample_kernel(Sample c, int vocab, SampleFound found_in) {
@@ -962,6 +962,10 @@ constexpr int SAMPLE_HELD = 32512;         // logits that fit LDS beside the bin
 hipError_t launch_sample(const Sample& c, int rows, int vocab, float* ws, size_t ws_elems, hipStream_t s) {
     if (rows <= 0) return hipSuccess;
     SampleFound w{};
+    // A row held in LDS, one workgroup to a CU, as long as there are no more rows than CUs; beyond, rows read again by workgroups of 512 threads, two or more to a CU.  us held /
+    // read again by 1024 threads / by 512: 256 rows of 32000, top-k 50 16 / 19 / 19, min-p 15 / 19 / 19, top-p 0.9 32 / 34 / 33, top-k 1000 29 / 31 / 46; 257 rows 28 / 31 / 20, 24 / 28 / 18,
+    // 59 / 62 / 43, 56 / 58 / 58; 1024 rows 65 / 72 / 45, 58 / 67 / 43, 126 / 132 / 89, 114 / 119 / 127; 256 rows of 128000 - / 38 / 44, - / 39 / 41, - / 85 / 98, - / 115 / 140; 512 rows - / 73 / 58,
+    // - / 72 / 58, - / 167 / 148, - / 186 / 217 (more wanted than 512 threads sort: the one side on which 1024 win; the settings are not known here).
     if (vocab <= SAMPLE_HELD && rows <= 256) {
         const int lds = ((vocab + 3) & ~3) * 4;
         const hipError_t e = hipFuncSetAttribute((const void*)sample_kernel<1024, 1024, true, false>, hipFuncAttributeMaxDynamicSharedMemorySize,
